@@ -399,6 +399,132 @@ int nnjit_cache_load(const char *path);
  * NNJIT_EINVAL or NNJIT_EHIP. */
 int nnjit_stream_read(const void *src, int64_t bytes, void *sink, int workgroups, void *stream);
 
+/* ------------------------------------------------------- serving a decoder
+ *
+ * What lies between a decoder layer's qkv linear and its output linear when
+ * sequences are served from a cache of their keys and values: rotary
+ * positions, appending the new keys and values, attention over the cache.
+ * (The paper serves whole transformers, Sec. 7.2, and describes products
+ * only; these operators have no counterpart in it.)
+ *
+ * Head rows.  q, k, v and outputs are rows of heads: element (row t, head h,
+ * dim i) of x lies at x[t * x_token + h * x_head + i]; strides are in
+ * elements and >= 0, the dims of a head are contiguous.  Column ranges of one
+ * qkv result are such rows.  Any alignment is served; rows that begin at
+ * multiples of 16 bytes (with head_dim a multiple of 16 bytes' worth) faster.
+ * head_dim is 1 .. 256.
+ *
+ * The structs below are plain descriptions that the caller keeps; the library
+ * reads them during the call only.  Errors, streams, capture and threads as
+ * stated at the top of this file; all pointers in them are DEVICE pointers. */
+
+/* The pool of pages: slot s of page g holds key head h at
+ * k[g * k_page + s * k_token + h * k_head + i], values alike.  Both
+ * [page][slot][head][dim] and [page][head][slot][dim] pools (and views of
+ * larger ones) can be described; a pool may pass 2^32 elements. */
+typedef struct nnjit_paged_kv {
+    void *k, *v;
+    int64_t k_page, k_token, k_head;   /* strides in elements */
+    int64_t v_page, v_token, v_head;
+    int64_t pages, page_size;          /* pages in the pool; tokens a page (any number >= 1) */
+    int64_t kv_heads, head_dim;
+    int dtype;                         /* NNJIT_F32 or NNJIT_F16 */
+} nnjit_paged_kv;
+
+/* The sequences of one step.  Rows q_start[b] .. q_start[b + 1] - 1 are the
+ * new tokens of sequence b (0 = q_start[0] <= q_start[1] <= ...; rows behind
+ * the last sequence are left alone, so a batch may be padded).  kv_len[b]
+ * counts its keys with the new ones: new token i has position kv_len[b] -
+ * (q_start[b + 1] - q_start[b]) + i.  Position p lies in slot p % page_size
+ * of page page_table[b * ld_table + p / page_size]; entries past the last
+ * used page are not used (they may hold anything).
+ * The arrays are read by the kernels, so a captured graph follows them; the
+ * library cannot check them.  The kernels stay inside the cache and the
+ * tensors all the same: a page id outside the pool is not written to and
+ * read as the nearest one, keys past the table's columns do not exist.
+ * max_q and max_kv bound the new tokens and the keys of any one sequence
+ * (rows and keys beyond them may be left out); they size the launch, and a
+ * value much larger than the lengths costs time, not correctness. */
+typedef struct nnjit_paged_batch {
+    int64_t sequences, tokens;         /* tokens: rows of q, k, v and out */
+    const int32_t *q_start;            /* [sequences + 1] */
+    const int32_t *kv_len;             /* [sequences] */
+    const int32_t *page_table;         /* [sequences][ld_table], table_pages used */
+    int64_t ld_table, table_pages;
+    int64_t max_q, max_kv;
+} nnjit_paged_batch;
+
+/* Rotary positions.  table: fp32 [positions][rotary_dim]: for position p the
+ * cos of rotary_dim / 2 pairs, then their sin.  The first rotary_dim dims
+ * (even, <= head_dim) of a head are turned: pairs (i, i + rotary_dim / 2)
+ * (HALF) or (2 i, 2 i + 1) (INTERLEAVED); the others pass unchanged. */
+enum nnjit_rotary_layout { NNJIT_ROTARY_HALF = 0, NNJIT_ROTARY_INTERLEAVED = 1 };
+typedef struct nnjit_rotary_table {
+    const float *table;
+    int64_t positions, rotary_dim;
+    int layout;
+} nnjit_rotary_table;
+
+/* How the frequencies f_i = base^(-2 i / rotary_dim) are changed for contexts
+ * `factor` times as long as the `original` one:
+ *   PLAIN   not
+ *   LINEAR  f_i / factor (positions are interpolated)
+ *   BASE    base times factor^(rotary_dim / (rotary_dim - 2)) (rotary_dim > 2)
+ *   TURNS   by n_i = original f_i / 2 pi, the turns over the original
+ *           context: f_i from n_i = fast on, f_i / factor up to n_i = slow,
+ *           between them the mean weighted linearly in n_i
+ *   INDEX   as TURNS with a ramp that is linear in the pair index i, between
+ *           the indices (rounded outward) whose pairs turn fast and slow times
+ * cos and sin are multiplied by `magnitude`. */
+enum nnjit_rotary_scaling_kind {
+    NNJIT_ROTARY_PLAIN = 0, NNJIT_ROTARY_LINEAR = 1, NNJIT_ROTARY_BASE = 2, NNJIT_ROTARY_TURNS = 3, NNJIT_ROTARY_INDEX = 4
+};
+typedef struct nnjit_rotary_scaling {
+    int kind;
+    double factor, original, fast, slow, magnitude;
+} nnjit_rotary_scaling;
+
+/* Fills a table as above for positions 0 .. positions - 1; angles, cos and
+ * sin are computed in 64 bits and rounded once.  scaling NULL: PLAIN,
+ * magnitude 1.  Asynchronous on stream. */
+int nnjit_rotary_fill(float *table, int64_t positions, int64_t rotary_dim, double base,
+                      const nnjit_rotary_scaling *scaling, void *stream);
+
+/* y = x turned by the angles of each row's position (positions[t], clamped
+ * to the table); transpose != 0: by the opposite angles, which is the
+ * transposed matrix: the gradient of x from that of y.  x and y may have
+ * different types; y may be x (same strides and type).  Turned in fp32 and
+ * rounded once. */
+int nnjit_rotary(const nnjit_rotary_table *rotary, int64_t tokens, int64_t heads, int64_t head_dim, const int32_t *positions,
+                 const void *x, int64_t x_token, int64_t x_head, int x_dtype,
+                 void *y, int64_t y_token, int64_t y_head, int y_dtype, int transpose, void *stream);
+
+/* Writes the new tokens' keys, turned, and values to their slots of the
+ * cache, rounded to its type, and turns the queries of the same rows into
+ * q_out (of the cache's type), in one launch.  k, v: head rows of kv_heads
+ * heads, q: of q_heads heads, all of src_dtype; q_heads == 0: no queries.
+ * rotary NULL: nothing is turned.  Two sequences must not share the pages
+ * that new tokens go to.  max_q and max_kv are not used. */
+int nnjit_kv_append(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch, const nnjit_rotary_table *rotary,
+                    const void *k, int64_t k_token, int64_t k_head, const void *v, int64_t v_token, int64_t v_head,
+                    int64_t q_heads, const void *q, int64_t q_token, int64_t q_head,
+                    void *q_out, int64_t qo_token, int64_t qo_head, int src_dtype, void *stream);
+
+/* out[t, h] = sum_j w_j v[j, h'] with w the softmax over the seen keys j of
+ * scale q[t, h] . k[j, h'], h' = h / (q_heads / kv_heads); q and out are of
+ * the cache's type.  A token at position p sees the keys j < kv_len; with
+ * causal != 0 those with j <= p only, and with window > 0 (causal only) those
+ * with j > p - window only.  A token that sees no key gets zeros.  What lies
+ * in places that a token does not see -- unused slots, other positions' keys
+ * and values, infinities and NaN among them -- does not touch its row.
+ * Softmax statistics and sums are held in fp32; fp16 probabilities are
+ * rounded for the matrix cores (see the kernels).  Results do not depend on
+ * the order in which workgroups run.  The stream's scratch (see "Stream
+ * capture" above) is used when keys are split over workgroups. */
+int nnjit_paged_attention(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch, int64_t q_heads,
+                          const void *q, int64_t q_token, int64_t q_head, void *out, int64_t out_token, int64_t out_head,
+                          float scale, int causal, int64_t window, void *stream);
+
 /* Message for the last error on this thread ("" if none).  The pointer stays
  * valid until the next nnjit_* call on the same thread. */
 const char *nnjit_last_error(void);

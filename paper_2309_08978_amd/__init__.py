@@ -9,7 +9,10 @@ raises instead of falling back to anything else.
 
 ``matmul`` / ``batched_matmul`` are conveniences that take tensors, derive
 (M, N, K), leading dimensions and batch strides from them, call the entry
-point and raise ``NnjitError`` on a negative code.
+point and raise ``NnjitError`` on a negative code.  ``rotary`` /
+``kv_append`` / ``paged_attention`` do the same for the operators of a served
+decoder, with ``RotaryTable``, ``PagedCache`` and ``PagedBatch`` as the
+handles that a program keeps.
 """
 from __future__ import annotations
 
@@ -23,6 +26,8 @@ LIB_PATH = os.path.join(HERE, "libnnjit.so")
 
 NNJIT_F32, NNJIT_F16 = 0, 1
 NNJIT_KIND_GEMM, NNJIT_KIND_BATCHED, NNJIT_KIND_GEMV, NNJIT_KIND_GEMV_Q4 = 0, 1, 2, 3
+NNJIT_ROTARY_HALF, NNJIT_ROTARY_INTERLEAVED = 0, 1
+NNJIT_ROTARY_PLAIN, NNJIT_ROTARY_LINEAR, NNJIT_ROTARY_BASE, NNJIT_ROTARY_TURNS, NNJIT_ROTARY_INDEX = 0, 1, 2, 3, 4
 NNJIT_OK, NNJIT_EINVAL, NNJIT_EDTYPE, NNJIT_ENOCFG, NNJIT_EHIP, NNJIT_ENOMEM = 0, -1, -2, -3, -4, -5
 ERROR_NAMES = {-1: "NNJIT_EINVAL", -2: "NNJIT_EDTYPE", -3: "NNJIT_ENOCFG", -4: "NNJIT_EHIP", -5: "NNJIT_ENOMEM"}
 
@@ -31,7 +36,8 @@ EXPORTED = ["nnjit_matmul", "nnjit_batched_matmul", "nnjit_batched_matmul_noallo
             "nnjit_num_configs", "nnjit_config_info", "nnjit_config_resources", "nnjit_lite_space",
             "nnjit_last_tune_stats", "nnjit_last_tune_stats_ex", "nnjit_last_tune_trace", "nnjit_cached_config", "nnjit_cached_ranked",
             "nnjit_set_online", "nnjit_online_status", "nnjit_cache_clear",
-            "nnjit_cache_save", "nnjit_cache_load", "nnjit_stream_read", "nnjit_last_error", "nnjit_version"]
+            "nnjit_cache_save", "nnjit_cache_load", "nnjit_stream_read", "nnjit_rotary_fill", "nnjit_rotary",
+            "nnjit_kv_append", "nnjit_paged_attention", "nnjit_last_error", "nnjit_version"]
 
 
 class NnjitError(RuntimeError):
@@ -57,6 +63,28 @@ class TuneStats(ctypes.Structure):
                 ("n_lite", ctypes.c_int), ("n_timed", ctypes.c_int), ("n_aborted", ctypes.c_int),
                 ("n_failed", ctypes.c_int), ("chosen", ctypes.c_int), ("best_us", ctypes.c_double),
                 ("default_us", ctypes.c_double), ("cache_hit", ctypes.c_int)]
+
+
+class PagedKvDesc(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + [
+        (n, ctypes.c_int64) for n in ("k_page", "k_token", "k_head", "v_page", "v_token", "v_head", "pages", "page_size",
+                                      "kv_heads", "head_dim")] + [("dtype", ctypes.c_int)]
+
+
+class PagedBatchDesc(ctypes.Structure):
+    _fields_ = [("sequences", ctypes.c_int64), ("tokens", ctypes.c_int64), ("q_start", ctypes.c_void_p),
+                ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p)] + [
+        (n, ctypes.c_int64) for n in ("ld_table", "table_pages", "max_q", "max_kv")]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("positions", ctypes.c_int64), ("rotary_dim", ctypes.c_int64),
+                ("layout", ctypes.c_int)]
+
+
+class RotaryScaling(ctypes.Structure):
+    """nnjit_rotary_scaling: RotaryScaling(kind, factor, original, fast, slow, magnitude)."""
+    _fields_ = [("kind", ctypes.c_int)] + [(n, ctypes.c_double) for n in ("factor", "original", "fast", "slow", "magnitude")]
 
 
 def mi355x_limits() -> DeviceLimits:
@@ -112,6 +140,10 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
             "nnjit_cache_save": [ctypes.c_char_p],
             "nnjit_cache_load": [ctypes.c_char_p],
             "nnjit_stream_read": [vp, i64, vp, ci, vp],
+            "nnjit_rotary_fill": [vp, i64, i64, ctypes.c_double, vp, vp],
+            "nnjit_rotary": [vp, i64, i64, i64, vp, vp, i64, i64, ci, vp, i64, i64, ci, ci, vp],
+            "nnjit_kv_append": [vp, vp, vp, vp, i64, i64, vp, i64, i64, i64, vp, i64, i64, vp, i64, i64, ci, vp],
+            "nnjit_paged_attention": [vp, vp, i64, vp, i64, i64, vp, i64, i64, ctypes.c_float, ci, i64, vp],
             "nnjit_last_error": [],
             "nnjit_version": [],
         }
@@ -282,6 +314,36 @@ def nnjit_cache_load(path) -> int:
 
 def nnjit_stream_read(src, nbytes, sink, workgroups, stream=None) -> int:
     return load().nnjit_stream_read(_ptr(src), nbytes, _ptr(sink), workgroups, _stream(stream))
+
+
+def _desc(d) -> Optional[int]:
+    """Address of a descriptor: a handle, a ctypes structure, an int or None."""
+    if d is None or isinstance(d, int):
+        return d
+    return ctypes.addressof(getattr(d, "desc", d))
+
+
+def nnjit_rotary_fill(table, positions, rotary_dim, base, scaling=None, stream=None) -> int:
+    return load().nnjit_rotary_fill(_ptr(table), positions, rotary_dim, base, _desc(scaling), _stream(stream))
+
+
+def nnjit_rotary(rotary, tokens, heads, head_dim, positions, x, x_token, x_head, x_dtype, y, y_token, y_head, y_dtype,
+                 transpose=0, stream=None) -> int:
+    return load().nnjit_rotary(_desc(rotary), tokens, heads, head_dim, _ptr(positions), _ptr(x), x_token, x_head, x_dtype,
+                               _ptr(y), y_token, y_head, y_dtype, transpose, _stream(stream))
+
+
+def nnjit_kv_append(cache, batch, rotary, k, k_token, k_head, v, v_token, v_head, q_heads, q, q_token, q_head, q_out,
+                    qo_token, qo_head, src_dtype, stream=None) -> int:
+    return load().nnjit_kv_append(_desc(cache), _desc(batch), _desc(rotary), _ptr(k), k_token, k_head, _ptr(v), v_token,
+                                  v_head, q_heads, _ptr(q), q_token, q_head, _ptr(q_out), qo_token, qo_head, src_dtype,
+                                  _stream(stream))
+
+
+def nnjit_paged_attention(cache, batch, q_heads, q, q_token, q_head, out, out_token, out_head, scale, causal=1, window=0,
+                          stream=None) -> int:
+    return load().nnjit_paged_attention(_desc(cache), _desc(batch), q_heads, _ptr(q), q_token, q_head, _ptr(out), out_token,
+                                        out_head, scale, causal, window, _stream(stream))
 
 
 def nnjit_last_error() -> str:
@@ -501,6 +563,213 @@ def gemv_q4(x, Wq, scales, group: int, N: int, y=None, stream=None, cfg: Optiona
     else:
         check(nnjit_gemv_q4_config(cfg, N, K, group, x, Wq, ldq, scales, lds, y, stream))
     return y
+
+
+def _separate(name: str, t):
+    """Reject a tensor that is written to if elements of it share memory."""
+    room = 1
+    for stride, size in sorted((t.stride(i), t.shape[i]) for i in range(t.dim())):
+        if size > 1:
+            if stride < room:
+                raise ValueError(f"elements of {name} overlap: shape {tuple(t.shape)}, strides {tuple(t.stride())}")
+            room = stride * (size - 1) + room
+    return t
+
+
+def _on_one_gpu(**tensors):
+    devs = {t.device for t in tensors.values()}
+    if len(devs) != 1 or next(iter(devs)).type != "cuda":
+        raise ValueError(f"{', '.join(tensors)} must be on one GPU, got {sorted(str(d) for d in devs)}")
+
+
+def _unit_dims(name: str, t):
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must have unit stride along the last dimension")
+
+
+def _int32(name: str, t, *shape):
+    import torch
+    if t.dtype != torch.int32 or t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
+        raise ValueError(f"{name} must be int32 of shape {shape}, got {t.dtype} {tuple(t.shape)}")
+    if t.dim() == 1 and t.shape[0] > 1 and t.stride(0) != 1:
+        raise ValueError(f"{name} must be contiguous")
+
+
+class RotaryTable:
+    """Cos and sin of rotary positions: ``table`` fp32 [positions, rotary_dim]
+    (per position the cos of every pair, then their sin), ``layout`` 'half'
+    (pairs i, i + rotary_dim / 2) or 'interleaved' (pairs 2 i, 2 i + 1)."""
+
+    def __init__(self, table, layout: str = "half"):
+        import torch
+        if layout not in ("half", "interleaved"):
+            raise ValueError(f"layout must be 'half' or 'interleaved', got {layout!r}")
+        if table.dtype != torch.float32 or table.dim() != 2 or table.shape[0] < 1 or table.shape[1] < 2 or table.shape[1] % 2:
+            raise ValueError(f"table must be float32 [positions, even rotary_dim], got {table.dtype} {tuple(table.shape)}")
+        if not table.is_contiguous():
+            raise ValueError("table must be contiguous")
+        _on_one_gpu(table=table)
+        self.table, self.layout = table, layout
+        self.rotary_dim, self.device_index = int(table.shape[1]), table.get_device()
+        self.desc = RotaryDesc(table.data_ptr(), table.shape[0], table.shape[1],
+                               NNJIT_ROTARY_HALF if layout == "half" else NNJIT_ROTARY_INTERLEAVED)
+        self.address = ctypes.addressof(self.desc)
+
+
+def rotary_table(positions: int, rotary_dim: int, base: float = 10000.0, layout: str = "half",
+                 scaling: Optional[RotaryScaling] = None, device="cuda", stream=None) -> RotaryTable:
+    """A RotaryTable for positions 0 .. positions - 1 (nnjit_rotary_fill)."""
+    import torch
+    table = torch.empty((positions, rotary_dim), dtype=torch.float32, device=device)
+    with torch.cuda.device(table.device):
+        check(nnjit_rotary_fill(table, positions, rotary_dim, base, scaling, stream))
+    return RotaryTable(table, layout)
+
+
+class PagedCache:
+    """A pool of pages of keys and values: ``k`` and ``v`` fp32 or fp16
+    [pages, page_size, kv_heads, head_dim], any strides with contiguous dims
+    (a [pages, kv_heads, page_size, head_dim] pool is passed as its
+    ``transpose(1, 2)``)."""
+
+    def __init__(self, k, v):
+        torch = _torch()
+        for name, t in (("k", k), ("v", v)):
+            if t.dim() != 4 or 0 in t.shape:
+                raise ValueError(f"{name} must be [pages, page_size, kv_heads, head_dim], got {tuple(t.shape)}")
+            if t.dtype not in _CODES:
+                raise TypeError(f"unsupported dtype {t.dtype}")
+            _unit_dims(name, t)
+            _separate(name, t)
+        if k.shape != v.shape or k.dtype != v.dtype:
+            raise ValueError(f"k is {k.dtype} {tuple(k.shape)} but v is {v.dtype} {tuple(v.shape)}")
+        _on_one_gpu(k=k, v=v)
+        self.k, self.v, self.dtype, self.device_index = k, v, k.dtype, k.get_device()
+        pages, page_size, self.kv_heads, self.head_dim = k.shape
+        self.desc = PagedKvDesc(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), v.stride(0), v.stride(1),
+                                v.stride(2), pages, page_size, self.kv_heads, self.head_dim, _CODES[k.dtype])
+        self.address = ctypes.addressof(self.desc)
+
+
+class PagedBatch:
+    """The sequences of one step (nnjit_paged_batch): ``q_start`` int32
+    [sequences + 1], ``kv_len`` int32 [sequences], ``page_table`` int32
+    [sequences, columns], all on the GPU; ``tokens`` rows of q, k, v and out;
+    ``max_q`` / ``max_kv`` bound the new tokens and keys of a sequence (default:
+    all rows; all that the table's columns hold)."""
+
+    def __init__(self, q_start, kv_len, page_table, tokens: int, max_q: Optional[int] = None, max_kv: Optional[int] = None):
+        sequences = int(kv_len.shape[0]) if kv_len.dim() == 1 else -1
+        _int32("kv_len", kv_len, max(sequences, 0))
+        _int32("q_start", q_start, sequences + 1)
+        _int32("page_table", page_table, sequences, None)
+        _unit_dims("page_table", page_table)
+        if sequences > 1 and page_table.stride(0) < page_table.shape[1]:
+            raise ValueError("rows of page_table overlap")
+        _on_one_gpu(q_start=q_start, kv_len=kv_len, page_table=page_table)
+        self.q_start, self.kv_len, self.page_table = q_start, kv_len, page_table
+        self.tokens, self.device_index = int(tokens), q_start.get_device()
+        self.desc = PagedBatchDesc(sequences, tokens, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
+                                   max(page_table.stride(0), page_table.shape[1]), page_table.shape[1],
+                                   tokens if max_q is None else max_q, 1 << 30 if max_kv is None else max_kv)
+        self.address = ctypes.addressof(self.desc)
+
+
+def _head_rows(name: str, t, tokens, heads, dim, dtype, device_index):
+    """Strides (token, head) of head rows, checked."""
+    if t.dim() != 3 or t.shape[0] != tokens or (heads is not None and t.shape[1] != heads) or t.shape[2] != dim:
+        raise ValueError(f"{name} must be [{tokens}, {'heads' if heads is None else heads}, {dim}], got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    st = t.stride()
+    if st[2] != 1 and dim > 1:
+        raise ValueError(f"{name} must have unit stride along the last dimension")
+    if not t.is_cuda or t.get_device() != device_index:
+        raise ValueError(f"{name} must be on one GPU with the other operands, got {t.device}")
+    return st
+
+
+def _written_rows(name: str, t, tokens, heads, dim, dtype, device_index):
+    st = _head_rows(name, t, tokens, heads, dim, dtype, device_index)
+    if not (st[1] >= dim and st[0] >= st[1] * heads):     # plain rows need no closer look
+        _separate(name, t)
+    return st
+
+
+def rotary(x, positions, table: RotaryTable, out=None, transpose: bool = False, stream=None):
+    """x [tokens, heads, head_dim] turned by the angles of positions (int32
+    [tokens]); ``transpose``: by the opposite ones (the gradient).  ``out``
+    (fp32 or fp16, allocated like x if None) may be x."""
+    torch = _torch()
+    if x.dim() != 3:
+        raise ValueError(f"x must be [tokens, heads, head_dim], got {tuple(x.shape)}")
+    tokens, heads, dim = x.shape
+    if out is None:
+        out = torch.empty((tokens, heads, dim), dtype=x.dtype, device=x.device)
+    if x.dtype not in _CODES or out.dtype not in _CODES:
+        raise TypeError(f"unsupported dtype {x.dtype} to {out.dtype}")
+    sx = _head_rows("x", x, tokens, heads, dim, x.dtype, table.device_index)
+    sy = _written_rows("out", out, tokens, heads, dim, out.dtype, table.device_index)
+    if positions.shape != (tokens,) or positions.dtype is not torch.int32 or positions.get_device() != table.device_index:
+        raise ValueError(f"positions must be int32 of shape ({tokens},) on x's GPU, got {positions.dtype} {tuple(positions.shape)}")
+    if tokens > 1 and positions.stride(0) != 1:
+        raise ValueError("positions must be contiguous")
+    check((_lib or load()).nnjit_rotary(table.address, tokens, heads, dim, positions.data_ptr(), x.data_ptr(), sx[0], sx[1],
+                                        _CODES[x.dtype], out.data_ptr(), sy[0], sy[1], _CODES[out.dtype],
+                                        1 if transpose else 0, _stream(stream)))
+    return out
+
+
+def kv_append(cache: PagedCache, batch: PagedBatch, k, v, rotary: Optional[RotaryTable] = None, q=None, q_out=None,
+              stream=None):
+    """Writes k (turned) and v [tokens, kv_heads, head_dim], fp32 or fp16, to
+    the batch's slots of the cache; turns q [tokens, heads, head_dim] of the
+    same type into q_out (of the cache's type, allocated if None), which is
+    returned (None without q)."""
+    torch = _torch()
+    n, dim, dev = batch.tokens, cache.head_dim, cache.device_index
+    dt = k.dtype
+    if dt not in _CODES:
+        raise TypeError(f"unsupported dtype {dt}")
+    if batch.device_index != dev or (rotary is not None and rotary.device_index != dev):
+        raise ValueError("cache, batch and rotary must be on one GPU")
+    sk = _head_rows("k", k, n, cache.kv_heads, dim, dt, dev)
+    sv = _head_rows("v", v, n, cache.kv_heads, dim, dt, dev)
+    heads, sq, so, qp, op = 0, (0, 0), (0, 0), None, None
+    if q is not None:
+        heads = q.shape[1] if q.dim() == 3 else -1
+        sq = _head_rows("q", q, n, heads, dim, dt, dev)
+        if q_out is None:
+            q_out = torch.empty((n, heads, dim), dtype=cache.dtype, device=q.device)
+        so = _written_rows("q_out", q_out, n, heads, dim, cache.dtype, dev)
+        qp, op = q.data_ptr(), q_out.data_ptr()
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    check((_lib or load()).nnjit_kv_append(cache.address, batch.address, None if rotary is None else rotary.address,
+                                           k.data_ptr(), sk[0], sk[1], v.data_ptr(), sv[0], sv[1], heads, qp, sq[0], sq[1],
+                                           op, so[0], so[1], _CODES[dt], _stream(stream)))
+    return q_out
+
+
+def paged_attention(q, cache: PagedCache, batch: PagedBatch, out=None, scale: Optional[float] = None, causal: bool = True,
+                    window: int = 0, stream=None):
+    """Attention of q [tokens, heads, head_dim] over the cached keys and values
+    of every row's sequence; q and out are of the cache's type.  ``scale``
+    defaults to head_dim ** -0.5; ``window`` > 0: the last ``window`` keys only."""
+    torch = _torch()
+    if q.dim() != 3:
+        raise ValueError(f"q must be [tokens, heads, head_dim], got {tuple(q.shape)}")
+    heads, dim, dev = q.shape[1], cache.head_dim, cache.device_index
+    if batch.device_index != dev:
+        raise ValueError("cache and batch must be on one GPU")
+    sq = _head_rows("q", q, batch.tokens, heads, dim, cache.dtype, dev)
+    if out is None:
+        out = torch.empty((batch.tokens, heads, dim), dtype=cache.dtype, device=q.device)
+    so = _written_rows("out", out, batch.tokens, heads, dim, cache.dtype, dev)
+    check((_lib or load()).nnjit_paged_attention(cache.address, batch.address, heads, q.data_ptr(), sq[0], sq[1],
+                                                 out.data_ptr(), so[0], so[1], dim ** -0.5 if scale is None else scale,
+                                                 1 if causal else 0, window, _stream(stream)))
+    return out
 
 
 def configs() -> list:

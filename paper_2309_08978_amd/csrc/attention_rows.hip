@@ -1,0 +1,505 @@
+// Attention over a paged cache for few rows (decode): tiles of 16 rows.
+//
+//   o[r] = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale q_r . k_j - m)
+//
+// in one pass over the keys with a running maximum m and sum.  A decode step
+// reads every key and value once for a handful of multiplications each:
+// bandwidth-bound, so the kernel keeps loads in flight and everything else in
+// registers.
+//
+// Each wave takes key tiles of its own (KT keys: 32 in fp16, 16 in fp32) for
+// all 16 rows and multiplies them on the matrix cores, straight from the
+// registers that the loads fill, without LDS or barriers:
+//
+//   S^T = K Q^T   (16 keys x 16 rows a product: lane c = lane % 16 loads the
+//                 16 bytes at chunk g = lane / 16 of key c, so lane (c, g)
+//                 receives row c's logits of the keys 4 g + j, j = 0 .. 3)
+//   O^T = V^T P^T (the probabilities are the second operand exactly as they
+//                 lie: lane (c, g) holds row c, keys 4 g + j.  The first
+//                 operand wants dims along c and the same keys: lane (c, g)
+//                 loads the VE consecutive dims VE c .. of keys 4 g + j -- 16
+//                 lanes read a whole value row -- and element e of them is
+//                 the operand of product e, which gives dims VE m + e)
+//
+// so lane (c, g) ends up with 4 VE consecutive dims of row c, next to row c's
+// maximum and sum: rescaling needs no exchange, the maximum two shuffles a
+// tile.  In fp16 the eight keys of an operand are gathered from eight loaded
+// vectors by byte permutes.  Probabilities go into the products in two fp16
+// parts (p = hi + lo, 22 bits): matrix cores have nothing else to do here.
+//
+// The waves of a workgroup are joined through LDS at the end.  Keys are split
+// over workgroups where sequences and key heads alone leave the chip idle; a
+// second kernel joins the splits in their order, so results do not depend on
+// which workgroup finishes first.
+#include <algorithm>
+
+#include "attention_common.h"
+#include "../../include/nnjit.h"
+
+namespace nnjit {
+
+namespace {
+
+template <typename T> struct RowsOf;
+template <> struct RowsOf<_Float16> {
+    static constexpr int KT = 32;               // keys of a wave's tile
+    static constexpr int CH = 8;                // elements of a 16-byte chunk
+    typedef f16x8 chunk;
+};
+template <> struct RowsOf<float> {
+    static constexpr int KT = 16;
+    static constexpr int CH = 4;
+    typedef f32x4 chunk;
+};
+
+// n consecutive elements, of which those at or past `valid` are zero
+template <typename V, bool VEC, typename T>
+__device__ __forceinline__ V load_some(const T *src, int valid, int n)
+{
+    if constexpr (VEC) {
+        V v = {};
+        if (valid > 0) v = *(const V *)src;     // valid is a multiple of n here
+        return v;
+    } else {
+        V v;
+        for (int i = 0; i < n; ++i) v[i] = i < valid ? src[i] : (T)0;
+        return v;
+    }
+}
+
+template <typename T, int DP, bool VEC, bool PAGE16, int NW>
+__global__ void __launch_bounds__(NW * 64)
+attention_rows_kernel(AttentionParams p)
+{
+    typedef RowsOf<T> R;
+    constexpr bool HALF = sizeof(T) == 2;
+    constexpr int KT = R::KT, CH = R::CH, SUB = KT / 16;
+    typedef typename R::chunk chunk;
+    constexpr int STEPS = DP / (4 * CH);                  // chunks of a key per lane
+    constexpr int VE = DP / 16 < CH ? DP / 16 : CH;       // dims of a value vector
+    constexpr int VH = DP / (16 * VE);                    // value vectors of a key per lane
+    constexpr int BLK = DP / 16;                          // products (of 16 dims) of a tile
+    typedef T vvec __attribute__((ext_vector_type(VE)));
+
+    __shared__ __attribute__((aligned(16))) float lds_o[NW][16][DP + 4];
+    __shared__ float lds_m[NW][16], lds_l[NW][16];
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = lane & 15, g = lane >> 4;
+
+    int id = xcd_remap(blockIdx.x, gridDim.x);
+    const int tile = id % p.row_tiles;
+    id /= p.row_tiles;
+    const int split = id % p.splits;
+    id /= p.splits;
+    const int kv_heads = p.q_heads / p.group;
+    const int head = id % kv_heads;
+    const int seq = id / kv_heads;
+    const RowTile t = row_tile(p, seq, tile, 16);
+    if (t.rows <= 0) return;
+
+    // keys of the tile's rows, and of this split
+    const int r_last = t.r0 + t.rows - 1;
+    const int lo_min = t.first_key(p, t.r0), lo_max = t.first_key(p, r_last);
+    const int hi_min = t.end_key(p, t.r0), hi_max = t.end_key(p, r_last);
+    const int base = lo_min & ~31;
+    const long long begin = base + (long long)split * p.split_keys;
+    const int k0 = (int)min(begin, (long long)hi_max);
+    const int k1 = (int)min(begin + p.split_keys, (long long)hi_max);
+    const bool rows_differ = lo_min != lo_max || hi_min != hi_max;
+
+    // this lane's row (rows past the tile's repeat its last one; not stored)
+    const int r = min(t.r0 + c, r_last);
+    const int token = t.q0 + p.group_div.quot(r);
+    const int q_head = head * p.group + r - p.group_div.quot(r) * p.group;
+    const int lo = max(t.first_key(p, r), k0), hi = min(t.end_key(p, r), k1);
+
+    chunk q[STEPS];
+    {
+        const T *src = (const T *)p.q.p + (long long)token * p.q.tok + (long long)q_head * p.q.head;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            const int d = (4 * s + g) * CH;
+            q[s] = load_some<chunk, VEC>(src + d, p.dim - d, CH);
+            if (p.negate) q[s] = -q[s];
+        }
+    }
+
+    const T *kp = (const T *)p.pool.k + (long long)head * p.pool.k_head;
+    const T *vp = (const T *)p.pool.v + (long long)head * p.pool.v_head;
+    const int page_size = p.pool.page_size.d;
+    const int last_key = max(hi_max - 1, 0);
+
+    // page ids of a tile's keys: per 16 keys where pages hold multiples of 16
+    // (one scalar load each), else for the keys that the lane loads
+    constexpr int IDS_K = SUB, IDS_V = PAGE16 ? 0 : SUB * 4;
+    struct Ids {
+        int k[IDS_K], v[IDS_V > 0 ? IDS_V : 1];
+    };
+    auto ids_of = [&](int kt) {
+        Ids ids;
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+            const int key = min(kt + 16 * s + (PAGE16 ? 0 : c), last_key);
+            ids.k[s] = t.table[p.pool.page_size.quot(key)];
+        }
+        if constexpr (!PAGE16) {
+#pragma unroll
+            for (int i = 0; i < SUB * 4; ++i) {
+                const int key = min(kt + 16 * (i / 4) + 4 * g + i % 4, last_key);
+                ids.v[i] = t.table[p.pool.page_size.quot(key)];
+            }
+        }
+        return ids;
+    };
+    // slot of a key; keys past the last one are read at some slot of the last
+    // page (PAGE16) or as the last key, and masked
+    auto slot_of = [&](int sub_key, int within) {
+        if constexpr (PAGE16) return sub_key - p.pool.page_size.quot(sub_key) * page_size + within;
+        const int key = min(sub_key + within, last_key);
+        return key - p.pool.page_size.quot(key) * page_size;
+    };
+
+    chunk kreg[SUB][STEPS];
+    vvec vreg[SUB * 4][VH];
+    auto load_k = [&](const Ids &ids, int kt) {
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+            const T *row = kp + (long long)safe_page(p, ids.k[s]) * p.pool.k_page + (long long)slot_of(kt + 16 * s, c) * p.pool.k_tok;
+#pragma unroll
+            for (int e = 0; e < STEPS; ++e) {
+                const int d = (4 * e + g) * CH;
+                kreg[s][e] = load_some<chunk, VEC>(row + d, p.dim - d, CH);
+            }
+        }
+    };
+    auto load_v = [&](const Ids &ids, int kt) {
+#pragma unroll
+        for (int i = 0; i < SUB * 4; ++i) {
+            const int s = i / 4;
+            const T *row = vp + (long long)safe_page(p, PAGE16 ? ids.k[s] : ids.v[i]) * p.pool.v_page +
+                           (long long)slot_of(kt + 16 * s, 4 * g + i % 4) * p.pool.v_tok;
+#pragma unroll
+            for (int h = 0; h < VH; ++h) {
+                const int d = h * 16 * VE + c * VE;
+                vreg[i][h] = load_some<vvec, VEC>(row + d, p.dim - d, VE);
+            }
+        }
+    };
+
+    f32x4 acc[BLK];
+#pragma unroll
+    for (int b = 0; b < BLK; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -__builtin_inff(), l = 0.f;
+    const float scale = p.scale_log2;
+
+    const int tiles = (k1 - k0 + KT - 1) / KT;
+    Ids ids;
+    if (wave < tiles) {
+        ids = ids_of(k0 + wave * KT);
+        load_k(ids, k0 + wave * KT);
+        load_v(ids, k0 + wave * KT);
+        ids = ids_of(k0 + (wave + NW) * KT);
+    }
+    for (int it = wave; it < tiles; it += NW) {
+        const int kt = k0 + it * KT;
+        const int kn = kt + NW * KT;
+        const bool more = it + NW < tiles;
+        f32x4 x[SUB];
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+            x[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < STEPS; ++e) {
+                if constexpr (HALF) {
+                    x[s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kreg[s][e], q[e], x[s], 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[s] = __builtin_amdgcn_mfma_f32_16x16x4f32(kreg[s][e][i], q[e][i], x[s], 0, 0, 0);
+                }
+            }
+        }
+        if (more) load_k(ids, kn);
+
+        const bool whole = kt >= lo_max && kt + KT <= min(hi_min, k1);
+        unsigned seen = ~0u;
+        if (!whole) {
+            seen = 0;
+#pragma unroll
+            for (int i = 0; i < SUB * 4; ++i) {
+                const int key = kt + 16 * (i / 4) + 4 * g + i % 4;
+                const bool see = key >= lo && key < hi;
+                x[i / 4][i % 4] = see ? x[i / 4][i % 4] : -__builtin_inff();
+                seen |= see ? 1u << i : 0u;
+                // keys that no row of the tile sees: whatever lies there
+                const bool any = key >= max(lo_min, k0) && key < k1;
+#pragma unroll
+                for (int h = 0; h < VH; ++h)
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) vreg[i][h][e] = any ? vreg[i][h][e] : (T)0;
+            }
+        }
+
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < SUB * 4; ++i) top = fmaxf(top, x[i / 4][i % 4]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float off = top == -__builtin_inff() ? 0.f : top * scale;   // a row that has seen nothing yet
+        const float shrink = exp2_fast(m * scale - off);
+        m = top;
+        float pr[SUB * 4], sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < SUB * 4; ++i) {
+            pr[i] = exp2_fast(fmaf(x[i / 4][i % 4], scale, -off));
+            sum += pr[i];
+        }
+        l = l * shrink + sum;
+#pragma unroll
+        for (int b = 0; b < BLK; ++b) acc[b] *= shrink;
+
+        if constexpr (HALF) {
+            // an infinity times the second part of a probability, which may be zero or
+            // negative, is a NaN: a tile with values that are not finite is taken carefully
+            Largest16 largest;
+#pragma unroll
+            for (int i = 0; i < SUB * 4; ++i)
+#pragma unroll
+                for (int h = 0; h < VH; ++h) largest.take(vreg[i][h]);
+            const bool careful = __any(!largest.finite());
+            f16x8 hi8, lo8, vis8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                hi8[i] = (_Float16)pr[i];
+                lo8[i] = (_Float16)(pr[i] - (float)hi8[i]);
+                vis8[i] = (_Float16)((seen >> i & 1) ? 1.f : 0.f);
+            }
+#pragma unroll
+            for (int b = 0; b < BLK; ++b) {
+                f16x8 v;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = vreg[i][b / VE][b % VE];
+                if (careful) {
+                    f16x8 cls;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        cls[i] = class_of(v[i]);
+                        v[i] = finite(v[i]) ? v[i] : (_Float16)0.f;
+                    }
+                    const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_f16(cls, vis8, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[b][j] = add_classes(acc[b][j], n[j]);
+                }
+                acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, hi8, acc[b], 0, 0, 0);
+                acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, lo8, acc[b], 0, 0, 0);
+            }
+        } else {
+            const bool careful = !whole && rows_differ;
+#pragma unroll
+            for (int b = 0; b < BLK; ++b) {
+                float v[4];
+                bool bad = false;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[j] = vreg[j][b / VE][b % VE];
+                    bad |= !finite(v[j]);
+                }
+                if (careful && __any(bad)) {
+                    f32x4 n = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        n = __builtin_amdgcn_mfma_f32_16x16x4f32(class_of(v[j]), (seen >> j & 1) ? 1.f : 0.f, n, 0, 0, 0);
+                        v[j] = finite(v[j]) ? v[j] : 0.f;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[b][j] = add_classes(acc[b][j], n[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j], pr[j], acc[b], 0, 0, 0);
+            }
+        }
+        if (more) {
+            load_v(ids, kn);
+            ids = ids_of(kn + NW * KT);
+        }
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+
+    // join the waves: weights exp2(m_w - M) of their sums
+    if (g == 0) {
+        lds_m[wave][c] = m * scale;
+        lds_l[wave][c] = l;
+    }
+    if (c < t.rows) {
+#pragma unroll
+        for (int h = 0; h < VH; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < VE; ++e) lds_o[wave][c][h * 16 * VE + (4 * g + j) * VE + e] = acc[h * VE + e][j];
+    }
+    __syncthreads();
+    const int dim = p.dim;
+    constexpr int QUADS = DP / 4;
+    for (int i = threadIdx.x; i < t.rows * QUADS; i += NW * 64) {
+        const int row = i / QUADS, d = (i % QUADS) * 4;
+        if (d >= dim) continue;
+        float most = -__builtin_inff();
+#pragma unroll
+        for (int w = 0; w < NW; ++w) most = fmaxf(most, lds_m[w][row]);
+        const float off = most == -__builtin_inff() ? 0.f : most;
+        float total = 0.f;
+        f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float weight = exp2_fast(lds_m[w][row] - off);
+            total += weight * lds_l[w][row];
+            o += weight * *(const f32x4 *)&lds_o[w][row][d];
+        }
+        const int rr = t.r0 + row, tok = p.group_div.quot(rr);
+        const int oh = head * p.group + rr - tok * p.group;
+        const bool sees = min(t.end_key(p, rr), k1) > max(t.first_key(p, rr), k0);
+        if (p.splits == 1) {
+            // a row without a key is 0; one whose logits are all -inf is 0 / 0
+            T *dst = (T *)p.o.p + (long long)(t.q0 + tok) * p.o.tok + (long long)oh * p.o.head + d;
+            typedef T quad __attribute__((ext_vector_type(4)));
+            quad out;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[e] = (T)(sees ? o[e] / total : 0.f);
+            if constexpr (VEC) {
+                *(quad *)dst = out;
+            } else {
+                for (int e = 0; e < 4 && d + e < dim; ++e) dst[e] = out[e];
+            }
+        } else {
+            const long long at = ((long long)split * p.batch.tokens + t.q0 + tok) * p.q_heads + oh;
+            float *dst = p.part + at * dim + d;
+            for (int e = 0; e < 4; ++e)
+                if (d + e < dim) dst[e] = o[e];
+            if (d == 0) {
+                // a sum that is a NaN stays one in the join (weight exp2(inf - inf));
+                // keys seen, but only logits of -inf: 0 / 0 unless another split has more
+                p.stat[at * 2] = total != total ? __builtin_inff() : most;
+                p.stat[at * 2 + 1] = sees && total == 0.f ? __builtin_nanf("") : total;
+            }
+        }
+    }
+}
+
+// Joins the splits of every row: o = sum_s w_s o_s / sum_s w_s l_s, w_s = exp2(m_s - M).
+// One workgroup a row; wave w takes the splits w, w + NW, ...; the waves are added in order.
+template <typename T, int NW>
+__global__ void __launch_bounds__(NW * 64)
+attention_join_kernel(AttentionParams p)
+{
+    __shared__ float lds_o[NW][kMaxHeadDim], lds_l[NW];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long rows = (long long)p.batch.tokens * p.q_heads;
+    const long long row = blockIdx.x;
+    const int token = (int)(row / p.q_heads), head = (int)(row % p.q_heads);
+    if (token < p.batch.q_start[0] || token >= p.batch.q_start[p.batch.sequences]) return;   // no sequence's
+
+    float most = -__builtin_inff();
+    bool none = false;
+    for (int s = lane; s < p.splits; s += 64) {
+        const float *st = p.stat + (s * rows + row) * 2;
+        most = fmaxf(most, st[0]);
+        none |= st[1] != st[1];
+    }
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) most = fmaxf(most, __shfl_xor(most, i));
+    const bool any_none = __any(none);
+    const float off = most == -__builtin_inff() ? 0.f : most;
+
+    constexpr int E = kMaxHeadDim / 64;
+    float o[E] = {}, total = 0.f;
+    for (int s = wave; s < p.splits; s += NW) {
+        const long long at = s * rows + row;
+        const float sm = p.stat[at * 2];
+        if (sm == -__builtin_inff()) continue;           // has seen nothing
+        const float w = exp2_fast(sm - off);
+        total += w * p.stat[at * 2 + 1];
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e * 64 + lane < p.dim) o[e] += w * p.part[at * p.dim + e * 64 + lane];
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) lds_o[wave][e * 64 + lane] = o[e];
+    if (lane == 0) lds_l[wave] = total;
+    __syncthreads();
+    if (threadIdx.x < (unsigned)p.dim) {
+        float sum = 0.f, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            sum += lds_o[w][threadIdx.x];
+            l += lds_l[w];
+        }
+        const bool empty = most == -__builtin_inff();
+        ((T *)p.o.p)[(long long)token * p.o.tok + (long long)head * p.o.head + threadIdx.x] =
+            (T)(empty ? (any_none ? __builtin_nanf("") : 0.f) : sum / l);
+    }
+}
+
+template <typename T, int DP, bool VEC>
+hipError_t launch_rows(const AttentionParams &p, int grid, hipStream_t stream)
+{
+    constexpr int NW = 4;
+    if (p.pool.page_size.d % 16 == 0) attention_rows_kernel<T, DP, VEC, true, NW><<<grid, NW * 64, 0, stream>>>(p);
+    else attention_rows_kernel<T, DP, VEC, false, NW><<<grid, NW * 64, 0, stream>>>(p);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_typed(const AttentionParams &p, bool vec, int grid, hipStream_t stream)
+{
+    hipError_t e;
+    if (!vec) e = p.dim <= 128 ? launch_rows<T, 128, false>(p, grid, stream) : launch_rows<T, 256, false>(p, grid, stream);
+    else if (p.dim <= 64) e = launch_rows<T, 64, true>(p, grid, stream);
+    else if (p.dim <= 128) e = launch_rows<T, 128, true>(p, grid, stream);
+    else e = launch_rows<T, 256, true>(p, grid, stream);
+    if (e != hipSuccess || p.splits == 1) return e;
+    attention_join_kernel<T, 4><<<(unsigned)(p.batch.tokens * p.q_heads), 256, 0, stream>>>(p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+AttentionPlan attention_plan(int dtype, int64_t tokens, int64_t sequences, int q_heads, int kv_heads, int dim, int64_t max_q,
+                             int64_t max_kv, int causal, int64_t window, int cus)
+{
+    AttentionPlan plan{};
+    const int64_t group = q_heads / kv_heads;
+    const int64_t tile_rows = 16, wave_keys = dtype == NNJIT_F16 ? 32 : 16;
+    plan.row_tiles = (int)((max_q * group + tile_rows - 1) / tile_rows);
+    // keys that one tile can see: with a window, from the first row's first key
+    // (rounded down to a multiple of 32) to the last row's last
+    int64_t span = max_kv;
+    if (causal && window > 0) {
+        const int64_t tokens_of_tile = (tile_rows + group - 1) / group + 1;
+        if (window < span && tokens_of_tile < span) span = std::min(span, window + tokens_of_tile + 31);
+    }
+    const int64_t groups = (int64_t)plan.row_tiles * kv_heads * sequences;
+    // two workgroups a compute unit, each wave with a tile of its own at least
+    int64_t splits = (2 * (int64_t)cus + groups - 1) / groups;
+    splits = std::min(splits, (span + 4 * wave_keys - 1) / (4 * wave_keys));
+    splits = std::max<int64_t>(splits, 1);
+    const int64_t per = (span + splits - 1) / splits;
+    plan.split_keys = (int)((per + 31) / 32 * 32);
+    if (plan.split_keys < 32) plan.split_keys = 32;
+    plan.splits = (int)std::max<int64_t>((span + plan.split_keys - 1) / plan.split_keys, 1);
+    plan.ws_floats = plan.splits > 1 ? plan.splits * tokens * q_heads * (dim + 2) : 0;
+    return plan;
+}
+
+hipError_t launch_attention(AttentionParams p, const AttentionPlan &plan, int dtype, bool vec, hipStream_t stream)
+{
+    p.row_tiles = plan.row_tiles;
+    p.splits = plan.splits;
+    p.split_keys = plan.split_keys;
+    const int grid = plan.row_tiles * plan.splits * (p.q_heads / p.group) * p.batch.sequences;
+    return dtype == NNJIT_F16 ? launch_typed<_Float16>(p, vec, grid, stream) : launch_typed<float>(p, vec, grid, stream);
+}
+
+}  // namespace nnjit

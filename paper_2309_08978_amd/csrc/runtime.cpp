@@ -17,6 +17,7 @@
 #include <tuple>
 #include <vector>
 
+#include "serving.h"
 #include "space.h"
 
 namespace nnjit {
@@ -1084,6 +1085,40 @@ int tune(int kind, int dtype, int64_t batch, int64_t M, int64_t N, int64_t K) {
 }
 
 }  // namespace
+
+// ---------------------- services of the entry points outside this file (serving.h)
+
+int runtime_fail(int code, const char *fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    return fail(code, "%s", buf);
+}
+
+void runtime_clear_error() { t_err.clear(); }
+
+int runtime_launch(hipStream_t stream, int64_t (*floats)(void *ctx, int cus),
+                   hipError_t (*launch)(void *ctx, const RuntimeDevice &), void *ctx, const char *what) {
+    try {
+        std::lock_guard<std::mutex> lk(g_mu);
+        Device *d = nullptr;
+        int rc = device_ready(&d);
+        if (rc != NNJIT_OK) return rc;
+        RuntimeDevice rd{nullptr, d->zero, d->limits.num_cus};
+        const int64_t need = floats ? floats(ctx, rd.cus) : 0;
+        if (need > 0) {
+            rc = workspace_for(*d, stream, need, &rd.ws);
+            if (rc != NNJIT_OK) return rc;
+        }
+        const hipError_t e = launch(ctx, rd);
+        return e == hipSuccess ? NNJIT_OK : hip_fail(e, what);
+    } catch (...) {
+        return NNJIT_ENOMEM;   // the only exception here is a failed host allocation
+    }
+}
+
 }  // namespace nnjit
 
 using namespace nnjit;

@@ -454,14 +454,10 @@ hipError_t launch_rows(const AttentionParams &p, int grid, hipStream_t stream)
 template <typename T>
 hipError_t launch_typed(const AttentionParams &p, bool vec, int grid, hipStream_t stream)
 {
-    hipError_t e;
-    if (!vec) e = p.dim <= 128 ? launch_rows<T, 128, false>(p, grid, stream) : launch_rows<T, 256, false>(p, grid, stream);
-    else if (p.dim <= 64) e = launch_rows<T, 64, true>(p, grid, stream);
-    else if (p.dim <= 128) e = launch_rows<T, 128, true>(p, grid, stream);
-    else e = launch_rows<T, 256, true>(p, grid, stream);
-    if (e != hipSuccess || p.splits == 1) return e;
-    attention_join_kernel<T, 4><<<(unsigned)(p.batch.tokens * p.q_heads), 256, 0, stream>>>(p);
-    return hipGetLastError();
+    if (!vec) return p.dim <= 128 ? launch_rows<T, 128, false>(p, grid, stream) : launch_rows<T, 256, false>(p, grid, stream);
+    if (p.dim <= 64) return launch_rows<T, 64, true>(p, grid, stream);
+    if (p.dim <= 128) return launch_rows<T, 128, true>(p, grid, stream);
+    return launch_rows<T, 256, true>(p, grid, stream);
 }
 
 }  // namespace
@@ -470,24 +466,27 @@ AttentionPlan attention_plan(int dtype, int64_t tokens, int64_t sequences, int q
                              int64_t max_kv, int causal, int64_t window, int cus)
 {
     AttentionPlan plan{};
-    const int64_t group = q_heads / kv_heads;
-    const int64_t tile_rows = 16, wave_keys = dtype == NNJIT_F16 ? 32 : 16;
-    plan.row_tiles = (int)((max_q * group + tile_rows - 1) / tile_rows);
+    const int64_t group = q_heads / kv_heads, rows = max_q * group;
+    const int64_t lanes = (int64_t)kv_heads * sequences;
+    auto tiles = [&](int64_t n) { return (rows + n - 1) / n; };
+    // few rows: 16-row tiles, each wave with keys of its own; many: 128-row tiles
+    // of four waves, or of 64 where those would leave compute units idle
+    plan.tile_rows = rows <= 32 ? 16 : dim > 128 || tiles(128) * lanes >= cus ? 128 : 64;
+    plan.row_tiles = (int)tiles(plan.tile_rows);
     // keys that one tile can see: with a window, from the first row's first key
     // (rounded down to a multiple of 32) to the last row's last
     int64_t span = max_kv;
     if (causal && window > 0) {
-        const int64_t tokens_of_tile = (tile_rows + group - 1) / group + 1;
-        if (window < span && tokens_of_tile < span) span = std::min(span, window + tokens_of_tile + 31);
+        const int64_t tokens_of_tile = (plan.tile_rows + group - 1) / group + 1;
+        if (window < span) span = std::min(span, window + tokens_of_tile + 31);
     }
-    const int64_t groups = (int64_t)plan.row_tiles * kv_heads * sequences;
-    // two workgroups a compute unit, each wave with a tile of its own at least
+    const int64_t groups = plan.row_tiles * lanes;
+    // two workgroups a compute unit, each with a few key tiles at least
+    const int64_t least = plan.tile_rows == 16 ? (dtype == NNJIT_F16 ? 128 : 64) : 256;
     int64_t splits = (2 * (int64_t)cus + groups - 1) / groups;
-    splits = std::min(splits, (span + 4 * wave_keys - 1) / (4 * wave_keys));
-    splits = std::max<int64_t>(splits, 1);
+    splits = std::max<int64_t>(std::min(splits, (span + least - 1) / least), 1);
     const int64_t per = (span + splits - 1) / splits;
-    plan.split_keys = (int)((per + 31) / 32 * 32);
-    if (plan.split_keys < 32) plan.split_keys = 32;
+    plan.split_keys = (int)std::max<int64_t>((per + 31) / 32 * 32, 32);
     plan.splits = (int)std::max<int64_t>((span + plan.split_keys - 1) / plan.split_keys, 1);
     plan.ws_floats = plan.splits > 1 ? plan.splits * tokens * q_heads * (dim + 2) : 0;
     return plan;
@@ -499,7 +498,16 @@ hipError_t launch_attention(AttentionParams p, const AttentionPlan &plan, int dt
     p.splits = plan.splits;
     p.split_keys = plan.split_keys;
     const int grid = plan.row_tiles * plan.splits * (p.q_heads / p.group) * p.batch.sequences;
-    return dtype == NNJIT_F16 ? launch_typed<_Float16>(p, vec, grid, stream) : launch_typed<float>(p, vec, grid, stream);
+    hipError_t e;
+    if (dtype == NNJIT_F16)
+        e = plan.tile_rows == 16 ? launch_typed<_Float16>(p, vec, grid, stream) : launch_attention_tiles_f16(p, plan.tile_rows, vec, grid, stream);
+    else
+        e = plan.tile_rows == 16 ? launch_typed<float>(p, vec, grid, stream) : launch_attention_tiles_f32(p, plan.tile_rows, vec, grid, stream);
+    if (e != hipSuccess || plan.splits == 1) return e;
+    const unsigned rows = (unsigned)(p.batch.tokens * p.q_heads);
+    if (dtype == NNJIT_F16) attention_join_kernel<_Float16, 4><<<rows, 256, 0, stream>>>(p);
+    else attention_join_kernel<float, 4><<<rows, 256, 0, stream>>>(p);
+    return hipGetLastError();
 }
 
 }  // namespace nnjit

@@ -290,9 +290,9 @@ int nnjit_paged_attention(const nnjit_paged_kv *cache, const nnjit_paged_batch *
     c.p.dim = (int)dim;
     c.p.pool = pool_of(cache);
     c.p.batch = batch_of(batch);
-    // a scale of 0 (all keys alike) would make NaNs of masked logits: the smallest
-    // normal number does the same for every finite logit below 2^100
-    c.p.scale_log2 = std::fmax(std::fabs(scale) * 1.44269504088896340736f, 1.17549435e-38f);
+    // a scale of 0 (all keys alike) would make NaNs of masked logits: 2^-100 leaves
+    // the weights of all q . k below 2^76 alike to the last bit
+    c.p.scale_log2 = std::fmax(std::fabs(scale) * 1.44269504088896340736f, 0x1p-100f);
     c.p.negate = scale < 0.f;
     c.p.causal = causal != 0;
     c.p.window = (int)std::min<int64_t>(window, kMaxInt);

@@ -81,7 +81,6 @@ struct AttentionParams {
     float scale_log2;          // |scale| log2(e)
     int negate;                // the scale is negative: queries are taken negated
     int causal, window;
-    int max_q;                 // rows of a sequence that the grid covers
     int row_tiles;             // row tiles of a sequence and key head
     int splits;                // workgroups along the keys
     int split_keys;            // keys of one split (a multiple of the key tile)
@@ -92,12 +91,14 @@ struct AttentionParams {
 
 // How one call is laid out on the chip; sizes the scratch.
 struct AttentionPlan {
-    int kernel;                // 0: 16-row tiles of single waves
+    int tile_rows;             // 16: attention_rows.hip; 64, 128: attention_tiles.h
     int row_tiles, splits, split_keys;
     int64_t ws_floats;         // partial sums and statistics
 };
 AttentionPlan attention_plan(int dtype, int64_t tokens, int64_t sequences, int q_heads, int kv_heads, int dim, int64_t max_q,
                              int64_t max_kv, int causal, int64_t window, int cus);
+hipError_t launch_attention_tiles_f16(const AttentionParams &p, int tile_rows, bool vec, int grid, hipStream_t stream);
+hipError_t launch_attention_tiles_f32(const AttentionParams &p, int tile_rows, bool vec, int grid, hipStream_t stream);
 hipError_t launch_attention(AttentionParams p, const AttentionPlan &plan, int dtype, bool vec, hipStream_t stream);
 
 // Runtime services for entry points outside runtime.cpp.

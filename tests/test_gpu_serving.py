@@ -48,6 +48,16 @@ def test_chunks(dtype, hq, hk, dim, causal, window):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("hq,hk,dim,causal,window", [(16, 16, 64, True, 0), (32, 16, 128, True, 0), (16, 16, 96, True, 20),
+                                                     (16, 16, 128, False, 0), (16, 16, 40, True, 0)])
+def test_chunks_that_fill_the_chip(dtype, hq, hk, dim, causal, window):
+    """Enough sequences and heads for the tallest row tiles."""
+    news = [33, 1, 7, 64, 2, 40, 12, 1, 1, 5, 100, 3, 9, 31, 32, 2, 35]
+    keys = [n + (7 * i) % 90 for i, n in enumerate(news)]
+    _case(news, keys, hq, hk, dim, 16, dtype, seed=21, causal=causal, window=window)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
 @pytest.mark.parametrize("page,order", [(1, "nhd"), (3, "hnd"), (32, "hnd"), (48, "nhd"), (64, "nhd"), (1000, "hnd")])
 def test_pages(dtype, page, order):
     """Pages of any size in both pool layouts, ends inside tiles."""

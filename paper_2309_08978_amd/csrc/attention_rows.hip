@@ -375,9 +375,7 @@ attention_rows_kernel(AttentionParams p)
             }
         } else {
             const long long at = ((long long)split * p.batch.tokens + t.q0 + tok) * p.q_heads + oh;
-            float *dst = p.part + at * dim + d;
-            for (int e = 0; e < 4; ++e)
-                if (d + e < dim) dst[e] = o[e];
+            *(f32x4 *)(p.part + at * p.part_dim + d) = o;
             if (d == 0) {
                 // a sum that is a NaN stays one in the join (weight exp2(inf - inf));
                 // keys seen, but only logits of -inf: 0 / 0 unless another split has more
@@ -389,57 +387,83 @@ attention_rows_kernel(AttentionParams p)
 }
 
 // Joins the splits of every row: o = sum_s w_s o_s / sum_s w_s l_s, w_s = exp2(m_s - M).
-// One workgroup a row; wave w takes the splits w, w + NW, ...; the waves are added in order.
-template <typename T, int NW>
-__global__ void __launch_bounds__(NW * 64)
+// A group of LPR lanes takes four dims a lane of one row; GPR groups of a
+// workgroup share a row, group i the splits i, i + GPR, ..., added in order:
+// 1 where rows fill the chip by themselves, else all groups of the workgroup,
+// so that a decode step's few rows of many splits are read in parallel.
+template <typename T, int LPR, int GPR>
+__global__ void __launch_bounds__(256)
 attention_join_kernel(AttentionParams p)
 {
-    __shared__ float lds_o[NW][kMaxHeadDim], lds_l[NW];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int GROUPS = 256 / LPR, ROWS = GROUPS / GPR;
+    __shared__ f32x4 lds_o[GPR > 1 ? GROUPS : 1][LPR];
+    __shared__ float lds_l[GROUPS];
+    const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR;
     const long long rows = (long long)p.batch.tokens * p.q_heads;
-    const long long row = blockIdx.x;
+    const long long row = (long long)blockIdx.x * ROWS + group / GPR;
     const int token = (int)(row / p.q_heads), head = (int)(row % p.q_heads);
-    if (token < p.batch.q_start[0] || token >= p.batch.q_start[p.batch.sequences]) return;   // no sequence's
+    const bool live = row < rows && token >= p.batch.q_start[0] && token < p.batch.q_start[p.batch.sequences];
 
-    float most = -__builtin_inff();
+    float most = -__builtin_inff(), total = 0.f;
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
     bool none = false;
-    for (int s = lane; s < p.splits; s += 64) {
-        const float *st = p.stat + (s * rows + row) * 2;
-        most = fmaxf(most, st[0]);
-        none |= st[1] != st[1];
-    }
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) most = fmaxf(most, __shfl_xor(most, i));
-    const bool any_none = __any(none);
-    const float off = most == -__builtin_inff() ? 0.f : most;
-
-    constexpr int E = kMaxHeadDim / 64;
-    float o[E] = {}, total = 0.f;
-    for (int s = wave; s < p.splits; s += NW) {
-        const long long at = s * rows + row;
-        const float sm = p.stat[at * 2];
-        if (sm == -__builtin_inff()) continue;           // has seen nothing
-        const float w = exp2_fast(sm - off);
-        total += w * p.stat[at * 2 + 1];
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (e * 64 + lane < p.dim) o[e] += w * p.part[at * p.dim + e * 64 + lane];
-    }
-#pragma unroll
-    for (int e = 0; e < E; ++e) lds_o[wave][e * 64 + lane] = o[e];
-    if (lane == 0) lds_l[wave] = total;
-    __syncthreads();
-    if (threadIdx.x < (unsigned)p.dim) {
-        float sum = 0.f, l = 0.f;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            sum += lds_o[w][threadIdx.x];
-            l += lds_l[w];
+    if (live) {
+        for (int s = 0; s < p.splits; ++s) {
+            const f32x2 st = *(const f32x2 *)(p.stat + (s * rows + row) * 2);
+            most = fmaxf(most, st[0]);
+            none |= st[1] != st[1];
         }
-        const bool empty = most == -__builtin_inff();
-        ((T *)p.o.p)[(long long)token * p.o.tok + (long long)head * p.o.head + threadIdx.x] =
-            (T)(empty ? (any_none ? __builtin_nanf("") : 0.f) : sum / l);
+        const float off = most == -__builtin_inff() ? 0.f : most;
+        const int d = min(4 * lane, p.part_dim - 4);
+#pragma unroll 4
+        for (int s = group % GPR; s < p.splits; s += GPR) {
+            const long long at = s * rows + row;
+            const f32x2 st = *(const f32x2 *)(p.stat + at * 2);
+            const f32x4 part = *(const f32x4 *)(p.part + at * p.part_dim + d);
+            const bool seen = st[0] != -__builtin_inff();          // else it has seen nothing, or only -inf
+            const float w = exp2_fast(st[0] - off);
+            total += seen ? w * st[1] : 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += seen ? w * part[e] : 0.f;
+        }
     }
+    if constexpr (GPR > 1) {
+        lds_o[group][lane] = o;
+        if (lane == 0) lds_l[group] = total;
+        __syncthreads();
+        if (group % GPR != 0) return;
+        o = f32x4{0.f, 0.f, 0.f, 0.f};
+        total = 0.f;
+        for (int g = 0; g < GPR; ++g) {
+            o += lds_o[group + g][lane];
+            total += lds_l[group + g];
+        }
+    }
+    if (!live) return;
+    const bool empty = most == -__builtin_inff();
+    T *dst = (T *)p.o.p + (long long)token * p.o.tok + (long long)head * p.o.head + 4 * lane;
+    for (int e = 0; e < 4; ++e)
+        if (4 * lane + e < p.dim) dst[e] = (T)(empty ? (none ? __builtin_nanf("") : 0.f) : o[e] / total);
+}
+
+template <typename T>
+hipError_t launch_join(const AttentionParams &p, hipStream_t stream)
+{
+    const long long rows = (long long)p.batch.tokens * p.q_heads;
+    // below four rows a compute unit, a workgroup a row
+    const bool few = rows < 1024;
+    auto grid = [&](int per) { return (unsigned)((rows + per - 1) / per); };
+    if (p.dim <= 64) {
+        if (few) attention_join_kernel<T, 16, 16><<<grid(1), 256, 0, stream>>>(p);
+        else attention_join_kernel<T, 16, 1><<<grid(16), 256, 0, stream>>>(p);
+    } else if (p.dim <= 128) {
+        if (few) attention_join_kernel<T, 32, 8><<<grid(1), 256, 0, stream>>>(p);
+        else attention_join_kernel<T, 32, 1><<<grid(8), 256, 0, stream>>>(p);
+    } else {
+        if (few) attention_join_kernel<T, 64, 4><<<grid(1), 256, 0, stream>>>(p);
+        else attention_join_kernel<T, 64, 1><<<grid(4), 256, 0, stream>>>(p);
+    }
+    return hipGetLastError();
 }
 
 template <typename T, int DP, bool VEC>
@@ -488,7 +512,7 @@ AttentionPlan attention_plan(int dtype, int64_t tokens, int64_t sequences, int q
     const int64_t per = (span + splits - 1) / splits;
     plan.split_keys = (int)std::max<int64_t>((per + 31) / 32 * 32, 32);
     plan.splits = (int)std::max<int64_t>((span + plan.split_keys - 1) / plan.split_keys, 1);
-    plan.ws_floats = plan.splits > 1 ? plan.splits * tokens * q_heads * (dim + 2) : 0;
+    plan.ws_floats = plan.splits > 1 ? plan.splits * tokens * q_heads * ((dim + 3) / 4 * 4 + 2) : 0;
     return plan;
 }
 
@@ -504,10 +528,7 @@ hipError_t launch_attention(AttentionParams p, const AttentionPlan &plan, int dt
     else
         e = plan.tile_rows == 16 ? launch_typed<float>(p, vec, grid, stream) : launch_attention_tiles_f32(p, plan.tile_rows, vec, grid, stream);
     if (e != hipSuccess || plan.splits == 1) return e;
-    const unsigned rows = (unsigned)(p.batch.tokens * p.q_heads);
-    if (dtype == NNJIT_F16) attention_join_kernel<_Float16, 4><<<rows, 256, 0, stream>>>(p);
-    else attention_join_kernel<float, 4><<<rows, 256, 0, stream>>>(p);
-    return hipGetLastError();
+    return dtype == NNJIT_F16 ? launch_join<_Float16>(p, stream) : launch_join<float>(p, stream);
 }
 
 }  // namespace nnjit

@@ -397,8 +397,7 @@ attention_tiles_kernel(AttentionParams p)
                             if (d + e < dim) dst[d + e] = out[e];
                     }
                 } else {
-                    for (int e = 0; e < 4; ++e)
-                        if (d + e < dim) p.part[at * dim + d + e] = o[e];
+                    if (d < dim) *(f32x4 *)(p.part + at * p.part_dim + d) = f32x4{o[0], o[1], o[2], o[3]};
                 }
             }
     if (p.splits > 1 && h == 0) {

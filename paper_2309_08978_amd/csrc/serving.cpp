@@ -139,8 +139,9 @@ hipError_t do_attention(void *ctx, const RuntimeDevice &d) {
     c.p.zero = d.zero;
     if (c.plan.splits > 1) {
         const int64_t rows = (int64_t)c.plan.splits * c.p.batch.tokens * c.p.q_heads;
+        c.p.part_dim = (c.p.dim + 3) / 4 * 4;
         c.p.part = d.ws;
-        c.p.stat = d.ws + rows * c.p.dim;
+        c.p.stat = d.ws + rows * c.p.part_dim;
     }
     return launch_attention(c.p, c.plan, c.dtype, c.vec, c.stream);
 }

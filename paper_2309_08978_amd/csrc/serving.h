@@ -84,7 +84,8 @@ struct AttentionParams {
     int row_tiles;             // row tiles of a sequence and key head
     int splits;                // workgroups along the keys
     int split_keys;            // keys of one split (a multiple of the key tile)
-    float *part;               // splits > 1: [splits][tokens * q_heads][dim], not normalised
+    int part_dim;              // dim rounded up to a multiple of 4
+    float *part;               // splits > 1: [splits][tokens * q_heads][part_dim], not normalised
     float *stat;               // splits > 1: [splits][tokens * q_heads][2]: largest logit (times log2 e), sum
     const void *zero;          // >= 64 bytes of zeros
 };

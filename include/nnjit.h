@@ -421,7 +421,8 @@ int nnjit_stream_read(const void *src, int64_t bytes, void *sink, int workgroups
 /* The pool of pages: slot s of page g holds key head h at
  * k[g * k_page + s * k_token + h * k_head + i], values alike.  Both
  * [page][slot][head][dim] and [page][head][slot][dim] pools (and views of
- * larger ones) can be described; a pool may pass 2^32 elements. */
+ * larger ones) can be described.  Page and token strides are below 2^32
+ * elements; a pool may be larger. */
 typedef struct nnjit_paged_kv {
     void *k, *v;
     int64_t k_page, k_token, k_head;   /* strides in elements */

@@ -60,19 +60,28 @@ constexpr float kPosInf = 1.f, kNegInf = 64.f, kNan = 4096.f;
 __device__ __forceinline__ bool finite(_Float16 v) { return (__builtin_bit_cast(unsigned short, v) & 0x7c00u) != 0x7c00u; }
 __device__ __forceinline__ bool finite(float v) { return (__builtin_bit_cast(unsigned, v) & 0x7f800000u) != 0x7f800000u; }
 
-template <typename T>
-__device__ __forceinline__ T class_of(T v)
+// (by integer operations: no branches)
+__device__ __forceinline__ _Float16 class_of(_Float16 v)
 {
-    return finite(v) ? (T)0 : v != v ? (T)kNan : v > (T)0 ? (T)kPosInf : (T)kNegInf;
+    const unsigned u = __builtin_bit_cast(unsigned short, v), size = u & 0x7fffu;
+    const unsigned inf = u & 0x8000u ? 0x5400u : 0x3c00u;   // 64, 1
+    return __builtin_bit_cast(_Float16, (unsigned short)(size > 0x7c00u ? 0x6c00u : size == 0x7c00u ? inf : 0u));
+}
+
+__device__ __forceinline__ float class_of(float v)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, v), size = u & 0x7fffffffu;
+    const float inf = u & 0x80000000u ? kNegInf : kPosInf;
+    return size > 0x7f800000u ? kNan : size == 0x7f800000u ? inf : 0.f;
 }
 
 __device__ __forceinline__ float add_classes(float sum, float counts)
 {
-    const int n = (int)counts;
-    if (n == 0) return sum;
-    const bool pos = n & 63, neg = (n >> 6) & 63, nan = n >= 4096;
-    const float inf = __builtin_inff();
-    return sum + ((nan || (pos && neg)) ? __builtin_nanf("") : pos ? inf : -inf);
+    const unsigned n = (unsigned)counts;
+    const unsigned pos = n & 63u, neg = n & 0xfc0u;
+    unsigned add = pos ? 0x7f800000u : neg ? 0xff800000u : 0u;
+    add = (pos && neg) || n >= 4096u ? 0x7fc00000u : add;
+    return sum + __builtin_bit_cast(float, add);
 }
 
 // Largest magnitude of halves, two at a time as integers (an infinity or NaN is
@@ -93,6 +102,15 @@ struct Largest16 {
     }
     __device__ __forceinline__ bool finite() const { return top[0] < 0x7c00 && top[1] < 0x7c00; }
 };
+
+// Largest logit (times log2 e) and sum of a row's split, as the join takes them.
+// A sum that is a NaN stays one (weight exp2(inf - inf)); keys seen, but only
+// logits of -inf: 0 / 0 unless another split has more.
+__device__ __forceinline__ void store_stat(const AttentionParams &p, long long at, float top, float sum, bool sees)
+{
+    p.stat[at * 2] = sum != sum ? __builtin_inff() : top;
+    p.stat[at * 2 + 1] = sees && sum == 0.f ? __builtin_nanf("") : sum;
+}
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 

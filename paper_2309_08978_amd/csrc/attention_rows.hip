@@ -34,7 +34,7 @@
 #include <algorithm>
 
 #include "attention_common.h"
-#include "../../include/nnjit.h"
+#include "nnjit.h"
 
 namespace nnjit {
 
@@ -166,7 +166,7 @@ attention_rows_kernel(AttentionParams p)
     auto load_k = [&](const Ids &ids, int kt) {
 #pragma unroll
         for (int s = 0; s < SUB; ++s) {
-            const T *row = kp + (long long)safe_page(p, ids.k[s]) * p.pool.k_page + (long long)slot_of(kt + 16 * s, c) * p.pool.k_tok;
+            const T *row = kp + page_offset(safe_page(p, ids.k[s]), p.pool.k_page, slot_of(kt + 16 * s, c), p.pool.k_tok);
 #pragma unroll
             for (int e = 0; e < STEPS; ++e) {
                 const int d = (4 * e + g) * CH;
@@ -178,8 +178,8 @@ attention_rows_kernel(AttentionParams p)
 #pragma unroll
         for (int i = 0; i < SUB * 4; ++i) {
             const int s = i / 4;
-            const T *row = vp + (long long)safe_page(p, PAGE16 ? ids.k[s] : ids.v[i]) * p.pool.v_page +
-                           (long long)slot_of(kt + 16 * s, 4 * g + i % 4) * p.pool.v_tok;
+            const T *row = vp + page_offset(safe_page(p, PAGE16 ? ids.k[s] : ids.v[i]), p.pool.v_page,
+                                            slot_of(kt + 16 * s, 4 * g + i % 4), p.pool.v_tok);
 #pragma unroll
             for (int h = 0; h < VH; ++h) {
                 const int d = h * 16 * VE + c * VE;
@@ -376,12 +376,7 @@ attention_rows_kernel(AttentionParams p)
         } else {
             const long long at = ((long long)split * p.batch.tokens + t.q0 + tok) * p.q_heads + oh;
             *(f32x4 *)(p.part + at * p.part_dim + d) = o;
-            if (d == 0) {
-                // a sum that is a NaN stays one in the join (weight exp2(inf - inf));
-                // keys seen, but only logits of -inf: 0 / 0 unless another split has more
-                p.stat[at * 2] = total != total ? __builtin_inff() : most;
-                p.stat[at * 2 + 1] = sees && total == 0.f ? __builtin_nanf("") : total;
-            }
+            if (d == 0) store_stat(p, at, most, total, sees);
         }
     }
 }

@@ -36,6 +36,8 @@
 // error is that of the result's own rounding to fp16.
 #pragma once
 
+#include <type_traits>
+
 #include "attention_common.h"
 
 namespace nnjit {
@@ -46,17 +48,100 @@ typedef __attribute__((address_space(3))) char lds_char;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
+// How keys and values reach LDS: ANY element by element, from any address;
+// CHUNKS copies of 16 bytes, a look-up a lane; PAGED16 copies whose keys lie in one page
+// (pages of a multiple of 16 tokens) and whole head dims (dim == DP), addresses
+// by scalar arithmetic.  The look-ups of CHUNKS cost about as many vector
+// instructions a step as the softmax.
+enum { ANY, CHUNKS, PAGED16 };
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"   // m0 is written on purpose
+// copy16_to_lds with a scalar base and a 32-bit offset a lane
+__device__ __forceinline__ void copy16_to_lds_from(const void *base, unsigned offset, unsigned lds)
+{
+    // the same in every lane, and said so: the operands must be scalar registers
+    const unsigned long long u = (unsigned long long)base;
+    const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)u), hi = __builtin_amdgcn_readfirstlane((unsigned)(u >> 32));
+    const unsigned long long s = lo | (unsigned long long)hi << 32;
+    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(s),
+                 "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// Larger of the two lanes l and l + 32.
+__device__ __forceinline__ float max_of_halves(float x)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const unsigned a = both[0], b = both[1];
+    return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+
 // What a row's weights may exceed 1 by before its reference is moved: 2^8.
 constexpr float kSlack = 8.f;
 
-template <typename T, int DP, bool VEC, int WR, int WK, int KB>
-__global__ void __launch_bounds__(WR * WK * 64, DP <= 128 ? 2 : 1)
+// Row r of a tile over the keys k0 .. k1 - 1, by one wave: a lane has dims
+// lane, lane + 64, ...; only keys that the row sees are touched.
+template <typename T, int DP>
+__device__ __forceinline__ void redo_row(const AttentionParams &p, const RowTile &t, int head, int split, int r, int k0, int k1, int lane)
+{
+    constexpr int E = (DP + 63) / 64;
+    const int lo = max(t.first_key(p, r), k0), hi = min(t.end_key(p, r), k1);
+    const int token = t.q0 + p.group_div.quot(r);
+    const int q_head = head * p.group + r - p.group_div.quot(r) * p.group;
+    const T *q = (const T *)p.q.p + (long long)token * p.q.tok + (long long)q_head * p.q.head;
+    float qv[E], o[E], m = -__builtin_inff(), l = 0.f;
+    for (int e = 0; e < E; ++e) {
+        qv[e] = lane + 64 * e < p.dim ? (float)q[lane + 64 * e] : 0.f;
+        if (p.negate) qv[e] = -qv[e];
+        o[e] = 0.f;
+    }
+#pragma unroll 1
+    for (int key = lo; key < hi; ++key) {
+        const int pi = p.pool.page_size.quot(key), slot = key - pi * (int)p.pool.page_size.d;
+        const int page = safe_page(p, t.table[pi]);
+        const T *k = (const T *)p.pool.k + (long long)head * p.pool.k_head + page_offset(page, p.pool.k_page, slot, p.pool.k_tok);
+        const T *v = (const T *)p.pool.v + (long long)head * p.pool.v_head + page_offset(page, p.pool.v_page, slot, p.pool.v_tok);
+        float x = 0.f;
+        for (int e = 0; e < E; ++e)
+            if (lane + 64 * e < p.dim) x += qv[e] * (float)k[lane + 64 * e];
+        for (int i = 1; i < 64; i <<= 1) x += __shfl_xor(x, i);
+        const float next = fmaxf(m, x), off = next == -__builtin_inff() ? 0.f : next;
+        const float shrink = exp2_fast((m - off) * p.scale_log2), w = exp2_fast((x - off) * p.scale_log2);
+        m = next;
+        l = l * shrink + w;
+        for (int e = 0; e < E; ++e)
+            if (lane + 64 * e < p.dim) o[e] = o[e] * shrink + w * (float)v[lane + 64 * e];
+    }
+    const long long at = ((long long)split * p.batch.tokens + token) * p.q_heads + q_head;
+    T *dst = (T *)p.o.p + (long long)token * p.o.tok + (long long)q_head * p.o.head;
+    for (int e = 0; e < E; ++e) {
+        const int d = lane + 64 * e;
+        if (p.splits == 1) {
+            if (d < p.dim) dst[d] = (T)(hi > lo ? o[e] / l : 0.f);
+        } else {
+            if (d < p.part_dim) p.part[at * p.part_dim + d] = o[e];
+        }
+    }
+    if (p.splits > 1 && lane == 0) store_stat(p, at, m * p.scale_log2, l, hi > lo);
+}
+
+// Bytes of a row in LDS, and how many workgroups' waves a SIMD holds beside
+// each other (two unless the buffers or the registers of one fill a CU).
+template <typename T, int DP>
+constexpr int row_pitch() { return (DP <= 64 ? 64 : DP <= 128 ? 128 : 256) * (int)sizeof(T); }
+template <typename T, int DP, int BLOCKS>
+constexpr int tiles_per_simd() { return DP <= 128 && 4 * 32 * BLOCKS * row_pitch<T, DP>() <= 80 * 1024 ? 2 : 1; }
+
+template <typename T, int DP, int HOW, int WR, int WK, int KB>
+__global__ void __launch_bounds__(WR * WK * 64, (tiles_per_simd<T, DP, KB * WK>()))
 attention_tiles_kernel(AttentionParams p)
 {
     constexpr bool HALF = sizeof(T) == 2;
     constexpr int NW = WR * WK;
     constexpr int CH = 16 / sizeof(T);                    // elements of a chunk
-    constexpr int PITCH = (DP <= 64 ? 64 : DP <= 128 ? 128 : 256) * (int)sizeof(T);
+    constexpr int PITCH = row_pitch<T, DP>();
     constexpr int CPR = PITCH / 16;                       // chunks of a row
     constexpr int BN = 32 * KB * WK;                      // keys of a step
     constexpr int TILE = BN * PITCH;
@@ -102,8 +187,7 @@ attention_tiles_kernel(AttentionParams p)
     // the wave's rows, and this lane's (rows past the end repeat the last one)
     const int w0 = min(t.r0 + 32 * wr, r_last), w1 = min(t.r0 + 32 * wr + 31, r_last);
     const bool wave_rows = t.r0 + 32 * wr <= r_last;
-    const int lo_w = max(t.first_key(p, w0), k0), lo_all = t.first_key(p, w1);
-    const int hi_w = min(t.end_key(p, w1), k1), hi_all = min(t.end_key(p, w0), k1);
+    const int lo_w = max(t.first_key(p, w0), k0), hi_w = min(t.end_key(p, w1), k1);
     const int r = min(t.r0 + 32 * wr + n, r_last);
     const int token = t.q0 + p.group_div.quot(r);
     const int q_head = head * p.group + r - p.group_div.quot(r) * p.group;
@@ -116,7 +200,7 @@ attention_tiles_kernel(AttentionParams p)
 #pragma unroll
         for (int s = 0; s < QS; ++s) {
             const int d = (2 * s + h) * CH;
-            if constexpr (VEC) {
+            if constexpr (HOW != ANY) {
                 q[s] = chunk{};
                 if (d < dim) q[s] = *(const chunk *)(src + d);
             } else {
@@ -131,47 +215,63 @@ attention_tiles_kernel(AttentionParams p)
     const int page_size = p.pool.page_size.d;
     const int last_key = max(hi_max - 1, 0);
 
-    // the keys of this lane's copies, relative to the step's first
-    int key_of[NI];
-    int k_col[NI], v_col[NI];                             // logical element columns
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-        const int at = (i * NW + wave) * 64 + lane;
-        key_of[i] = at / CPR;
-        k_col[i] = ((at % CPR) ^ k_swz(key_of[i])) * CH;
-        v_col[i] = ((at % CPR) ^ v_swz(key_of[i])) * CH;
-    }
+    // Copy i of this wave brings KPI keys, key_of[i] the lane's, from the step's
+    // first key on.  Page ids are looked up a step before they are used.
+    constexpr int KPI = 64 / CPR;
+    auto key_of = [&](int i, int ln) { return (i * NW + wave) * KPI + ln / CPR; };
+    auto k_col = [&](int i, int ln) { return ((ln % CPR) ^ k_swz(key_of(i, ln))) * CH; };
+    auto v_col = [&](int i, int ln) { return ((ln % CPR) ^ v_swz(key_of(i, ln))) * CH; };
     struct Ids {
         int page[NI];
     };
     auto ids_of = [&](int kt) {
         Ids ids;
 #pragma unroll
-        for (int i = 0; i < NI; ++i) ids.page[i] = t.table[p.pool.page_size.quot(min(kt + key_of[i], last_key))];
+        for (int i = 0; i < NI; ++i)
+            ids.page[i] = t.table[p.pool.page_size.quot(min(kt + key_of(i, HOW == PAGED16 ? 0 : lane), last_key))];
         return ids;
     };
     auto copy_step = [&](const Ids &ids, int kt, int b) {
+        const unsigned k_lds = (unsigned)(uintptr_t)k_buf(b) + wave * 1024, v_lds = (unsigned)(uintptr_t)v_buf(b) + wave * 1024;
+        int ln = lane;
+        if constexpr (HOW == PAGED16) {
+            if (kt >= first && kt + BN <= k1) {
+                // every key is there and a copy's keys lie in one page: scalar addresses, lane offsets that never change
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    const int key = kt + key_of(i, 0);
+                    const int slot = key - p.pool.page_size.quot(key) * page_size;
+                    const int page = safe_page(p, __builtin_amdgcn_readfirstlane(ids.page[i]));
+                    const T *ks = kp + page_offset(page, p.pool.k_page, slot, p.pool.k_tok);
+                    const T *vs = vp + page_offset(page, p.pool.v_page, slot, p.pool.v_tok);
+                    const int kc = k_col(i, lane), vc = v_col(i, lane);   // past dim (DP 96 in rows of 128): never read
+                    copy16_to_lds_from(ks, ((unsigned)(lane / CPR) * p.pool.k_tok + (kc < DP ? kc : 0)) * (unsigned)sizeof(T), k_lds + i * NW * 1024);
+                    copy16_to_lds_from(vs, ((unsigned)(lane / CPR) * p.pool.v_tok + (vc < DP ? vc : 0)) * (unsigned)sizeof(T), v_lds + i * NW * 1024);
+                }
+                return;
+            }
+            asm volatile("" : "+v"(ln));   // what the few other steps need is not kept in registers
+        }
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            const int key = min(kt + key_of[i], last_key);
-            const int slot = key - p.pool.page_size.quot(key) * page_size;
-            const long long page = safe_page(p, ids.page[i]);
-            const T *ks = kp + page * p.pool.k_page + (long long)slot * p.pool.k_tok + k_col[i];
-            const T *vs = vp + page * p.pool.v_page + (long long)slot * p.pool.v_tok + v_col[i];
+            const int at = kt + key_of(i, ln), kc = k_col(i, ln), vc = v_col(i, ln);
+            const int key = min(at, last_key);
+            const int slot = key - p.pool.page_size.quot(key) * page_size, page = safe_page(p, ids.page[i]);
+            const T *ks = kp + page_offset(page, p.pool.k_page, slot, p.pool.k_tok) + kc;
+            const T *vs = vp + page_offset(page, p.pool.v_page, slot, p.pool.v_tok) + vc;
             // keys that no row sees are zeros: what lies in their slots must not be multiplied, not even by 0
-            const bool ok = kt + key_of[i] >= first && kt + key_of[i] < k1;
-            const unsigned at = (unsigned)((i * NW + wave) * 1024);
-            if constexpr (VEC) {
-                copy16_to_lds(ok && k_col[i] < dim ? ks : (const T *)p.zero, (unsigned)(uintptr_t)k_buf(b) + at);
-                copy16_to_lds(ok && v_col[i] < dim ? vs : (const T *)p.zero, (unsigned)(uintptr_t)v_buf(b) + at);
+            const bool ok = at >= first && at < k1;
+            if constexpr (HOW != ANY) {
+                copy16_to_lds(ok && kc < dim ? ks : (const T *)p.zero, __builtin_amdgcn_readfirstlane(k_lds + i * NW * 1024));
+                copy16_to_lds(ok && vc < dim ? vs : (const T *)p.zero, __builtin_amdgcn_readfirstlane(v_lds + i * NW * 1024));
             } else {
-                chunk kc, vc;
+                chunk ke, ve;
                 for (int e = 0; e < CH; ++e) {
-                    kc[e] = ok && k_col[i] + e < dim ? ks[e] : (T)0;
-                    vc[e] = ok && v_col[i] + e < dim ? vs[e] : (T)0;
+                    ke[e] = ok && kc + e < dim ? ks[e] : (T)0;
+                    ve[e] = ok && vc + e < dim ? vs[e] : (T)0;
                 }
-                *(__attribute__((address_space(3))) chunk *)(k_buf(b) + at + lane * 16) = kc;
-                *(__attribute__((address_space(3))) chunk *)(v_buf(b) + at + lane * 16) = vc;
+                *(__attribute__((address_space(3))) chunk *)(k_buf(b) + (i * NW + wave) * 1024 + lane * 16) = ke;
+                *(__attribute__((address_space(3))) chunk *)(v_buf(b) + (i * NW + wave) * 1024 + lane * 16) = ve;
             }
         }
     };
@@ -189,18 +289,72 @@ attention_tiles_kernel(AttentionParams p)
     const int v_row = HALF ? (kw + 4 * h + tr_r) * PITCH + (lane & 3) * 8 : (kw + 4 * h) * PITCH + n * VW * 4;
     const int v_unit = HALF ? (lane >> 4) & 1 : 0;
 
-    auto compute = [&](int kt, int b) {
-        const int key0 = kt + kw;
-        if (!wave_rows || key0 >= hi_w || key0 + 32 * KB <= lo_w) return;
+    // V of the wave's 32-key block kb: fp16, product u (of two) and block db of 32
+    // dims: eight keys of one dim
+    auto read_v16 = [&](int b, int kb, int u, int db) {
+        const int unit = (2 * db + v_unit) ^ (v_swz(tr_r) >> 1);
+        s16x4 part[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_s16x4 *)(v_buf(b) + v_row + (32 * kb + 8 * (2 * u + e)) * PITCH + unit * 32));
+        return __builtin_bit_cast(f16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    // fp32: key i (of 16 a half wave), dims group g: VW dims of one key
+    typedef float vvec __attribute__((ext_vector_type(VW)));
+    auto read_v32 = [&](int b, int kb, int i, int g) {
+        return *(__attribute__((address_space(3))) vvec *)(v_buf(b) + v_row + (32 * kb + 8 * (i / 4) + i % 4) * PITCH + g * 32 * VW * 4);
+    };
+
+    // O^T += V^T P^T, P in x.  CHECK: note in `dirty` if any of the values is not finite
+    bool dirty = false;
+    auto add_values = [&](auto check, const f32x16 *x, int b) {
+        constexpr bool CHECK = decltype(check)::value;
+        Largest16 largest;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            if constexpr (HALF) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    f16x8 pr;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) pr[i] = (_Float16)x[kb][8 * u + i];
+#pragma unroll
+                    for (int db = 0; db < BLK; ++db) {
+                        const f16x8 v = read_v16(b, kb, u, db);
+                        if constexpr (CHECK) largest.take(v);
+                        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pr, acc[db], 0, 0, 0);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+#pragma unroll
+                    for (int g = 0; g < BLK / VW; ++g) {
+                        const vvec v = read_v32(b, kb, i, g);
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) {
+                            const float value = v[e];
+                            if constexpr (CHECK) dirty |= !finite(value);
+                            acc[g * VW + e] = __builtin_amdgcn_mfma_f32_32x32x2f32(value, x[kb][i], acc[g * VW + e], 0, 0, 0);
+                        }
+                    }
+            }
+        }
+        if constexpr (CHECK && HALF) dirty |= !largest.finite();
+    };
+
+    // one step of this wave; WHOLE: every row sees every key of it
+    auto step = [&](auto is_whole, int key0, int b) {
+        constexpr bool WHOLE = decltype(is_whole)::value;
         f32x16 x[KB];
-        lds_char *kb_ = k_buf(b), *vb_ = v_buf(b);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
             x[kb] = f32x16{};
 #pragma unroll
             for (int s = 0; s < QS; ++s) {
                 const int c = (2 * s + h) ^ k_swz(n);
-                const chunk a = *(__attribute__((address_space(3))) chunk *)(kb_ + k_row + kb * 32 * PITCH + c * 16);
+                const chunk a = *(__attribute__((address_space(3))) chunk *)(k_buf(b) + k_row + kb * 32 * PITCH + c * 16);
                 if constexpr (HALF) {
                     x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[s], x[kb], 0, 0, 0);
                 } else {
@@ -209,29 +363,21 @@ attention_tiles_kernel(AttentionParams p)
                 }
             }
         }
-        const bool whole = key0 >= lo_all && key0 + 32 * KB <= hi_all;
-        unsigned seen[KB];
+        if constexpr (!WHOLE) {
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) seen[kb] = ~0u;
-        if (!whole) {
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                seen[kb] = 0;
+            for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int key = key0 + 32 * kb + 8 * (i / 4) + 4 * h + i % 4;
-                    const bool see = key >= lo && key < hi;
-                    x[kb][i] = see ? x[kb][i] : -__builtin_inff();
-                    seen[kb] |= see ? 1u << i : 0u;
+                    x[kb][i] = key >= lo && key < hi ? x[kb][i] : -__builtin_inff();
                 }
-            }
         }
         float top = x[0][0];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
-        top = fmaxf(top, __shfl_xor(top, 32));
+        top = max_of_halves(top);
         if (__any(top - m > slack)) {
             const float next = fmaxf(m, top);
             const float shrink = exp2_fast((m - (next == -__builtin_inff() ? 0.f : next)) * scale);
@@ -248,111 +394,70 @@ attention_tiles_kernel(AttentionParams p)
                 x[kb][i] = exp2_fast(fmaf(x[kb][i], scale, -off));
                 l += x[kb][i];
             }
-        if constexpr (HALF) {
-#pragma unroll
-            for (int u = 0; u < 2 * KB; ++u) {
-                const int kb = u / 2, i0 = 8 * (u % 2);
-                f16x8 pr;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) pr[i] = (_Float16)x[kb][i0 + i];
-#pragma unroll
-                for (int db = 0; db < BLK; ++db) {
-                    const int unit = (2 * db + v_unit) ^ (v_swz(tr_r) >> 1);
-                    s16x4 part[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            (lds_s16x4 *)(vb_ + v_row + (32 * kb + 8 * (2 * (u % 2) + e)) * PITCH + unit * 32));
-                    f16x8 v = __builtin_bit_cast(f16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                    if (!whole) {
-                        Largest16 largest;
-                        largest.take(v);
-                        if (__any(!largest.finite())) {
-                            f16x8 cls, vis;
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                cls[i] = class_of(v[i]);
-                                v[i] = finite(v[i]) ? v[i] : (_Float16)0.f;
-                                vis[i] = (_Float16)((seen[kb] >> (i0 + i) & 1) ? 1.f : 0.f);
-                            }
-                            const f32x16 c = __builtin_amdgcn_mfma_f32_32x32x16_f16(cls, vis, f32x16{}, 0, 0, 0);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) acc[db][i] = add_classes(acc[db][i], c[i]);
-                        }
-                    }
-                    acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pr, acc[db], 0, 0, 0);
-                }
-            }
-        } else {
-            typedef float vvec __attribute__((ext_vector_type(VW)));
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-#pragma unroll
-                    for (int g = 0; g < BLK / VW; ++g) {
-                        vvec v = *(__attribute__((address_space(3))) vvec *)(vb_ + v_row + (32 * kb + 8 * (i / 4) + i % 4) * PITCH +
-                                                                              g * 32 * VW * 4);
-                        bool bad = false;
-#pragma unroll
-                        for (int e = 0; e < VW; ++e) bad |= !finite((float)v[e]);
-                        if (!whole && __any(bad)) {
-                            const float vis = (seen[kb] >> i & 1) ? 1.f : 0.f;
-#pragma unroll
-                            for (int e = 0; e < VW; ++e) {
-                                const f32x16 c = __builtin_amdgcn_mfma_f32_32x32x2f32(class_of((float)v[e]), vis, f32x16{}, 0, 0, 0);
-                                v[e] = finite((float)v[e]) ? v[e] : 0.f;
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) acc[g * VW + e][j] = add_classes(acc[g * VW + e][j], c[j]);
-                            }
-                        }
-#pragma unroll
-                        for (int e = 0; e < VW; ++e)
-                            acc[g * VW + e] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], x[kb][i], acc[g * VW + e], 0, 0, 0);
-                    }
-                }
-        }
+        add_values(std::bool_constant<!WHOLE>{}, x, b);
     };
 
     const int start = k0 & ~31;                           // k0 is a multiple of 32 or hi_max (no keys)
     const int steps = k1 > k0 ? (k1 - start + BN - 1) / BN : 0;
+    // steps whole_from .. whole_to - 1: every row of the workgroup sees every key.
+    // The others, a few at either end, run a loop of their own: one loop with
+    // both kinds of step in it would hold the sums in two sets of registers.
+    const int lo_max = t.first_key(p, r_last), hi_min = min(t.end_key(p, t.r0), k1);
+    const int whole_from = min(max((lo_max - start + BN - 1) / BN, 0), steps);
+    const int whole_to = hi_min > start ? max((hi_min - start) / BN, whole_from) : whole_from;
+    Ids ids;
     if (steps > 0) {
-        Ids ids = ids_of(start);
+        ids = ids_of(start);
         copy_step(ids, start, 0);
         ids = ids_of(start + BN);
-        for (int it = 0; it < steps; ++it) {
-            // this step's copies have arrived, and every wave has read the other buffer
-            wait_vmcnt<0>();
-            lds_barrier();
-            const int kt = start + it * BN;
-            if (it + 1 < steps) {
-                copy_step(ids, kt + BN, (it + 1) & 1);
-                ids = ids_of(kt + 2 * BN);
+    }
+    auto next_step = [&](int it) {
+        // this step's copies have arrived, and every wave has read the other buffer
+        wait_vmcnt<0>();
+        lds_barrier();
+        if (it + 1 < steps) {
+            copy_step(ids, start + (it + 1) * BN, (it + 1) & 1);
+            ids = ids_of(start + (it + 2) * BN);
+        }
+    };
+    for (int it = 0; it < steps;) {
+        const int part_to = it < whole_from ? whole_from : steps;
+        if (it < whole_from || it >= whole_to) {
+            for (; it < part_to; ++it) {
+                next_step(it);
+                const int key0 = start + it * BN + kw;
+                if (wave_rows && key0 < hi_w && key0 + 32 * KB > lo_w) step(std::false_type{}, key0, it & 1);
             }
-            compute(kt, it & 1);
+        }
+        for (; it < whole_to; ++it) {
+            next_step(it);
+            step(std::true_type{}, 0, it & 1);
         }
     }
     l += __shfl_xor(l, 32);
+    dirty = __any(dirty);
 
     if constexpr (WK > 1) {
         // join the key groups: the sums of group g > 0 through LDS, in order
-        static_assert(WR * (BLK * 16 + 2) * 64 * 4 <= 4 * TILE, "sums of a key group must fit");
-        __attribute__((address_space(3))) float *box = (__attribute__((address_space(3))) float *)(lds_char *)smem +
-                                                       wr * (BLK * 16 + 2) * 64 + lane;
+        constexpr int BOX = (BLK * 16 + 3) * 64;          // words a wave
+        static_assert(WR * BOX * 4 <= 4 * TILE, "sums of a key group must fit");
+        __attribute__((address_space(3))) float *box = (__attribute__((address_space(3))) float *)(lds_char *)smem + wr * BOX + lane;
 #pragma unroll
         for (int g = 1; g < WK; ++g) {
             lds_barrier();
             if (wk == g) {
                 box[0] = m;
                 box[64] = l;
+                box[128] = dirty ? 1.f : 0.f;
 #pragma unroll
                 for (int blk = 0; blk < BLK; ++blk)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) box[(2 + blk * 16 + i) * 64] = acc[blk][i];
+                    for (int i = 0; i < 16; ++i) box[(3 + blk * 16 + i) * 64] = acc[blk][i];
             }
             lds_barrier();
             if (wk == 0) {
                 const float om = box[0], ol = box[64];
+                dirty |= box[128] != 0.f;
                 const float next = fmaxf(m, om);
                 const float off = next == -__builtin_inff() ? 0.f : next;
                 const float mine = exp2_fast((m - off) * scale), theirs = exp2_fast((om - off) * scale);
@@ -361,18 +466,26 @@ attention_tiles_kernel(AttentionParams p)
 #pragma unroll
                 for (int blk = 0; blk < BLK; ++blk)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[blk][i] = acc[blk][i] * mine + box[(2 + blk * 16 + i) * 64] * theirs;
+                    for (int i = 0; i < 16; ++i) acc[blk][i] = acc[blk][i] * mine + box[(3 + blk * 16 + i) * 64] * theirs;
             }
         }
         if (wk != 0) return;
     }
 
+    if (__any(dirty)) {
+        // a step that some of the rows saw only in part held a value that is not
+        // finite: 0 times it has spoilt rows that do not see it.  The wave's rows
+        // are taken anew, key by key (rare: correctness, not speed)
+#pragma unroll 1
+        for (int i = 0; i < 32 && t.r0 + 32 * wr + i <= r_last; ++i)
+            redo_row<T, DP>(p, t, head, split, t.r0 + 32 * wr + i, k0, k1, lane);
+        return;
+    }
     if (t.r0 + 32 * wr + n > r_last) return;
     // block g VW + e holds dims 32 VW g + VW j + e, j = 8 (i / 4) + 4 h + i % 4: runs of 4 VW dims
     const bool sees = hi > lo;
     const float inv = p.splits == 1 ? 1.f / l : 1.f;
-    const long long row = (long long)token * p.q_heads + q_head;
-    const long long at = (long long)split * p.batch.tokens * p.q_heads + row;
+    const long long at = ((long long)split * p.batch.tokens + token) * p.q_heads + q_head;
     T *dst = (T *)p.o.p + (long long)token * p.o.tok + (long long)q_head * p.o.head;
 #pragma unroll
     for (int g = 0; g < BLK / VW; ++g)
@@ -390,7 +503,7 @@ attention_tiles_kernel(AttentionParams p)
                     quad out;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) out[e] = (T)(sees ? o[e] * inv : 0.f);
-                    if constexpr (VEC) {
+                    if constexpr (HOW != ANY) {
                         if (d < dim) *(quad *)(dst + d) = out;
                     } else {
                         for (int e = 0; e < 4; ++e)
@@ -400,25 +513,29 @@ attention_tiles_kernel(AttentionParams p)
                     if (d < dim) *(f32x4 *)(p.part + at * p.part_dim + d) = f32x4{o[0], o[1], o[2], o[3]};
                 }
             }
-    if (p.splits > 1 && h == 0) {
-        // a sum that is a NaN stays one in the join (weight exp2(inf - inf));
-        // keys seen, but only logits of -inf: 0 / 0 unless another split has more
-        p.stat[at * 2] = l != l ? __builtin_inff() : m * scale;
-        p.stat[at * 2 + 1] = sees && l == 0.f ? __builtin_nanf("") : l;
-    }
+    if (p.splits > 1 && h == 0) store_stat(p, at, m * scale, l, sees);
 }
 
-template <typename T, int DP, bool VEC, int KB>
+template <typename T, int DP, int HOW, int KB>
 hipError_t launch_shape(const AttentionParams &p, int tile_rows, int grid, hipStream_t stream)
 {
     if (tile_rows == 128) {
-        attention_tiles_kernel<T, DP, VEC, 4, 1, KB><<<grid, 256, 0, stream>>>(p);
+        attention_tiles_kernel<T, DP, HOW, 4, 1, KB><<<grid, 256, 0, stream>>>(p);
     } else if constexpr (DP <= 128) {
-        attention_tiles_kernel<T, DP, VEC, 2, 2, 1><<<grid, 256, 0, stream>>>(p);
+        attention_tiles_kernel<T, DP, HOW, 2, 2, 1><<<grid, 256, 0, stream>>>(p);
     } else {
         return hipErrorInvalidValue;   // the plan asks for none
     }
     return hipGetLastError();
+}
+
+template <typename T, int DP, int KB>
+hipError_t launch_chunks(const AttentionParams &p, int tile_rows, int grid, hipStream_t stream)
+{
+    // lane offsets of PAGED16 are 32 bits: at most 8 keys and a row
+    const bool near = p.pool.k_tok < (1u << 24) && p.pool.v_tok < (1u << 24);
+    return p.dim == DP && p.pool.page_size.d % 16 == 0 && near ? launch_shape<T, DP, PAGED16, KB>(p, tile_rows, grid, stream)
+                                                               : launch_shape<T, DP, CHUNKS, KB>(p, tile_rows, grid, stream);
 }
 
 template <typename T>
@@ -426,13 +543,13 @@ hipError_t launch_tiles(const AttentionParams &p, int tile_rows, bool vec, int g
 {
     constexpr int KB = sizeof(T) == 2 ? 2 : 1;
     if (!vec) {
-        return p.dim <= 128 ? launch_shape<T, 128, false, KB>(p, tile_rows, grid, stream)
-                            : launch_shape<T, 256, false, 1>(p, tile_rows, grid, stream);
+        return p.dim <= 128 ? launch_shape<T, 128, ANY, KB>(p, tile_rows, grid, stream)
+                            : launch_shape<T, 256, ANY, 1>(p, tile_rows, grid, stream);
     }
-    if (p.dim <= 64) return launch_shape<T, 64, true, KB>(p, tile_rows, grid, stream);
-    if (p.dim <= 96) return launch_shape<T, 96, true, KB>(p, tile_rows, grid, stream);
-    if (p.dim <= 128) return launch_shape<T, 128, true, KB>(p, tile_rows, grid, stream);
-    return launch_shape<T, 256, true, 1>(p, tile_rows, grid, stream);
+    if (p.dim <= 64) return launch_chunks<T, 64, KB>(p, tile_rows, grid, stream);
+    if (p.dim <= 96) return launch_chunks<T, 96, KB>(p, tile_rows, grid, stream);
+    if (p.dim <= 128) return launch_chunks<T, 128, KB>(p, tile_rows, grid, stream);
+    return launch_chunks<T, 256, 1>(p, tile_rows, grid, stream);
 }
 
 }  // namespace

@@ -21,7 +21,7 @@
 // 16 lanes cover a head of 128 contiguously.
 #include "kcommon.h"
 #include "serving.h"
-#include "../../include/nnjit.h"
+#include "nnjit.h"
 
 namespace nnjit {
 
@@ -59,8 +59,8 @@ rotary_kernel(RotaryParams p)
             const int page = b.page_table[(long long)seq * b.ld_table + pi];
             if (page >= 0 && page < p.pool.pages) {
                 const int slot = pos - pi * (int)p.pool.page_size.d;
-                kdst = (D *)p.pool.k + (long long)page * p.pool.k_page + (long long)slot * p.pool.k_tok;
-                vdst = (D *)p.pool.v + (long long)page * p.pool.v_page + (long long)slot * p.pool.v_tok;
+                kdst = (D *)p.pool.k + page_offset(page, p.pool.k_page, slot, p.pool.k_tok);
+                vdst = (D *)p.pool.v + page_offset(page, p.pool.v_page, slot, p.pool.v_tok);
             }
         }
     } else {

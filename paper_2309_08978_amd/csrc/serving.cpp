@@ -4,7 +4,7 @@
 #include <cmath>
 #include <cstdint>
 
-#include "../../include/nnjit.h"
+#include "nnjit.h"
 #include "serving.h"
 
 namespace nnjit {
@@ -65,6 +65,8 @@ int check_cache(const nnjit_paged_kv *c) {
     if (!c->k || !c->v) return runtime_fail(NNJIT_EINVAL, "the cache's K or V is NULL");
     if (c->k_page < 0 || c->k_token < 0 || c->k_head < 0 || c->v_page < 0 || c->v_token < 0 || c->v_head < 0)
         return runtime_fail(NNJIT_EINVAL, "negative stride of the cache");
+    if (std::max({c->k_page, c->k_token, c->v_page, c->v_token}) > (int64_t)0xffffffff)
+        return runtime_fail(NNJIT_EINVAL, "page and token strides of the cache must be below 2^32 elements");
     return NNJIT_OK;
 }
 
@@ -85,11 +87,11 @@ PagePool pool_of(const nnjit_paged_kv *c) {
     PagePool p;
     p.k = c->k;
     p.v = c->v;
-    p.k_page = c->k_page;
-    p.k_tok = c->k_token;
+    p.k_page = (unsigned)c->k_page;
+    p.k_tok = (unsigned)c->k_token;
     p.k_head = c->k_head;
-    p.v_page = c->v_page;
-    p.v_tok = c->v_token;
+    p.v_page = (unsigned)c->v_page;
+    p.v_tok = (unsigned)c->v_token;
     p.v_head = c->v_head;
     p.pages = (int)c->pages;
     p.page_size = FastDiv((unsigned)c->page_size);

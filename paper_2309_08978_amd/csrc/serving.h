@@ -10,22 +10,30 @@ namespace nnjit {
 // Largest head dimension of the serving operators.
 constexpr int kMaxHeadDim = 256;
 
-// n / d and n % d for 0 <= n < 2^31 by one multiplication (d >= 1): with
-// 2^(l-1) < d <= 2^l and mul = ceil(2^(31+l) / d), which is below 2^32, the
-// quotient is floor(n mul / 2^(31+l)) (Granlund and Montgomery, "Division by
-// invariant integers using multiplication", 1994).
+// n / d for 0 <= n < 2^31 by one multiplication (d >= 1): with
+// 2^(l-1) < d <= 2^l, l >= 1, and mul = ceil(2^(31+l) / d), which is below
+// 2^32, the quotient is floor(n mul / 2^(31+l)) (Granlund and Montgomery,
+// "Division by invariant integers using multiplication", 1994).  d = 1 takes n
+// itself in the place of the product's upper half.
 struct FastDiv {
     unsigned d, mul;
-    int shift;
-    FastDiv() : d(1), mul(1u << 31), shift(31) {}
-    explicit FastDiv(unsigned div) : d(div)
+    int shift;                 // l - 1
+    unsigned self;             // all ones for d = 1
+    FastDiv() : FastDiv(1) {}
+    explicit FastDiv(unsigned div) : d(div), mul(0), shift(0), self(~0u)
     {
-        int l = 0;
+        if (div == 1) return;
+        int l = 1;
         while ((1ull << l) < div) ++l;
-        shift = 31 + l;
-        mul = (unsigned)(((1ull << shift) + div - 1) / div);
+        mul = (unsigned)(((1ull << (31 + l)) + div - 1) / div);
+        shift = l - 1;
+        self = 0;
     }
-    __host__ __device__ __forceinline__ int quot(int n) const { return (int)(((unsigned long long)(unsigned)n * mul) >> shift); }
+    __host__ __device__ __forceinline__ int quot(int n) const
+    {
+        const unsigned upper = (unsigned)(((unsigned long long)(unsigned)n * mul) >> 32);
+        return (int)((upper + ((unsigned)n & self)) >> shift);
+    }
 };
 
 // One tensor of head rows: element (row, head, i) at p[row * tok + head * head + i].
@@ -38,11 +46,16 @@ struct HeadRows {
 // k[page * k_page + slot * k_tok + head * k_head + i], V alike.
 struct PagePool {
     void *k, *v;
-    long long k_page, k_tok, k_head;
-    long long v_page, v_tok, v_head;
+    unsigned k_page, k_tok, v_page, v_tok;   // below 2^32 elements; offsets are taken in 64 bits
+    long long k_head, v_head;
     int pages;
     FastDiv page_size;
 };
+
+__device__ __forceinline__ long long page_offset(int page, unsigned page_stride, int slot, unsigned tok_stride)
+{
+    return (long long)((unsigned long long)(unsigned)page * page_stride + (unsigned long long)(unsigned)slot * tok_stride);
+}
 
 // The batch: device arrays as described in include/nnjit.h.
 struct PageBatch {

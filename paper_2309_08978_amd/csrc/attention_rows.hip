@@ -32,6 +32,7 @@
 // second kernel joins the splits in their order, so results do not depend on
 // which workgroup finishes first.
 #include <algorithm>
+#include <cmath>
 
 #include "attention_common.h"
 #include "nnjit.h"
@@ -403,14 +404,22 @@ attention_join_kernel(AttentionParams p)
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
     bool none = false;
     if (live) {
-        for (int s = 0; s < p.splits; ++s) {
+        // the largest logit: a lane per split
+        for (int s = lane; s < p.splits; s += LPR) {
             const f32x2 st = *(const f32x2 *)(p.stat + (s * rows + row) * 2);
             most = fmaxf(most, st[0]);
             none |= st[1] != st[1];
         }
+    }
+#pragma unroll
+    for (int i = 1; i < LPR; i <<= 1) {
+        most = fmaxf(most, __shfl_xor(most, i));
+        none |= (bool)__shfl_xor((int)none, i);
+    }
+    if (live) {
         const float off = most == -__builtin_inff() ? 0.f : most;
         const int d = min(4 * lane, p.part_dim - 4);
-#pragma unroll 4
+#pragma unroll 8
         for (int s = group % GPR; s < p.splits; s += GPR) {
             const long long at = s * rows + row;
             const f32x2 st = *(const f32x2 *)(p.stat + at * 2);
@@ -481,34 +490,73 @@ hipError_t launch_typed(const AttentionParams &p, bool vec, int grid, hipStream_
 
 }  // namespace
 
+namespace {
+
+// Estimated time of a step of a kernel's workgroups: max(a, b o) us with `o`
+// workgroups to a compute unit, linear in the head dimension d (in units of
+// 128), and no less than its bytes at 5.5 TB/s.  Fitted to measured times (within about 15% over 64 .. 8192 keys, 8 ..
+// 384 sequences times key heads, dims 64 and 128): a is a step's latency, b its
+// share of a CU's matrix cores and LDS.
+struct StepCost {
+    int tile_rows, keys;       // rows of a tile; keys of a step
+    double a0, a1, b0, b1;     // a = a0 + a1 d, b = b0 + b1 d
+};
+constexpr StepCost kStepF16[] = {{16, 128, 1.5, 0, 0.5, 1.0}, {64, 64, 0.35, 0.8, 0.325, 0.35}, {128, 64, 0.5, 1.1, 0.4, 0.65}};
+constexpr StepCost kStepF32[] = {{16, 64, 0.9, 1.2, 0.5, 1.0}, {64, 64, 0.3, 4.6, 0, 4.7}, {128, 64, 1.6, 7.4, 0, 7.6}};
+
+}  // namespace
+
+// The kernel and the splits of the keys that these estimates call cheapest.
+// Tall tiles read keys and values least often but leave CUs idle where rows are
+// few (512 new tokens on 3584 cached, 32 heads of 128, in us: 128 rows unsplit 93,
+// 64 rows 82, in two splits 59, 128 rows in four 55; 777 alone: 25, 23, 40, 42);
+// up to 128 rows of up to 128 keys the 16-row kernel starts soonest (7 against 8);
+// a split costs a second launch and writes and reads the partial sums (512 new
+// tokens alone: 16 unsplit, 28 in two).
 AttentionPlan attention_plan(int dtype, int64_t tokens, int64_t sequences, int q_heads, int kv_heads, int dim, int64_t max_q,
                              int64_t max_kv, int causal, int64_t window, int cus)
 {
-    AttentionPlan plan{};
-    const int64_t group = q_heads / kv_heads, rows = max_q * group;
-    const int64_t lanes = (int64_t)kv_heads * sequences;
-    auto tiles = [&](int64_t n) { return (rows + n - 1) / n; };
-    // few rows: 16-row tiles, each wave with keys of its own; many: 128-row tiles
-    // of four waves, or of 64 where those would leave compute units idle
-    plan.tile_rows = rows <= 32 ? 16 : dim > 128 || tiles(128) * lanes >= cus ? 128 : 64;
-    plan.row_tiles = (int)tiles(plan.tile_rows);
-    // keys that one tile can see: with a window, from the first row's first key
-    // (rounded down to a multiple of 32) to the last row's last
-    int64_t span = max_kv;
-    if (causal && window > 0) {
-        const int64_t tokens_of_tile = (plan.tile_rows + group - 1) / group + 1;
-        if (window < span) span = std::min(span, window + tokens_of_tile + 31);
+    const int64_t group = q_heads / kv_heads, rows = max_q * group, lanes = (int64_t)kv_heads * sequences;
+    const int elt = dtype == NNJIT_F16 ? 2 : 4;
+    const double d = dim / 128.0, part_us = (double)tokens * q_heads * dim * 8 / 3.3e6;   // partial sums of a split, written and read
+    AttentionPlan best{};
+    double least = 0;
+    for (const StepCost &c : dtype == NNJIT_F16 ? kStepF16 : kStepF32) {
+        if (c.tile_rows == 64 && dim > 128) continue;      // not built: registers
+        if (c.tile_rows > 16 && rows <= 16) break;         // tiles that rows do not fill are no better, and less exact
+        const int64_t row_tiles = (rows + c.tile_rows - 1) / c.tile_rows;
+        // keys that one tile can see: with a window, from the first row's first key
+        // (rounded down to a multiple of 32) to the last row's last
+        int64_t span = max_kv;
+        if (causal && window > 0 && window < span) span = std::min(span, window + (c.tile_rows + group - 1) / group + 32);
+        for (int64_t want = 1; want <= 256; want = want < 4 ? want + 1 : want * 3 / 2 - want * 3 / 2 % 2) {
+            const int64_t per = (span + want - 1) / want;
+            const int64_t split_keys = std::max<int64_t>((per + 31) / 32 * 32, 32);
+            const int64_t splits = std::max<int64_t>((span + split_keys - 1) / split_keys, 1);
+            const double o = (double)row_tiles * lanes * splits / cus;
+            // keys and values come once from memory for all row tiles; one workgroup a CU does
+            // not draw its full rate, a few CUs with one more take longer, and so do
+            // sequences of different lengths unless there are many workgroups
+            const double even = o < 4 ? std::ceil(o) : o;
+            double bytes_us = 2.0 * c.keys * dim * elt * (even / row_tiles) * 256 / (5.5e6 * std::min(1.0, 0.9 + 0.05 * o));
+            if (sequences > 1 && o < 8) bytes_us *= 1.15;
+            // fp32 products fill the matrix cores of a CU: its second workgroup takes as long again
+            const double share = elt == 4 && c.tile_rows > 16 ? std::ceil(o) : o;
+            const double step = std::max({c.a0 + c.a1 * d, (c.b0 + c.b1 * d) * share, bytes_us});
+            const double cost = ((split_keys < span ? split_keys : span) + c.keys - 1) / c.keys * step + (splits > 1 ? 3.8 + splits * part_us : 0) +
+                                (c.tile_rows == 16 ? 0 : 1.5);   // a later start: copies, then products
+            if (best.tile_rows == 0 || cost < least) {
+                least = cost;
+                best.tile_rows = c.tile_rows;
+                best.row_tiles = (int)row_tiles;
+                best.splits = (int)splits;
+                best.split_keys = (int)split_keys;
+            }
+            if (splits < want || o > 16) break;            // more splits than keys, or than the chip holds
+        }
     }
-    const int64_t groups = plan.row_tiles * lanes;
-    // two workgroups a compute unit, each with a few key tiles at least
-    const int64_t least = plan.tile_rows == 16 ? (dtype == NNJIT_F16 ? 128 : 64) : 256;
-    int64_t splits = (2 * (int64_t)cus + groups - 1) / groups;
-    splits = std::max<int64_t>(std::min(splits, (span + least - 1) / least), 1);
-    const int64_t per = (span + splits - 1) / splits;
-    plan.split_keys = (int)std::max<int64_t>((per + 31) / 32 * 32, 32);
-    plan.splits = (int)std::max<int64_t>((span + plan.split_keys - 1) / plan.split_keys, 1);
-    plan.ws_floats = plan.splits > 1 ? plan.splits * tokens * q_heads * ((dim + 3) / 4 * 4 + 2) : 0;
-    return plan;
+    best.ws_floats = best.splits > 1 ? best.splits * tokens * q_heads * ((dim + 3) / 4 * 4 + 2) : 0;
+    return best;
 }
 
 hipError_t launch_attention(AttentionParams p, const AttentionPlan &plan, int dtype, bool vec, hipStream_t stream)

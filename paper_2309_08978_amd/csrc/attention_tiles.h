@@ -127,15 +127,15 @@ __device__ __forceinline__ void redo_row(const AttentionParams &p, const RowTile
     if (p.splits > 1 && lane == 0) store_stat(p, at, m * p.scale_log2, l, hi > lo);
 }
 
-// Bytes of a row in LDS, and how many workgroups' waves a SIMD holds beside
-// each other (two unless the buffers or the registers of one fill a CU).
+// Bytes of a row in LDS, and the waves a SIMD is to hold: two, of two
+// workgroups, unless the buffers or the registers of one fill a CU.
 template <typename T, int DP>
 constexpr int row_pitch() { return (DP <= 64 ? 64 : DP <= 128 ? 128 : 256) * (int)sizeof(T); }
 template <typename T, int DP, int BLOCKS>
-constexpr int tiles_per_simd() { return DP <= 128 && 4 * 32 * BLOCKS * row_pitch<T, DP>() <= 80 * 1024 ? 2 : 1; }
+constexpr int waves_per_simd() { return DP <= 128 && 4 * 32 * BLOCKS * row_pitch<T, DP>() <= 80 * 1024 ? 2 : 1; }
 
 template <typename T, int DP, int HOW, int WR, int WK, int KB>
-__global__ void __launch_bounds__(WR * WK * 64, (tiles_per_simd<T, DP, KB * WK>()))
+__global__ void __launch_bounds__(WR * WK * 64, (waves_per_simd<T, DP, KB * WK>()))
 attention_tiles_kernel(AttentionParams p)
 {
     constexpr bool HALF = sizeof(T) == 2;
@@ -218,35 +218,41 @@ attention_tiles_kernel(AttentionParams p)
     // Copy i of this wave brings KPI keys, key_of[i] the lane's, from the step's
     // first key on.  Page ids are looked up a step before they are used.
     constexpr int KPI = 64 / CPR;
-    auto key_of = [&](int i, int ln) { return (i * NW + wave) * KPI + ln / CPR; };
+    constexpr int WKEYS = NI * KPI;                       // keys that a wave copies: 8 or 16 in a row
+    static_assert(16 % WKEYS == 0, "a wave's keys must lie in one page of 16");
+    auto key_of = [&](int i, int ln) { return wave * WKEYS + i * KPI + ln / CPR; };
     auto k_col = [&](int i, int ln) { return ((ln % CPR) ^ k_swz(key_of(i, ln))) * CH; };
     auto v_col = [&](int i, int ln) { return ((ln % CPR) ^ v_swz(key_of(i, ln))) * CH; };
+    constexpr int IDS = HOW == PAGED16 ? 1 : NI;
     struct Ids {
-        int page[NI];
+        int page[IDS];
     };
     auto ids_of = [&](int kt) {
         Ids ids;
 #pragma unroll
-        for (int i = 0; i < NI; ++i)
+        for (int i = 0; i < IDS; ++i)
             ids.page[i] = t.table[p.pool.page_size.quot(min(kt + key_of(i, HOW == PAGED16 ? 0 : lane), last_key))];
         return ids;
     };
-    auto copy_step = [&](const Ids &ids, int kt, int b) {
-        const unsigned k_lds = (unsigned)(uintptr_t)k_buf(b) + wave * 1024, v_lds = (unsigned)(uintptr_t)v_buf(b) + wave * 1024;
+    auto copy_rows = [&](auto of_keys, const Ids &ids, int kt, int b) {
+        constexpr bool KEYS = decltype(of_keys)::value;
+        lds_char *buf = KEYS ? k_buf(b) : v_buf(b);
+        const T *base = KEYS ? kp : vp;
+        const unsigned page_stride = KEYS ? p.pool.k_page : p.pool.v_page, tok_stride = KEYS ? p.pool.k_tok : p.pool.v_tok;
+        const unsigned lds = (unsigned)(uintptr_t)buf + wave * NI * 1024;
         int ln = lane;
         if constexpr (HOW == PAGED16) {
             if (kt >= first && kt + BN <= k1) {
-                // every key is there and a copy's keys lie in one page: scalar addresses, lane offsets that never change
+                // every key is there, the wave's lie in one page: a scalar address, lane offsets that never change
+                const int key = kt + key_of(0, 0);
+                const int slot = key - p.pool.page_size.quot(key) * page_size;
+                const int page = safe_page(p, __builtin_amdgcn_readfirstlane(ids.page[0]));
+                const T *src = base + page_offset(page, page_stride, slot, tok_stride);
 #pragma unroll
                 for (int i = 0; i < NI; ++i) {
-                    const int key = kt + key_of(i, 0);
-                    const int slot = key - p.pool.page_size.quot(key) * page_size;
-                    const int page = safe_page(p, __builtin_amdgcn_readfirstlane(ids.page[i]));
-                    const T *ks = kp + page_offset(page, p.pool.k_page, slot, p.pool.k_tok);
-                    const T *vs = vp + page_offset(page, p.pool.v_page, slot, p.pool.v_tok);
-                    const int kc = k_col(i, lane), vc = v_col(i, lane);   // past dim (DP 96 in rows of 128): never read
-                    copy16_to_lds_from(ks, ((unsigned)(lane / CPR) * p.pool.k_tok + (kc < DP ? kc : 0)) * (unsigned)sizeof(T), k_lds + i * NW * 1024);
-                    copy16_to_lds_from(vs, ((unsigned)(lane / CPR) * p.pool.v_tok + (vc < DP ? vc : 0)) * (unsigned)sizeof(T), v_lds + i * NW * 1024);
+                    const int col = KEYS ? k_col(i, lane) : v_col(i, lane);   // past dim (DP 96 in rows of 128): never read
+                    copy16_to_lds_from(src + i * KPI * tok_stride,
+                                       ((unsigned)(lane / CPR) * tok_stride + (col < DP ? col : 0)) * (unsigned)sizeof(T), lds + i * 1024);
                 }
                 return;
             }
@@ -254,24 +260,19 @@ attention_tiles_kernel(AttentionParams p)
         }
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            const int at = kt + key_of(i, ln), kc = k_col(i, ln), vc = v_col(i, ln);
+            const int at = kt + key_of(i, ln), col = KEYS ? k_col(i, ln) : v_col(i, ln);
             const int key = min(at, last_key);
-            const int slot = key - p.pool.page_size.quot(key) * page_size, page = safe_page(p, ids.page[i]);
-            const T *ks = kp + page_offset(page, p.pool.k_page, slot, p.pool.k_tok) + kc;
-            const T *vs = vp + page_offset(page, p.pool.v_page, slot, p.pool.v_tok) + vc;
+            const int slot = key - p.pool.page_size.quot(key) * page_size;
+            // PAGED16: keys past the last one are taken from the page of the wave's first (and replaced by zeros)
+            const T *src = base + page_offset(safe_page(p, ids.page[HOW == PAGED16 ? 0 : i]), page_stride, slot, tok_stride) + col;
             // keys that no row sees are zeros: what lies in their slots must not be multiplied, not even by 0
             const bool ok = at >= first && at < k1;
             if constexpr (HOW != ANY) {
-                copy16_to_lds(ok && kc < dim ? ks : (const T *)p.zero, __builtin_amdgcn_readfirstlane(k_lds + i * NW * 1024));
-                copy16_to_lds(ok && vc < dim ? vs : (const T *)p.zero, __builtin_amdgcn_readfirstlane(v_lds + i * NW * 1024));
+                copy16_to_lds(ok && col < dim ? src : (const T *)p.zero, __builtin_amdgcn_readfirstlane(lds + i * 1024));
             } else {
-                chunk ke, ve;
-                for (int e = 0; e < CH; ++e) {
-                    ke[e] = ok && kc + e < dim ? ks[e] : (T)0;
-                    ve[e] = ok && vc + e < dim ? vs[e] : (T)0;
-                }
-                *(__attribute__((address_space(3))) chunk *)(k_buf(b) + (i * NW + wave) * 1024 + lane * 16) = ke;
-                *(__attribute__((address_space(3))) chunk *)(v_buf(b) + (i * NW + wave) * 1024 + lane * 16) = ve;
+                chunk x;
+                for (int e = 0; e < CH; ++e) x[e] = ok && col + e < dim ? src[e] : (T)0;
+                *(__attribute__((address_space(3))) chunk *)(buf + (wave * NI + i) * 1024 + lane * 16) = x;
             }
         }
     };
@@ -408,7 +409,8 @@ attention_tiles_kernel(AttentionParams p)
     Ids ids;
     if (steps > 0) {
         ids = ids_of(start);
-        copy_step(ids, start, 0);
+        copy_rows(std::true_type{}, ids, start, 0);
+        copy_rows(std::false_type{}, ids, start, 0);
         ids = ids_of(start + BN);
     }
     auto next_step = [&](int it) {
@@ -416,7 +418,8 @@ attention_tiles_kernel(AttentionParams p)
         wait_vmcnt<0>();
         lds_barrier();
         if (it + 1 < steps) {
-            copy_step(ids, start + (it + 1) * BN, (it + 1) & 1);
+            copy_rows(std::true_type{}, ids, start + (it + 1) * BN, (it + 1) & 1);
+            copy_rows(std::false_type{}, ids, start + (it + 1) * BN, (it + 1) & 1);
             ids = ids_of(start + (it + 2) * BN);
         }
     };
@@ -438,38 +441,39 @@ attention_tiles_kernel(AttentionParams p)
     dirty = __any(dirty);
 
     if constexpr (WK > 1) {
-        // join the key groups: the sums of group g > 0 through LDS, in order
+        // join the key groups: those of groups 1 .. WK - 1 through LDS, in order
         constexpr int BOX = (BLK * 16 + 3) * 64;          // words a wave
-        static_assert(WR * BOX * 4 <= 4 * TILE, "sums of a key group must fit");
-        __attribute__((address_space(3))) float *box = (__attribute__((address_space(3))) float *)(lds_char *)smem + wr * BOX + lane;
+        static_assert(WR * (WK - 1) * BOX * 4 <= 4 * TILE, "sums of the key groups must fit");
+        typedef __attribute__((address_space(3))) float lds_float;
+        auto box_of = [&](int g) { return (lds_float *)(lds_char *)smem + (wr * (WK - 1) + g - 1) * BOX + lane; };
+        lds_barrier();
+        if (wk > 0) {
+            lds_float *box = box_of(wk);
+            box[0] = m;
+            box[64] = l;
+            box[128] = dirty ? 1.f : 0.f;
+#pragma unroll
+            for (int blk = 0; blk < BLK; ++blk)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) box[(3 + blk * 16 + i) * 64] = acc[blk][i];
+        }
+        lds_barrier();
+        if (wk > 0) return;
 #pragma unroll
         for (int g = 1; g < WK; ++g) {
-            lds_barrier();
-            if (wk == g) {
-                box[0] = m;
-                box[64] = l;
-                box[128] = dirty ? 1.f : 0.f;
+            lds_float *box = box_of(g);
+            const float om = box[0], ol = box[64];
+            dirty |= box[128] != 0.f;
+            const float next = fmaxf(m, om);
+            const float off = next == -__builtin_inff() ? 0.f : next;
+            const float mine = exp2_fast((m - off) * scale), theirs = exp2_fast((om - off) * scale);
+            m = next;
+            l = l * mine + ol * theirs;
 #pragma unroll
-                for (int blk = 0; blk < BLK; ++blk)
+            for (int blk = 0; blk < BLK; ++blk)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) box[(3 + blk * 16 + i) * 64] = acc[blk][i];
-            }
-            lds_barrier();
-            if (wk == 0) {
-                const float om = box[0], ol = box[64];
-                dirty |= box[128] != 0.f;
-                const float next = fmaxf(m, om);
-                const float off = next == -__builtin_inff() ? 0.f : next;
-                const float mine = exp2_fast((m - off) * scale), theirs = exp2_fast((om - off) * scale);
-                m = next;
-                l = l * mine + ol * theirs;
-#pragma unroll
-                for (int blk = 0; blk < BLK; ++blk)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[blk][i] = acc[blk][i] * mine + box[(3 + blk * 16 + i) * 64] * theirs;
-            }
+                for (int i = 0; i < 16; ++i) acc[blk][i] = acc[blk][i] * mine + box[(3 + blk * 16 + i) * 64] * theirs;
         }
-        if (wk != 0) return;
     }
 
     if (__any(dirty)) {

@@ -677,11 +677,13 @@ class PagedBatch:
 
 def _head_rows(name: str, t, tokens, heads, dim, dtype, device_index):
     """Strides (token, head) of head rows, checked."""
-    if t.dim() != 3 or t.shape[0] != tokens or (heads is not None and t.shape[1] != heads) or t.shape[2] != dim:
-        raise ValueError(f"{name} must be [{tokens}, {'heads' if heads is None else heads}, {dim}], got {tuple(t.shape)}")
+    st = t.stride()
+    if t.shape == (tokens, heads, dim) and t.dtype is dtype and st[2] == 1 and t.get_device() == device_index:
+        return st
+    if t.dim() != 3 or t.shape[0] != tokens or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError(f"{name} must be [{tokens}, {heads}, {dim}], got {tuple(t.shape)}")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    st = t.stride()
     if st[2] != 1 and dim > 1:
         raise ValueError(f"{name} must have unit stride along the last dimension")
     if not t.is_cuda or t.get_device() != device_index:
@@ -701,22 +703,24 @@ def rotary(x, positions, table: RotaryTable, out=None, transpose: bool = False, 
     [tokens]); ``transpose``: by the opposite ones (the gradient).  ``out``
     (fp32 or fp16, allocated like x if None) may be x."""
     torch = _torch()
-    if x.dim() != 3:
-        raise ValueError(f"x must be [tokens, heads, head_dim], got {tuple(x.shape)}")
-    tokens, heads, dim = x.shape
+    shape = x.shape
+    if len(shape) != 3:
+        raise ValueError(f"x must be [tokens, heads, head_dim], got {tuple(shape)}")
+    tokens, heads, dim = shape
     if out is None:
         out = torch.empty((tokens, heads, dim), dtype=x.dtype, device=x.device)
-    if x.dtype not in _CODES or out.dtype not in _CODES:
-        raise TypeError(f"unsupported dtype {x.dtype} to {out.dtype}")
-    sx = _head_rows("x", x, tokens, heads, dim, x.dtype, table.device_index)
-    sy = _written_rows("out", out, tokens, heads, dim, out.dtype, table.device_index)
-    if positions.shape != (tokens,) or positions.dtype is not torch.int32 or positions.get_device() != table.device_index:
+    xd, yd, dev = x.dtype, out.dtype, table.device_index
+    if xd not in _CODES or yd not in _CODES:
+        raise TypeError(f"unsupported dtype {xd} to {yd}")
+    sx = _head_rows("x", x, tokens, heads, dim, xd, dev)
+    sy = _written_rows("out", out, tokens, heads, dim, yd, dev)
+    if positions.shape != (tokens,) or positions.dtype is not torch.int32 or positions.get_device() != dev:
         raise ValueError(f"positions must be int32 of shape ({tokens},) on x's GPU, got {positions.dtype} {tuple(positions.shape)}")
     if tokens > 1 and positions.stride(0) != 1:
         raise ValueError("positions must be contiguous")
     check((_lib or load()).nnjit_rotary(table.address, tokens, heads, dim, positions.data_ptr(), x.data_ptr(), sx[0], sx[1],
-                                        _CODES[x.dtype], out.data_ptr(), sy[0], sy[1], _CODES[out.dtype],
-                                        1 if transpose else 0, _stream(stream)))
+                                        _CODES[xd], out.data_ptr(), sy[0], sy[1], _CODES[yd], 1 if transpose else 0,
+                                        _stream(stream)))
     return out
 
 
@@ -757,9 +761,10 @@ def paged_attention(q, cache: PagedCache, batch: PagedBatch, out=None, scale: Op
     of every row's sequence; q and out are of the cache's type.  ``scale``
     defaults to head_dim ** -0.5; ``window`` > 0: the last ``window`` keys only."""
     torch = _torch()
-    if q.dim() != 3:
-        raise ValueError(f"q must be [tokens, heads, head_dim], got {tuple(q.shape)}")
-    heads, dim, dev = q.shape[1], cache.head_dim, cache.device_index
+    shape = q.shape
+    if len(shape) != 3:
+        raise ValueError(f"q must be [tokens, heads, head_dim], got {tuple(shape)}")
+    heads, dim, dev = shape[1], cache.head_dim, cache.device_index
     if batch.device_index != dev:
         raise ValueError("cache and batch must be on one GPU")
     sq = _head_rows("q", q, batch.tokens, heads, dim, cache.dtype, dev)

@@ -84,6 +84,34 @@ __device__ __forceinline__ float add_classes(float sum, float counts)
     return sum + __builtin_bit_cast(float, add);
 }
 
+// Elements col .. col + 7 of a row, zeros at and past `room`.
+template <bool VEC>
+__device__ __forceinline__ f32x8 load_eight(const float *row, int col, int room)
+{
+    f32x8 x = {};
+    if constexpr (VEC) {
+        f32x4 a = {}, b = {};
+        if (col < room) a = *(const f32x4 *)(row + col);
+        if (col + 4 < room) b = *(const f32x4 *)(row + col + 4);
+        x = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+        for (int i = 0; i < 8; ++i) x[i] = col + i < room ? row[col + i] : 0.f;
+    }
+    return x;
+}
+
+// Whether eight values are their bf16 parts' sums: finite, and none rounds to a bf16 infinity.
+__device__ __forceinline__ bool splittable(f32x8 x)
+{
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float v = x[i];
+        top = max(top, __builtin_bit_cast(unsigned, v) & 0x7fffffffu);
+    }
+    return top < 0x7f7f8000u;
+}
+
 // Largest magnitude of halves, two at a time as integers (an infinity or NaN is
 // the largest of all).
 struct Largest16 {

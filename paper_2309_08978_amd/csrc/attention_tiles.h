@@ -53,7 +53,10 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 // (pages of a multiple of 16 tokens) and whole head dims (dim == DP), addresses
 // by scalar arithmetic.  The look-ups of CHUNKS cost about as many vector
 // instructions a step as the softmax.
-enum { ANY, CHUNKS, PAGED16 };
+// SPLIT: fp32 on the bf16 matrix cores (kcommon.h): every chunk is loaded into
+// registers a step ahead, split into three bf16 parts and stored to three
+// planes, each laid out like fp16 rows; SPLIT_ANY loads element by element.
+enum { ANY, CHUNKS, PAGED16, SPLIT, SPLIT_ANY };
 
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"   // m0 is written on purpose
@@ -129,19 +132,23 @@ __device__ __forceinline__ void redo_row(const AttentionParams &p, const RowTile
 
 // Bytes of a row in LDS, and the waves a SIMD is to hold: two, of two
 // workgroups, unless the buffers or the registers of one fill a CU.
-template <typename T, int DP>
-constexpr int row_pitch() { return (DP <= 64 ? 64 : DP <= 128 ? 128 : 256) * (int)sizeof(T); }
-template <typename T, int DP, int BLOCKS>
-constexpr int waves_per_simd() { return DP <= 128 && 4 * 32 * BLOCKS * row_pitch<T, DP>() <= 80 * 1024 ? 2 : 1; }
+template <typename T, int DP, int HOW>
+constexpr int row_pitch() { return (DP <= 64 ? 64 : DP <= 128 ? 128 : 256) * (HOW >= SPLIT ? 2 : (int)sizeof(T)); }
+template <typename T, int DP, int HOW, int BLOCKS>
+constexpr int lds_bytes() { return (HOW >= SPLIT ? 6 : 4) * 32 * BLOCKS * row_pitch<T, DP, HOW>(); }
+template <typename T, int DP, int HOW, int BLOCKS>
+constexpr int waves_per_simd() { return DP <= 128 && lds_bytes<T, DP, HOW, BLOCKS>() <= 80 * 1024 ? 2 : 1; }
 
 template <typename T, int DP, int HOW, int WR, int WK, int KB>
-__global__ void __launch_bounds__(WR * WK * 64, (waves_per_simd<T, DP, KB * WK>()))
+__global__ void __launch_bounds__(WR * WK * 64, (waves_per_simd<T, DP, HOW, KB * WK>()))
 attention_tiles_kernel(AttentionParams p)
 {
-    constexpr bool HALF = sizeof(T) == 2;
+    constexpr bool PARTS = HOW >= SPLIT;                  // fp32 in three bf16 parts
+    constexpr bool VEC = HOW != ANY && HOW != SPLIT_ANY;
+    constexpr bool HALF = sizeof(T) == 2 || PARTS;        // 16-bit rows in LDS
     constexpr int NW = WR * WK;
-    constexpr int CH = 16 / sizeof(T);                    // elements of a chunk
-    constexpr int PITCH = row_pitch<T, DP>();
+    constexpr int CH = HALF ? 8 : 4;                      // elements of a chunk in LDS
+    constexpr int PITCH = row_pitch<T, DP, HOW>();
     constexpr int CPR = PITCH / 16;                       // chunks of a row
     constexpr int BN = 32 * KB * WK;                      // keys of a step
     constexpr int TILE = BN * PITCH;
@@ -149,12 +156,14 @@ attention_tiles_kernel(AttentionParams p)
     static_assert(NI * 64 * NW == BN * CPR, "copies must split evenly over waves");
     constexpr int QS = HALF ? DP / 16 : DP / 8;           // chunks of a query row per lane
     constexpr int BLK = DP / 32;                          // output blocks of 32 dims
-    constexpr int VW = HALF ? 1 : DP % 128 == 0 ? 4 : DP % 64 == 0 ? 2 : 1;   // dims a lane reads side by side
+    constexpr int VW = HALF ? 1 : 4;                      // dims a lane reads side by side
+    static_assert(HALF || DP % 128 == 0, "whole runs of four dims");
     typedef T chunk __attribute__((ext_vector_type(CH)));
 
-    __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];   // K, K, V, V
+    // K, K, V, V: two steps; in parts the three planes of K and of V of one step
+    __shared__ __attribute__((aligned(1024))) char smem[lds_bytes<T, DP, HOW, KB * WK>()];
     auto k_buf = [&](int b) -> lds_char * { return (lds_char *)smem + b * TILE; };
-    auto v_buf = [&](int b) -> lds_char * { return (lds_char *)smem + (2 + b) * TILE; };
+    auto v_buf = [&](int b) -> lds_char * { return (lds_char *)smem + ((PARTS ? 3 : 2) + b) * TILE; };
 
     // chunk c of key row `key` sits at c ^ swizzle
     auto k_swz = [](int key) { return CPR >= 16 ? (key & 15) : ((key >> 1) & 7); };
@@ -194,13 +203,25 @@ attention_tiles_kernel(AttentionParams p)
     const int lo = max(t.first_key(p, r), k0), hi = min(t.end_key(p, r), k1);
     const int dim = p.dim;
 
-    chunk q[QS];
-    {
+    chunk q[PARTS ? 1 : QS];
+    Split8 qp[PARTS ? QS : 1];
+    bool dirty = false;                                   // see redo_row
+    if constexpr (PARTS) {
+        const T *src = (const T *)p.q.p + (long long)token * p.q.tok + (long long)q_head * p.q.head;
+#pragma unroll
+        for (int s = 0; s < QS; ++s) {
+            f32x8 x = load_eight<VEC>((const float *)src, (2 * s + h) * CH, dim);
+            if (p.negate) x = -x;
+            float top = 0.f;
+            qp[s] = split8(x, top);
+            dirty |= !splittable(x);
+        }
+    } else {
         const T *src = (const T *)p.q.p + (long long)token * p.q.tok + (long long)q_head * p.q.head;
 #pragma unroll
         for (int s = 0; s < QS; ++s) {
             const int d = (2 * s + h) * CH;
-            if constexpr (HOW != ANY) {
+            if constexpr (VEC) {
                 q[s] = chunk{};
                 if (d < dim) q[s] = *(const chunk *)(src + d);
             } else {
@@ -219,7 +240,7 @@ attention_tiles_kernel(AttentionParams p)
     // first key on.  Page ids are looked up a step before they are used.
     constexpr int KPI = 64 / CPR;
     constexpr int WKEYS = NI * KPI;                       // keys that a wave copies: 8 or 16 in a row
-    static_assert(16 % WKEYS == 0, "a wave's keys must lie in one page of 16");
+    static_assert(HOW != PAGED16 || 16 % WKEYS == 0, "a wave's keys must lie in one page of 16");
     auto key_of = [&](int i, int ln) { return wave * WKEYS + i * KPI + ln / CPR; };
     auto k_col = [&](int i, int ln) { return ((ln % CPR) ^ k_swz(key_of(i, ln))) * CH; };
     auto v_col = [&](int i, int ln) { return ((ln % CPR) ^ v_swz(key_of(i, ln))) * CH; };
@@ -267,13 +288,49 @@ attention_tiles_kernel(AttentionParams p)
             const T *src = base + page_offset(safe_page(p, ids.page[HOW == PAGED16 ? 0 : i]), page_stride, slot, tok_stride) + col;
             // keys that no row sees are zeros: what lies in their slots must not be multiplied, not even by 0
             const bool ok = at >= first && at < k1;
-            if constexpr (HOW != ANY) {
+            if constexpr (VEC) {
                 copy16_to_lds(ok && col < dim ? src : (const T *)p.zero, __builtin_amdgcn_readfirstlane(lds + i * 1024));
             } else {
                 chunk x;
                 for (int e = 0; e < CH; ++e) x[e] = ok && col + e < dim ? src[e] : (T)0;
                 *(__attribute__((address_space(3))) chunk *)(buf + (wave * NI + i) * 1024 + lane * 16) = x;
             }
+        }
+    };
+
+    // PARTS: the thread's chunks of a step, loaded and, a step later, stored
+    struct Raw {
+        f32x8 k[PARTS ? NI : 1], v[PARTS ? NI : 1];
+    };
+    auto load_raw = [&](const Ids &ids, int kt) {
+        Raw raw;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int at = kt + key_of(i, lane), col = (lane % CPR) * CH;
+            const int key = min(at, last_key);
+            const int slot = key - p.pool.page_size.quot(key) * page_size, page = safe_page(p, ids.page[HOW >= SPLIT ? i : 0]);
+            // keys that no row sees are zeros
+            const int room = at >= first && at < k1 ? dim : 0;
+            raw.k[i] = load_eight<VEC>((const float *)kp + page_offset(page, p.pool.k_page, slot, p.pool.k_tok), col, room);
+            raw.v[i] = load_eight<VEC>((const float *)vp + page_offset(page, p.pool.v_page, slot, p.pool.v_tok), col, room);
+        }
+        return raw;
+    };
+    auto store_raw = [&](const Raw &raw) {
+        typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int key = key_of(i, lane), c = lane % CPR;
+            dirty |= !splittable(raw.k[i]) || !splittable(raw.v[i]);
+            float top = 0.f;
+            const Split8 ks = split8(raw.k[i], top), vs = split8(raw.v[i], top);
+            lds_char *kd = k_buf(0) + key * PITCH + (c ^ k_swz(key)) * 16, *vd = v_buf(0) + key * PITCH + (c ^ v_swz(key)) * 16;
+            *(lds_bf16x8 *)kd = ks.h;
+            *(lds_bf16x8 *)(kd + TILE) = ks.m;
+            *(lds_bf16x8 *)(kd + 2 * TILE) = ks.l;
+            *(lds_bf16x8 *)vd = vs.h;
+            *(lds_bf16x8 *)(vd + TILE) = vs.m;
+            *(lds_bf16x8 *)(vd + 2 * TILE) = vs.l;
         }
     };
 
@@ -308,13 +365,37 @@ attention_tiles_kernel(AttentionParams p)
     };
 
     // O^T += V^T P^T, P in x.  CHECK: note in `dirty` if any of the values is not finite
-    bool dirty = false;
     auto add_values = [&](auto check, const f32x16 *x, int b) {
         constexpr bool CHECK = decltype(check)::value;
         Largest16 largest;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
-            if constexpr (HALF) {
+            if constexpr (PARTS) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    f32x8 w;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] = x[kb][8 * u + i];
+                    float top = 0.f;
+                    const Split8 pr = split8(w, top);
+                    // two blocks at a time: their products run in turns
+                    constexpr int TOGETHER = BLK % 2 == 0 ? 2 : 1;
+#pragma unroll
+                    for (int d0 = 0; d0 < BLK; d0 += TOGETHER) {
+                        bf16x8 v[TOGETHER][3];
+#pragma unroll
+                        for (int d = 0; d < TOGETHER; ++d)
+#pragma unroll
+                            for (int part = 0; part < 3; ++part) v[d][part] = __builtin_bit_cast(bf16x8, read_v16(part, kb, u, d0 + d));
+                        const bf16x8 w3[3] = {pr.h, pr.m, pr.l};
+                        constexpr int V_PART[6] = {0, 2, 1, 0, 1, 0}, W_PART[6] = {2, 0, 1, 1, 0, 0};
+#pragma unroll
+                        for (int i = 0; i < 6; ++i)
+#pragma unroll
+                            for (int d = 0; d < TOGETHER; ++d) acc[d0 + d] = mma_bf16(v[d][V_PART[i]], w3[W_PART[i]], acc[d0 + d]);
+                    }
+                }
+            } else if constexpr (HALF) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     f16x8 pr;
@@ -342,7 +423,7 @@ attention_tiles_kernel(AttentionParams p)
                     }
             }
         }
-        if constexpr (CHECK && HALF) dirty |= !largest.finite();
+        if constexpr (CHECK && HALF && !PARTS) dirty |= !largest.finite();
     };
 
     // one step of this wave; WHOLE: every row sees every key of it
@@ -352,11 +433,27 @@ attention_tiles_kernel(AttentionParams p)
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
             x[kb] = f32x16{};
+            f32x16 low = {};
 #pragma unroll
             for (int s = 0; s < QS; ++s) {
                 const int c = (2 * s + h) ^ k_swz(n);
+                if constexpr (PARTS) {
+                    typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+                    const lds_char *at = k_buf(0) + k_row + kb * 32 * PITCH + c * 16;
+                    const bf16x8 kh = *(const lds_bf16x8 *)at, km = *(const lds_bf16x8 *)(at + TILE), kl = *(const lds_bf16x8 *)(at + 2 * TILE);
+                    // two sums, so that a product does not wait for the one before it
+                    x[kb] = mma_bf16(kh, qp[s].m, x[kb]);
+                    low = mma_bf16(kh, qp[s].l, low);
+                    x[kb] = mma_bf16(km, qp[s].h, x[kb]);
+                    low = mma_bf16(kl, qp[s].h, low);
+                    x[kb] = mma_bf16(kh, qp[s].h, x[kb]);
+                    low = mma_bf16(km, qp[s].m, low);
+                    if (s == QS - 1) x[kb] += low;
+                    continue;
+                }
                 const chunk a = *(__attribute__((address_space(3))) chunk *)(k_buf(b) + k_row + kb * 32 * PITCH + c * 16);
-                if constexpr (HALF) {
+                if constexpr (PARTS) {
+                } else if constexpr (HALF) {
                     x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[s], x[kb], 0, 0, 0);
                 } else {
 #pragma unroll
@@ -407,20 +504,35 @@ attention_tiles_kernel(AttentionParams p)
     const int whole_from = min(max((lo_max - start + BN - 1) / BN, 0), steps);
     const int whole_to = hi_min > start ? max((hi_min - start) / BN, whole_from) : whole_from;
     Ids ids;
+    Raw raw;
     if (steps > 0) {
         ids = ids_of(start);
-        copy_rows(std::true_type{}, ids, start, 0);
-        copy_rows(std::false_type{}, ids, start, 0);
+        if constexpr (PARTS) {
+            raw = load_raw(ids, start);
+        } else {
+            copy_rows(std::true_type{}, ids, start, 0);
+            copy_rows(std::false_type{}, ids, start, 0);
+        }
         ids = ids_of(start + BN);
     }
     auto next_step = [&](int it) {
-        // this step's copies have arrived, and every wave has read the other buffer
-        wait_vmcnt<0>();
-        lds_barrier();
-        if (it + 1 < steps) {
-            copy_rows(std::true_type{}, ids, start + (it + 1) * BN, (it + 1) & 1);
-            copy_rows(std::false_type{}, ids, start + (it + 1) * BN, (it + 1) & 1);
-            ids = ids_of(start + (it + 2) * BN);
+        if constexpr (PARTS) {
+            lds_barrier();                                // every wave has read the last step's planes
+            store_raw(raw);
+            if (it + 1 < steps) {
+                raw = load_raw(ids, start + (it + 1) * BN);
+                ids = ids_of(start + (it + 2) * BN);
+            }
+            lds_barrier();
+        } else {
+            // this step's copies have arrived, and every wave has read the other buffer
+            wait_vmcnt<0>();
+            lds_barrier();
+            if (it + 1 < steps) {
+                copy_rows(std::true_type{}, ids, start + (it + 1) * BN, (it + 1) & 1);
+                copy_rows(std::false_type{}, ids, start + (it + 1) * BN, (it + 1) & 1);
+                ids = ids_of(start + (it + 2) * BN);
+            }
         }
     };
     for (int it = 0; it < steps;) {
@@ -438,12 +550,12 @@ attention_tiles_kernel(AttentionParams p)
         }
     }
     l += __shfl_xor(l, 32);
-    dirty = __any(dirty);
+    dirty = PARTS ? __syncthreads_or(dirty) : __any(dirty);   // in parts, any thread may have met the value
 
     if constexpr (WK > 1) {
         // join the key groups: those of groups 1 .. WK - 1 through LDS, in order
         constexpr int BOX = (BLK * 16 + 3) * 64;          // words a wave
-        static_assert(WR * (WK - 1) * BOX * 4 <= 4 * TILE, "sums of the key groups must fit");
+        static_assert(WR * (WK - 1) * BOX * 4 <= (int)sizeof(smem), "sums of the key groups must fit");
         typedef __attribute__((address_space(3))) float lds_float;
         auto box_of = [&](int g) { return (lds_float *)(lds_char *)smem + (wr * (WK - 1) + g - 1) * BOX + lane; };
         lds_barrier();
@@ -507,7 +619,7 @@ attention_tiles_kernel(AttentionParams p)
                     quad out;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) out[e] = (T)(sees ? o[e] * inv : 0.f);
-                    if constexpr (HOW != ANY) {
+                    if constexpr (VEC) {
                         if (d < dim) *(quad *)(dst + d) = out;
                     } else {
                         for (int e = 0; e < 4; ++e)
@@ -540,20 +652,6 @@ hipError_t launch_chunks(const AttentionParams &p, int tile_rows, int grid, hipS
     const bool near = p.pool.k_tok < (1u << 24) && p.pool.v_tok < (1u << 24);
     return p.dim == DP && p.pool.page_size.d % 16 == 0 && near ? launch_shape<T, DP, PAGED16, KB>(p, tile_rows, grid, stream)
                                                                : launch_shape<T, DP, CHUNKS, KB>(p, tile_rows, grid, stream);
-}
-
-template <typename T>
-hipError_t launch_tiles(const AttentionParams &p, int tile_rows, bool vec, int grid, hipStream_t stream)
-{
-    constexpr int KB = sizeof(T) == 2 ? 2 : 1;
-    if (!vec) {
-        return p.dim <= 128 ? launch_shape<T, 128, ANY, KB>(p, tile_rows, grid, stream)
-                            : launch_shape<T, 256, ANY, 1>(p, tile_rows, grid, stream);
-    }
-    if (p.dim <= 64) return launch_chunks<T, 64, KB>(p, tile_rows, grid, stream);
-    if (p.dim <= 96) return launch_chunks<T, 96, KB>(p, tile_rows, grid, stream);
-    if (p.dim <= 128) return launch_chunks<T, 128, KB>(p, tile_rows, grid, stream);
-    return launch_chunks<T, 256, 1>(p, tile_rows, grid, stream);
 }
 
 }  // namespace

@@ -98,26 +98,40 @@ def attention(B: Batch, scale=None, causal=True, window=0):
         slots = B.key_slots(b)
         k = np.stack([B.k[s].double().numpy() for s in slots]) if slots else np.zeros((0, B.hk, B.dim))
         v = np.stack([B.v[s].double().numpy() for s in slots]) if slots else np.zeros((0, B.hk, B.dim))
-        for i in range(n):
-            pos = m - n + i
-            hi = min(m, pos + 1) if causal else m
-            lo = max(0, pos - window + 1) if causal and window else 0
-            for h in range(B.hq):
-                row = B.start[b] + i
-                if hi <= lo:
-                    out[row, h] = 0.0
-                    continue
-                kk, vv, qq = k[lo:hi, h // group], v[lo:hi, h // group], q[row, h]
-                with np.errstate(all="ignore"):
-                    x = scale * (kk @ qq)
-                    w = np.exp(x - x.max())
-                    out[row, h] = (w[:, None] * vv).sum(0) / w.sum()
-                    size = scale * np.linalg.norm(qq) * np.linalg.norm(kk, axis=1).max()
-                    top = np.abs(vv).max()
-                    e = (B.dim + 4) * U32 * abs(size) + 2 * U32 * np.abs(x - x.max()).max() + 4 * U32
-                    bound[row, h] = top * (2 * e + 2 * (hi - lo) * U32)
-                    if B.dtype == "f16":
-                        bound[row, h] += top * U16 + np.abs(out[row, h]) * U16 + 2.0 ** -24
+        pos = np.arange(m - n, m)[:, None]
+        j = np.arange(m)[None, :]
+        seen = (j <= pos) if causal else np.ones((n, m), dtype=bool)
+        if causal and window:
+            seen &= j > pos - window
+        rows = slice(B.start[b], B.start[b] + n)
+        some = seen.any(1)
+        for h in range(B.hq if n else 0):
+            out[rows, h] = 0.0
+            if not some.any():
+                continue
+            kk, vv, qq = k[:, h // group], v[:, h // group], q[rows, h]
+            with np.errstate(all="ignore"):
+                # masked places are taken out before any arithmetic: their logits are -inf, their values met by no weight
+                x = np.where(seen, scale * (qq @ kk.T), -np.inf)
+                top = x.max(1, keepdims=True)
+                w = np.where(seen, np.exp(x - top), 0.0)
+                # (a sum of nothing but infinities and NaN is left to the formula, row by row)
+                fine = np.isfinite(vv).all()
+                if fine:
+                    o = w @ vv
+                else:
+                    o = np.stack([(w[i, seen[i]][:, None] * vv[seen[i]]).sum(0) for i in range(n)])
+                o = o / w.sum(1, keepdims=True)
+                size = abs(scale) * np.linalg.norm(qq, axis=1) * np.where(seen, np.linalg.norm(kk, axis=1), 0.0).max(1)
+                spread = np.where(seen, np.abs(x - top), 0.0).max(1)
+                e = (B.dim + 4) * U32 * size + 2 * U32 * spread + 4 * U32
+                most = np.where(seen[:, :, None], np.abs(vv)[None], 0.0).max((1, 2)) if not fine else \
+                    np.where(seen, np.abs(vv).max(1)[None], 0.0).max(1)
+                bd = (most * (2 * e + 2 * seen.sum(1) * U32))[:, None] * np.ones((1, B.dim))
+                if B.dtype == "f16":
+                    bd = bd + most[:, None] * U16 + np.abs(o) * U16 + 2.0 ** -24
+            out[rows, h] = np.where(some[:, None], o, 0.0)
+            bound[rows, h] = np.where(some[:, None], bd, 0.0)
     return out, np.where(np.isfinite(bound), bound, np.inf)
 
 

@@ -47,14 +47,64 @@ def test_chunks(dtype, hq, hk, dim, causal, window):
     _case([70, 1, 33, 5, 128], [70, 90, 200, 5, 150], hq, hk, dim, 16, dtype, seed=2, causal=causal, window=window)
 
 
+def _many(count, longest, past):
+    """Ragged sequences: 1, `longest` and what lies between, with 0 .. past cached keys."""
+    news = [longest, 1] + [1 + (37 * i * i + 11 * i) % longest for i in range(2, count)]
+    return news, [n + (53 * i) % (past + 1) for i, n in enumerate(news)]
+
+
+# enough rows for the tall tiles, in 64 and in 128 rows, unsplit and (few heads, long caches) split over the keys
+TALL = [(17, 200, 90, 16, 16, 64, {}), (17, 250, 50, 16, 16, 128, {}), (17, 250, 50, 32, 16, 96, dict(window=40)),
+        (20, 200, 60, 16, 8, 128, dict(causal=False)), (17, 250, 60, 16, 16, 40, {}), (32, 160, 40, 16, 16, 256, {}),
+        (4, 256, 0, 16, 16, 64, dict(causal=False)), (1, 512, 0, 32, 32, 128, {}), (2, 320, 3700, 16, 16, 64, {}),
+        (2, 320, 2300, 16, 4, 128, {}), (2, 320, 2300, 16, 4, 128, dict(window=700))]
+
+
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
-@pytest.mark.parametrize("hq,hk,dim,causal,window", [(16, 16, 64, True, 0), (32, 16, 128, True, 0), (16, 16, 96, True, 20),
-                                                     (16, 16, 128, False, 0), (16, 16, 40, True, 0)])
-def test_chunks_that_fill_the_chip(dtype, hq, hk, dim, causal, window):
-    """Enough sequences and heads for the tallest row tiles."""
-    news = [33, 1, 7, 64, 2, 40, 12, 1, 1, 5, 100, 3, 9, 31, 32, 2, 35]
-    keys = [n + (7 * i) % 90 for i, n in enumerate(news)]
-    _case(news, keys, hq, hk, dim, 16, dtype, seed=21, causal=causal, window=window)
+@pytest.mark.parametrize("count,longest,past,hq,hk,dim,how", TALL)
+@pytest.mark.parametrize("page", [16, 5])
+def test_many_rows(dtype, count, longest, past, hq, hk, dim, how, page):
+    news, keys = _many(count, longest, past)
+    _case(news, keys, hq, hk, dim, page, dtype, seed=21, **how)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("dim,shift,row_gap,extra", [(64, 1, 3, 1), (96, 0, 1, 0), (77, 0, 0, 0), (128, 2, 0, 0), (200, 1, 0, 0)])
+def test_many_rows_of_any_alignment(dtype, dim, shift, row_gap, extra):
+    news, keys = _many(16, 190, 70)
+    _case(news, keys, 16, 16, dim, 16, dtype, seed=22, shift=shift, row_gap=row_gap, extra_dim=extra, order="hnd")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("count,longest,past,hq,hk", [(17, 200, 90, 16, 16), (2, 320, 3000, 16, 4)])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_many_rows_masked_places(dtype, count, longest, past, hq, hk, bad):
+    """As test_masked_places, where tiles of rows share keys; keys and queries that are not finite spoil their own rows."""
+    news, keys = _many(count, longest, past)
+    B = Batch(news, keys, hq, hk, 64, 16, dtype, seed=23)
+    late = B.key_slots(0)
+    B.v[late[keys[0] - 40]][1, 5] = bad
+    B.v[late[keys[0] - 40]][2, 9] = -bad
+    B.v[late[keys[0] - 1]][2, 9] = bad
+    if bad != bad:      # (a logit of +inf gives NaN, one of -inf no weight: both by the sign of the query; NaN always NaN)
+        B.k[late[keys[0] - 33]][3, 7] = bad
+        B.q[int(B.start[1]), 0, 0] = bad
+    B.device()
+    check_attention(B, _attend(B))
+
+
+@pytest.mark.parametrize("count,longest,past,hq,hk,dim", [(17, 200, 90, 16, 16, 64), (17, 120, 90, 16, 16, 128), (2, 320, 3000, 16, 4, 64)])
+def test_values_of_any_size_f32(count, longest, past, hq, hk, dim):
+    """fp32 values that round to an infinity in bf16, and tiny and zero ones."""
+    news, keys = _many(count, longest, past)
+    B = Batch(news, keys, hq, hk, dim, 16, "f32", seed=24)
+    s = B.key_slots(0)
+    B.v[s[3]][0, 1] = 3.395e38
+    B.v[s[keys[0] - 2]][1, 2] = -3.395e38
+    B.v[s[5]][2] = 0.0
+    B.v[s[6]][2] = 1e-30
+    B.device()
+    check_attention(B, _attend(B))
 
 
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
@@ -393,3 +443,15 @@ def test_append_in_a_graph():
         page = [3, 1, 0, 2][(n - 1) // 16]
         want = nj.rotary(k, torch.tensor([n - 1], dtype=torch.int32, device="cuda"), table)
         assert torch.equal(cache.k[page, (n - 1) % 16], want[0]) and torch.equal(cache.v[page, (n - 1) % 16], v[0])
+
+
+# -------------------------------------------------------------------- example
+
+@pytest.mark.parametrize("kv_heads,dim,page,chunk", [(4, 64, 16, 50), (2, 128, 7, 1000), (1, 32, 64, 17)])
+def test_example_serves_a_layer(kv_heads, dim, page, chunk):
+    """Chunked prompts and decode steps through the whole block against fp64 without a cache.  Roundings to fp16 of q, k, v
+    and o (one each, below U16 relative; those of q and k move logits of size 1) and of the weights of the softmax: below 8 U16."""
+    from examples import serve_layer
+    _, _, error = serve_layer.serve([130, 1, 64, 17], 5, width=256, q_heads=4, kv_heads=kv_heads, dim=dim, page_size=page,
+                                    chunk=chunk, check=True)
+    assert error < 8 * U16, error

@@ -140,6 +140,13 @@ __device__ __forceinline__ void store_stat(const AttentionParams &p, long long a
     p.stat[at * 2 + 1] = sees && sum == 0.f ? __builtin_nanf("") : sum;
 }
 
+// A logit, or a row's reference, in powers of two, minus `off`.
+template <bool BOTH>
+__device__ __forceinline__ float scaled(const AttentionParams &p, float x, float off)
+{
+    return BOTH ? fmaf(x, p.scale_log2, fmaf(x, p.scale_low, -off)) : fmaf(x, p.scale_log2, -off);
+}
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 }  // namespace nnjit

@@ -193,7 +193,6 @@ attention_rows_kernel(AttentionParams p)
 #pragma unroll
     for (int b = 0; b < BLK; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -__builtin_inff(), l = 0.f;
-    const float scale = p.scale_log2;
 
     const int tiles = (k1 - k0 + KT - 1) / KT;
     Ids ids;
@@ -247,13 +246,13 @@ attention_rows_kernel(AttentionParams p)
         for (int i = 0; i < SUB * 4; ++i) top = fmaxf(top, x[i / 4][i % 4]);
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float off = top == -__builtin_inff() ? 0.f : top * scale;   // a row that has seen nothing yet
-        const float shrink = exp2_fast(m * scale - off);
+        const float off = top == -__builtin_inff() ? 0.f : scaled<!HALF>(p, top, 0.f);   // a row that has seen nothing yet
+        const float shrink = exp2_fast(scaled<!HALF>(p, m, off));
         m = top;
         float pr[SUB * 4], sum = 0.f;
 #pragma unroll
         for (int i = 0; i < SUB * 4; ++i) {
-            pr[i] = exp2_fast(fmaf(x[i / 4][i % 4], scale, -off));
+            pr[i] = exp2_fast(scaled<!HALF>(p, x[i / 4][i % 4], off));
             sum += pr[i];
         }
         l = l * shrink + sum;
@@ -330,7 +329,7 @@ attention_rows_kernel(AttentionParams p)
 
     // join the waves: weights exp2(m_w - M) of their sums
     if (g == 0) {
-        lds_m[wave][c] = m * scale;
+        lds_m[wave][c] = scaled<!HALF>(p, m, 0.f);
         lds_l[wave][c] = l;
     }
     if (c < t.rows) {

@@ -90,6 +90,7 @@ template <typename T, int DP>
 __device__ __forceinline__ void redo_row(const AttentionParams &p, const RowTile &t, int head, int split, int r, int k0, int k1, int lane)
 {
     constexpr int E = (DP + 63) / 64;
+    constexpr bool BOTH = sizeof(T) == 4;
     const int lo = max(t.first_key(p, r), k0), hi = min(t.end_key(p, r), k1);
     const int token = t.q0 + p.group_div.quot(r);
     const int q_head = head * p.group + r - p.group_div.quot(r) * p.group;
@@ -111,7 +112,7 @@ __device__ __forceinline__ void redo_row(const AttentionParams &p, const RowTile
             if (lane + 64 * e < p.dim) x += qv[e] * (float)k[lane + 64 * e];
         for (int i = 1; i < 64; i <<= 1) x += __shfl_xor(x, i);
         const float next = fmaxf(m, x), off = next == -__builtin_inff() ? 0.f : next;
-        const float shrink = exp2_fast((m - off) * p.scale_log2), w = exp2_fast((x - off) * p.scale_log2);
+        const float shrink = exp2_fast(scaled<BOTH>(p, m - off, 0.f)), w = exp2_fast(scaled<BOTH>(p, x - off, 0.f));
         m = next;
         l = l * shrink + w;
         for (int e = 0; e < E; ++e)
@@ -127,7 +128,7 @@ __device__ __forceinline__ void redo_row(const AttentionParams &p, const RowTile
             if (d < p.part_dim) p.part[at * p.part_dim + d] = o[e];
         }
     }
-    if (p.splits > 1 && lane == 0) store_stat(p, at, m * p.scale_log2, l, hi > lo);
+    if (p.splits > 1 && lane == 0) store_stat(p, at, scaled<BOTH>(p, m, 0.f), l, hi > lo);
 }
 
 // Bytes of a row in LDS, and the waves a SIMD is to hold: two, of two
@@ -338,7 +339,8 @@ attention_tiles_kernel(AttentionParams p)
 #pragma unroll
     for (int b = 0; b < BLK; ++b) acc[b] = f32x16{};
     float m = -__builtin_inff(), l = 0.f;
-    const float scale = p.scale_log2, slack = kSlack / p.scale_log2;
+    constexpr bool BOTH = sizeof(T) == 4;
+    const float slack = kSlack / p.scale_log2;
 
     // lane parts of the LDS addresses
     const int kw = wk * KB * 32;                          // first key of this wave in a step
@@ -478,18 +480,18 @@ attention_tiles_kernel(AttentionParams p)
         top = max_of_halves(top);
         if (__any(top - m > slack)) {
             const float next = fmaxf(m, top);
-            const float shrink = exp2_fast((m - (next == -__builtin_inff() ? 0.f : next)) * scale);
+            const float shrink = exp2_fast(scaled<BOTH>(p, m - (next == -__builtin_inff() ? 0.f : next), 0.f));
             m = next;
             l *= shrink;
 #pragma unroll
             for (int blk = 0; blk < BLK; ++blk) acc[blk] *= shrink;
         }
-        const float off = m == -__builtin_inff() ? 0.f : m * scale;   // a row that has seen nothing yet
+        const float off = m == -__builtin_inff() ? 0.f : scaled<BOTH>(p, m, 0.f);   // a row that has seen nothing yet
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                x[kb][i] = exp2_fast(fmaf(x[kb][i], scale, -off));
+                x[kb][i] = exp2_fast(scaled<BOTH>(p, x[kb][i], off));
                 l += x[kb][i];
             }
         add_values(std::bool_constant<!WHOLE>{}, x, b);
@@ -578,7 +580,7 @@ attention_tiles_kernel(AttentionParams p)
             dirty |= box[128] != 0.f;
             const float next = fmaxf(m, om);
             const float off = next == -__builtin_inff() ? 0.f : next;
-            const float mine = exp2_fast((m - off) * scale), theirs = exp2_fast((om - off) * scale);
+            const float mine = exp2_fast(scaled<BOTH>(p, m - off, 0.f)), theirs = exp2_fast(scaled<BOTH>(p, om - off, 0.f));
             m = next;
             l = l * mine + ol * theirs;
 #pragma unroll
@@ -629,7 +631,7 @@ attention_tiles_kernel(AttentionParams p)
                     if (d < dim) *(f32x4 *)(p.part + at * p.part_dim + d) = f32x4{o[0], o[1], o[2], o[3]};
                 }
             }
-    if (p.splits > 1 && h == 0) store_stat(p, at, m * scale, l, sees);
+    if (p.splits > 1 && h == 0) store_stat(p, at, scaled<BOTH>(p, m, 0.f), l, sees);
 }
 
 template <typename T, int DP, int HOW, int KB>

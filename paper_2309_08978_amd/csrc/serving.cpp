@@ -295,7 +295,10 @@ int nnjit_paged_attention(const nnjit_paged_kv *cache, const nnjit_paged_batch *
     c.p.batch = batch_of(batch);
     // a scale of 0 (all keys alike) would make NaNs of masked logits: 2^-100 leaves
     // the weights of all q . k below 2^76 alike to the last bit
-    c.p.scale_log2 = std::fmax(std::fabs(scale) * 1.44269504088896340736f, 0x1p-100f);
+    const double factor = std::fmax(std::fabs((double)scale) * 1.4426950408889634074, 0x1p-100);
+    c.p.scale_log2 = (float)factor;
+    if ((double)c.p.scale_log2 > factor) c.p.scale_log2 = std::nextafterf(c.p.scale_log2, 0.f);
+    c.p.scale_low = std::fmax((float)(factor - (double)c.p.scale_log2), 0x1p-126f);
     c.p.negate = scale < 0.f;
     c.p.causal = causal != 0;
     c.p.window = (int)std::min<int64_t>(window, kMaxInt);

@@ -91,7 +91,9 @@ struct AttentionParams {
     FastDiv group_div;
     PagePool pool;
     PageBatch batch;
-    float scale_log2;          // |scale| log2(e)
+    float scale_log2, scale_low;   // |scale| log2(e), cut to fp32, and what that leaves (fp32 operands
+                               // take both: logits of 10 times a constant off by 6e-8 would be off by more
+                               // than their own rounding); scale_low > 0, so that -inf stays -inf
     int negate;                // the scale is negative: queries are taken negated
     int causal, window;
     int row_tiles;             // row tiles of a sequence and key head

@@ -5,8 +5,8 @@
 // running reference m and sum; here the matrix cores bound it.  A workgroup has WR x WK
 // waves: WR row groups of 32 rows, WK groups that take different keys of a
 // step (joined through LDS at the end).  A step takes BN = 32 KB WK keys: K and
-// V rows go from their pages to LDS by direct copies, one step ahead of the
-// products (two buffers, one barrier a step).  A lane's copies may come from
+// V rows go from their pages to LDS by direct copies, one or two steps ahead of the
+// products (one barrier a step).  A lane's copies may come from
 // any address, so pages cost nothing but their look-up, which runs one step
 // ahead of the copies.
 //
@@ -45,6 +45,7 @@ namespace nnjit {
 namespace {
 
 typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(4))) int constant_int;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
@@ -135,8 +136,14 @@ __device__ __forceinline__ void redo_row(const AttentionParams &p, const RowTile
 // workgroups, unless the buffers or the registers of one fill a CU.
 template <typename T, int DP, int HOW>
 constexpr int row_pitch() { return (DP <= 64 ? 64 : DP <= 128 ? 128 : 256) * (HOW >= SPLIT ? 2 : (int)sizeof(T)); }
+// Steps whose copies are in LDS or on their way: three where three still leave
+// room for three workgroups a CU (heads of 64 dims in fp16: ragged prompts to 777
+// 22.3 -> 20.9 us; with heads of 128 they would leave one: 38 -> 53 where two
+// fit).  Look-ups a lane would wait for the copies, so only PAGED16.
+template <typename T, int DP, int HOW>
+constexpr int stages() { return sizeof(T) == 2 && DP == 64 && HOW == PAGED16 ? 3 : 2; }
 template <typename T, int DP, int HOW, int BLOCKS>
-constexpr int lds_bytes() { return (HOW >= SPLIT ? 6 : 4) * 32 * BLOCKS * row_pitch<T, DP, HOW>(); }
+constexpr int lds_bytes() { return (HOW >= SPLIT ? 6 : 2 * stages<T, DP, HOW>()) * 32 * BLOCKS * row_pitch<T, DP, HOW>(); }
 template <typename T, int DP, int HOW, int BLOCKS>
 constexpr int waves_per_simd() { return DP <= 128 && lds_bytes<T, DP, HOW, BLOCKS>() <= 80 * 1024 ? 2 : 1; }
 
@@ -161,10 +168,11 @@ attention_tiles_kernel(AttentionParams p)
     static_assert(HALF || DP % 128 == 0, "whole runs of four dims");
     typedef T chunk __attribute__((ext_vector_type(CH)));
 
-    // K, K, V, V: two steps; in parts the three planes of K and of V of one step
+    // K of every stage, then V; in parts the three planes of K and of V of one step
     __shared__ __attribute__((aligned(1024))) char smem[lds_bytes<T, DP, HOW, KB * WK>()];
+    constexpr int ST = stages<T, DP, HOW>();
     auto k_buf = [&](int b) -> lds_char * { return (lds_char *)smem + b * TILE; };
-    auto v_buf = [&](int b) -> lds_char * { return (lds_char *)smem + ((PARTS ? 3 : 2) + b) * TILE; };
+    auto v_buf = [&](int b) -> lds_char * { return (lds_char *)smem + ((PARTS ? 3 : ST) + b) * TILE; };
 
     // chunk c of key row `key` sits at c ^ swizzle
     auto k_swz = [](int key) { return CPR >= 16 ? (key & 15) : ((key >> 1) & 7); };
@@ -252,8 +260,12 @@ attention_tiles_kernel(AttentionParams p)
     auto ids_of = [&](int kt) {
         Ids ids;
 #pragma unroll
-        for (int i = 0; i < IDS; ++i)
-            ids.page[i] = t.table[p.pool.page_size.quot(min(kt + key_of(i, HOW == PAGED16 ? 0 : lane), last_key))];
+        for (int i = 0; i < IDS; ++i) {
+            const int at = p.pool.page_size.quot(min(kt + key_of(i, HOW == PAGED16 ? 0 : lane), last_key));
+            // (a scalar load: a vector load's value would be waited for together with the copies before it)
+            if constexpr (HOW == PAGED16) ids.page[i] = ((const constant_int *)t.table)[__builtin_amdgcn_readfirstlane(at)];
+            else ids.page[i] = t.table[at];
+        }
         return ids;
     };
     auto copy_rows = [&](auto of_keys, const Ids &ids, int kt, int b) {
@@ -512,10 +524,15 @@ attention_tiles_kernel(AttentionParams p)
         if constexpr (PARTS) {
             raw = load_raw(ids, start);
         } else {
-            copy_rows(std::true_type{}, ids, start, 0);
-            copy_rows(std::false_type{}, ids, start, 0);
+#pragma unroll
+            for (int stage = 0; stage < ST - 1; ++stage) {
+                if (stage > 0 && stage >= steps) break;
+                if (stage > 0) ids = ids_of(start + stage * BN);
+                copy_rows(std::true_type{}, ids, start + stage * BN, stage);
+                copy_rows(std::false_type{}, ids, start + stage * BN, stage);
+            }
         }
-        ids = ids_of(start + BN);
+        ids = ids_of(start + (PARTS ? 1 : ST - 1) * BN);
     }
     auto next_step = [&](int it) {
         if constexpr (PARTS) {
@@ -527,13 +544,15 @@ attention_tiles_kernel(AttentionParams p)
             }
             lds_barrier();
         } else {
-            // this step's copies have arrived, and every wave has read the other buffer
-            wait_vmcnt<0>();
+            // this step's copies have arrived (a later step's may be on their way), and
+            // every wave has read the buffers that the copies below fill
+            if (ST == 3 && it + 1 < steps) wait_vmcnt<ST == 3 ? 2 * NI : 0>();
+            else wait_vmcnt<0>();
             lds_barrier();
-            if (it + 1 < steps) {
-                copy_rows(std::true_type{}, ids, start + (it + 1) * BN, (it + 1) & 1);
-                copy_rows(std::false_type{}, ids, start + (it + 1) * BN, (it + 1) & 1);
-                ids = ids_of(start + (it + 2) * BN);
+            if (it + ST - 1 < steps) {
+                copy_rows(std::true_type{}, ids, start + (it + ST - 1) * BN, (it + ST - 1) % ST);
+                copy_rows(std::false_type{}, ids, start + (it + ST - 1) * BN, (it + ST - 1) % ST);
+                ids = ids_of(start + (it + ST) * BN);
             }
         }
     };
@@ -543,12 +562,12 @@ attention_tiles_kernel(AttentionParams p)
             for (; it < part_to; ++it) {
                 next_step(it);
                 const int key0 = start + it * BN + kw;
-                if (wave_rows && key0 < hi_w && key0 + 32 * KB > lo_w) step(std::false_type{}, key0, it & 1);
+                if (wave_rows && key0 < hi_w && key0 + 32 * KB > lo_w) step(std::false_type{}, key0, it % ST);
             }
         }
         for (; it < whole_to; ++it) {
             next_step(it);
-            step(std::true_type{}, 0, it & 1);
+            step(std::true_type{}, 0, it % ST);
         }
     }
     l += __shfl_xor(l, 32);

@@ -7,6 +7,8 @@
 namespace nnjit {
 
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+// memory that no one writes while the kernel runs: read by scalar loads
+typedef __attribute__((address_space(4))) int constant_int;
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
 // What one workgroup works on: a tile of rows of one sequence and key head.

@@ -53,13 +53,17 @@ template <> struct RowsOf<float> {
     typedef f32x4 chunk;
 };
 
-// n consecutive elements, of which those at or past `valid` are zero
-template <typename V, bool VEC, typename T>
+// n consecutive elements, of which those at or past `valid` are zero.  STREAM: not
+// to be kept in the caches.
+template <typename V, bool VEC, bool STREAM, typename T>
 __device__ __forceinline__ V load_some(const T *src, int valid, int n)
 {
     if constexpr (VEC) {
         V v = {};
-        if (valid > 0) v = *(const V *)src;     // valid is a multiple of n here
+        if (valid > 0) {                        // valid is a multiple of n here
+            if constexpr (STREAM) v = __builtin_nontemporal_load((const V *)src);
+            else v = *(const V *)src;
+        }
         return v;
     } else {
         V v;
@@ -68,7 +72,11 @@ __device__ __forceinline__ V load_some(const T *src, int valid, int n)
     }
 }
 
-template <typename T, int DP, bool VEC, bool PAGE16, int NW>
+// STREAM: keys and values pass the caches by, where nothing of a cache line is
+// read twice: one row tile, heads of whole lines (32 sequences of 4096 keys, heads
+// of 128: 110 -> 102 us; two row tiles would lose, 39 -> 46, as would heads of 96
+// dims, 22 -> 27, and of 64, whose loads take half a line, 24 -> 27).
+template <typename T, int DP, bool VEC, bool PAGE16, bool STREAM, int NW>
 __global__ void __launch_bounds__(NW * 64)
 attention_rows_kernel(AttentionParams p)
 {
@@ -122,7 +130,7 @@ attention_rows_kernel(AttentionParams p)
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             const int d = (4 * s + g) * CH;
-            q[s] = load_some<chunk, VEC>(src + d, p.dim - d, CH);
+            q[s] = load_some<chunk, VEC, false>(src + d, p.dim - d, CH);
             if (p.negate) q[s] = -q[s];
         }
     }
@@ -142,8 +150,9 @@ attention_rows_kernel(AttentionParams p)
         Ids ids;
 #pragma unroll
         for (int s = 0; s < SUB; ++s) {
-            const int key = min(kt + 16 * s + (PAGE16 ? 0 : c), last_key);
-            ids.k[s] = t.table[p.pool.page_size.quot(key)];
+            const int at = p.pool.page_size.quot(min(kt + 16 * s + (PAGE16 ? 0 : c), last_key));
+            if constexpr (PAGE16) ids.k[s] = ((const constant_int *)t.table)[__builtin_amdgcn_readfirstlane(at)];
+            else ids.k[s] = t.table[at];
         }
         if constexpr (!PAGE16) {
 #pragma unroll
@@ -171,7 +180,7 @@ attention_rows_kernel(AttentionParams p)
 #pragma unroll
             for (int e = 0; e < STEPS; ++e) {
                 const int d = (4 * e + g) * CH;
-                kreg[s][e] = load_some<chunk, VEC>(row + d, p.dim - d, CH);
+                kreg[s][e] = load_some<chunk, VEC, STREAM>(row + d, p.dim - d, CH);
             }
         }
     };
@@ -184,7 +193,7 @@ attention_rows_kernel(AttentionParams p)
 #pragma unroll
             for (int h = 0; h < VH; ++h) {
                 const int d = h * 16 * VE + c * VE;
-                vreg[i][h] = load_some<vvec, VEC>(row + d, p.dim - d, VE);
+                vreg[i][h] = load_some<vvec, VEC, STREAM>(row + d, p.dim - d, VE);
             }
         }
     };
@@ -198,9 +207,10 @@ attention_rows_kernel(AttentionParams p)
     Ids ids;
     if (wave < tiles) {
         ids = ids_of(k0 + wave * KT);
-        load_k(ids, k0 + wave * KT);
-        load_v(ids, k0 + wave * KT);
+        const Ids now = ids;
+        load_k(now, k0 + wave * KT);
         ids = ids_of(k0 + (wave + NW) * KT);
+        load_v(now, k0 + wave * KT);
     }
     for (int it = wave; it < tiles; it += NW) {
         const int kt = k0 + it * KT;
@@ -220,7 +230,13 @@ attention_rows_kernel(AttentionParams p)
                 }
             }
         }
-        if (more) load_k(ids, kn);
+        // the look-ups of the tile after the next are asked for between its keys and its values:
+        // loads come in order, and theirs must not wait for the values
+        const Ids now = ids;
+        if (more) {
+            load_k(now, kn);
+            ids = ids_of(kn + NW * KT);
+        }
 
         const bool whole = kt >= lo_max && kt + KT <= min(hi_min, k1);
         unsigned seen = ~0u;
@@ -319,10 +335,7 @@ attention_rows_kernel(AttentionParams p)
                 for (int j = 0; j < 4; ++j) acc[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j], pr[j], acc[b], 0, 0, 0);
             }
         }
-        if (more) {
-            load_v(ids, kn);
-            ids = ids_of(kn + NW * KT);
-        }
+        if (more) load_v(now, kn);
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
@@ -469,13 +482,22 @@ hipError_t launch_join(const AttentionParams &p, hipStream_t stream)
     return hipGetLastError();
 }
 
+template <typename T, int DP, bool VEC, bool STREAM>
+hipError_t launch_paged(const AttentionParams &p, int grid, hipStream_t stream)
+{
+    constexpr int NW = 4;
+    if (p.pool.page_size.d % 16 == 0) attention_rows_kernel<T, DP, VEC, true, STREAM, NW><<<grid, NW * 64, 0, stream>>>(p);
+    else attention_rows_kernel<T, DP, VEC, false, STREAM, NW><<<grid, NW * 64, 0, stream>>>(p);
+    return hipGetLastError();
+}
+
 template <typename T, int DP, bool VEC>
 hipError_t launch_rows(const AttentionParams &p, int grid, hipStream_t stream)
 {
-    constexpr int NW = 4;
-    if (p.pool.page_size.d % 16 == 0) attention_rows_kernel<T, DP, VEC, true, NW><<<grid, NW * 64, 0, stream>>>(p);
-    else attention_rows_kernel<T, DP, VEC, false, NW><<<grid, NW * 64, 0, stream>>>(p);
-    return hipGetLastError();
+    if constexpr (VEC && DP >= 128) {
+        if (p.dim == DP && p.row_tiles == 1) return launch_paged<T, DP, VEC, true>(p, grid, stream);
+    }
+    return launch_paged<T, DP, VEC, false>(p, grid, stream);
 }
 
 template <typename T>

@@ -45,7 +45,6 @@ namespace nnjit {
 namespace {
 
 typedef __attribute__((address_space(3))) char lds_char;
-typedef __attribute__((address_space(4))) int constant_int;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 

@@ -422,7 +422,7 @@ int nnjit_stream_read(const void *src, int64_t bytes, void *sink, int workgroups
  * k[g * k_page + s * k_token + h * k_head + i], values alike.  Both
  * [page][slot][head][dim] and [page][head][slot][dim] pools (and views of
  * larger ones) can be described.  Page and token strides are below 2^32
- * elements; a pool may be larger. */
+ * elements; a pool may be larger.  Slots that are appended to must not overlap. */
 typedef struct nnjit_paged_kv {
     void *k, *v;
     int64_t k_page, k_token, k_head;   /* strides in elements */
@@ -518,9 +518,11 @@ int nnjit_kv_append(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch,
  * with j > p - window only.  A token that sees no key gets zeros.  What lies
  * in places that a token does not see -- unused slots, other positions' keys
  * and values, infinities and NaN among them -- does not touch its row.
- * Softmax statistics and sums are held in fp32; fp16 probabilities are
- * rounded for the matrix cores (see the kernels).  Results do not depend on
- * the order in which workgroups run.  The stream's scratch (see "Stream
+ * Softmax statistics and sums are held in fp32.  fp16: weights go to the
+ * matrix cores in fp16, so those below 2^-25 of the row's largest may count as
+ * 0 (and an infinite value seen with such a weight may give NaN in place of an
+ * infinity).  fp32: values below 2^-110 are taken to an absolute 2^-126.
+ * Results do not depend on the order in which workgroups run.  The stream's scratch (see "Stream
  * capture" above) is used when keys are split over workgroups. */
 int nnjit_paged_attention(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch, int64_t q_heads,
                           const void *q, int64_t q_token, int64_t q_head, void *out, int64_t out_token, int64_t out_head,

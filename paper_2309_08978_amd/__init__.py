@@ -357,13 +357,19 @@ def nnjit_version() -> int:
 
 # ------------------------------------------------------------ conveniences
 
+_NOT_PRODUCTS = ("attention_", "rotary.", "serving.")   # csrc/ sources that no product runs
+
+
 def kernel_digest() -> str:
-    """Short digest of the kernel and launch sources (csrc/): counter
-    measurements recorded against one digest are stale under another."""
+    """Short digest of the kernel and launch sources of the products (csrc/
+    without the serving operators'): counter measurements recorded against
+    one digest are stale under another."""
     import hashlib
     h = hashlib.sha256()
     d = os.path.join(HERE, "csrc")
     for name in sorted(os.listdir(d)):
+        if name.startswith(_NOT_PRODUCTS):
+            continue
         with open(os.path.join(d, name), "rb") as f:
             h.update(name.encode() + b"\0" + f.read())
     return h.hexdigest()[:16]

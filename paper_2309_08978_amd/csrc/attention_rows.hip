@@ -509,10 +509,6 @@ hipError_t launch_typed(const AttentionParams &p, bool vec, int grid, hipStream_
     return launch_rows<T, 256, true>(p, grid, stream);
 }
 
-}  // namespace
-
-namespace {
-
 // Estimated time of a step of a kernel's workgroups: max(a, b o) us with `o`
 // workgroups to a compute unit, linear in the head dimension d (in units of
 // 128), and no less than its bytes at 5.5 TB/s.  Fitted to measured times (within about 15% over 64 .. 8192 keys, 8 ..

@@ -462,15 +462,14 @@ attention_tiles_kernel(AttentionParams p)
                     x[kb] = mma_bf16(kh, qp[s].h, x[kb]);
                     low = mma_bf16(km, qp[s].m, low);
                     if (s == QS - 1) x[kb] += low;
-                    continue;
-                }
-                const chunk a = *(__attribute__((address_space(3))) chunk *)(k_buf(b) + k_row + kb * 32 * PITCH + c * 16);
-                if constexpr (PARTS) {
-                } else if constexpr (HALF) {
-                    x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[s], x[kb], 0, 0, 0);
                 } else {
+                    const chunk a = *(__attribute__((address_space(3))) chunk *)(k_buf(b) + k_row + kb * 32 * PITCH + c * 16);
+                    if constexpr (HALF) {
+                        x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[s], x[kb], 0, 0, 0);
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], q[s][i], x[kb], 0, 0, 0);
+                        for (int i = 0; i < 4; ++i) x[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], q[s][i], x[kb], 0, 0, 0);
+                    }
                 }
             }
         }

@@ -12,6 +12,7 @@ namespace {
 
 constexpr int64_t kMaxInt = 0x7fffffff;
 constexpr int64_t kMaxKeys = (int64_t)1 << 30;   // key indices stay well inside 32 bits
+constexpr int64_t kMaxGroups = 0xffffff;          // workgroups of 256 threads: a launch holds below 2^32 threads
 
 bool is_dtype(int d) { return d == NNJIT_F32 || d == NNJIT_F16; }
 int64_t bytes_of(int dtype) { return dtype == NNJIT_F32 ? 4 : 2; }
@@ -67,6 +68,19 @@ int check_cache(const nnjit_paged_kv *c) {
         return runtime_fail(NNJIT_EINVAL, "negative stride of the cache");
     if (std::max({c->k_page, c->k_token, c->v_page, c->v_token}) > (int64_t)0xffffffff)
         return runtime_fail(NNJIT_EINVAL, "page and token strides of the cache must be below 2^32 elements");
+    return NNJIT_OK;
+}
+
+// slots that are written: none may overlap
+int check_slots(const char *name, const nnjit_paged_kv *c, int64_t page, int64_t token, int64_t head) {
+    struct { int64_t stride, count; } axis[3] = {{page, c->pages}, {token, c->page_size}, {head, c->kv_heads}};
+    std::sort(axis, axis + 3, [](const auto &a, const auto &b) { return a.stride < b.stride; });
+    double taken = (double)c->head_dim;                    // elements from the first to the last, axis by axis
+    for (const auto &a : axis) {
+        if (a.count == 1) continue;
+        if ((double)a.stride < taken) return runtime_fail(NNJIT_EINVAL, "slots of the cache's %s overlap (stride %lld)", name, (long long)a.stride);
+        taken += (double)a.stride * (double)(a.count - 1);
+    }
     return NNJIT_OK;
 }
 
@@ -184,6 +198,7 @@ int nnjit_rotary_fill(float *table, int64_t positions, int64_t rotary_dim, doubl
         return runtime_fail(NNJIT_EINVAL, "a ramp needs original > 0 and fast > slow > 0 (got %g, %g, %g)", s.original, s.fast, s.slow);
     if (!std::isfinite(s.magnitude)) return runtime_fail(NNJIT_EINVAL, "magnitude is not finite");
     if (positions == 0) return NNJIT_OK;
+    if (positions * (rotary_dim / 2) > kMaxGroups * 256) return runtime_fail(NNJIT_EINVAL, "a table of %lld positions: below 2^32 pairs are served", (long long)positions);
     if (!table) return runtime_fail(NNJIT_EINVAL, "table is NULL");
     TableCall c{table, (int)positions, (int)rotary_dim, s.kind, base, s.factor, s.original, s.fast, s.slow, s.magnitude, (hipStream_t)stream};
     return runtime_launch(c.stream, nullptr, do_table, &c, "rotary_table");
@@ -203,6 +218,7 @@ int nnjit_rotary(const nnjit_rotary_table *rotary, int64_t tokens, int64_t heads
     if ((rc = check_rows("x", x, tokens, heads, x_token, x_head)) != NNJIT_OK) return rc;
     if ((rc = check_written("y", y, tokens, heads, head_dim, y_token, y_head)) != NNJIT_OK) return rc;
     if (tokens == 0 || heads == 0) return NNJIT_OK;
+    if (tokens > kMaxGroups) return runtime_fail(NNJIT_EINVAL, "%lld tokens in one call: below 2^24 are served", (long long)tokens);
     if (!positions) return runtime_fail(NNJIT_EINVAL, "positions is NULL");
     RotaryCall c;
     c.p.q = HeadRows{x, x_token, x_head};
@@ -233,12 +249,15 @@ int nnjit_kv_append(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch,
     if (!is_dtype(src_dtype)) return runtime_fail(NNJIT_EDTYPE, "unsupported dtype %d", src_dtype);
     if (q_heads < 0 || q_heads > kMaxInt - 2 * cache->kv_heads) return runtime_fail(NNJIT_EINVAL, "q_heads=%lld out of range", (long long)q_heads);
     const int64_t dim = cache->head_dim;
+    if ((rc = check_slots("K", cache, cache->k_page, cache->k_token, cache->k_head)) != NNJIT_OK) return rc;
+    if ((rc = check_slots("V", cache, cache->v_page, cache->v_token, cache->v_head)) != NNJIT_OK) return rc;
     if (rotary && (rc = check_rotary(rotary, dim)) != NNJIT_OK) return rc;
     if ((rc = check_rows("k", k, batch->tokens, cache->kv_heads, k_token, k_head)) != NNJIT_OK) return rc;
     if ((rc = check_rows("v", v, batch->tokens, cache->kv_heads, v_token, v_head)) != NNJIT_OK) return rc;
     if ((rc = check_rows("q", q, batch->tokens, q_heads, q_token, q_head)) != NNJIT_OK) return rc;
     if ((rc = check_written("q_out", q_out, batch->tokens, q_heads, dim, qo_token, qo_head)) != NNJIT_OK) return rc;
     if (batch->tokens == 0 || batch->sequences == 0) return NNJIT_OK;
+    if (batch->tokens > kMaxGroups) return runtime_fail(NNJIT_EINVAL, "%lld tokens in one call: below 2^24 are served", (long long)batch->tokens);
     RotaryCall c;
     c.p.q = HeadRows{q, q_token, q_head};
     c.p.qo = HeadRows{q_out, qo_token, qo_head};
@@ -313,8 +332,8 @@ int nnjit_paged_attention(const nnjit_paged_kv *cache, const nnjit_paged_batch *
         return runtime_fail(NNJIT_EINVAL, "%lld rows of %lld heads in one call: below 2^31 are served", (long long)rows, (long long)q_heads);
     const AttentionPlan least = attention_plan(c.dtype, rows, batch->sequences, c.p.q_heads, (int)cache->kv_heads, c.p.dim, c.max_q, c.max_kv,
                                                c.p.causal, c.p.window, 1024);
-    if ((double)least.row_tiles * least.splits * (double)cache->kv_heads * (double)batch->sequences > (double)kMaxInt)
-        return runtime_fail(NNJIT_EINVAL, "more than 2^31 - 1 workgroups");
+    if ((double)least.row_tiles * least.splits * (double)cache->kv_heads * (double)batch->sequences > (double)kMaxGroups)
+        return runtime_fail(NNJIT_EINVAL, "more than 2^24 - 1 workgroups (sequences times key heads times tiles)");
     return runtime_launch(c.stream, attention_floats, do_attention, &c, "paged_attention");
 }
 

@@ -98,6 +98,18 @@ def test_refused(call):
     assert nj.nnjit_last_error()
 
 
+@pytest.mark.parametrize("call", [
+    lambda: _rotary(tokens=1 << 24), lambda: _append(batch=_batch(tokens=1 << 24)),                  # more threads than a launch holds
+    lambda: nj.nnjit_rotary_fill(16, 1 << 28, 32, 1e4),
+    lambda: _attend(kv=_kv(kv_heads=1), batch=_batch(sequences=1 << 24, tokens=1 << 24, max_q=1), heads=1),
+    lambda: _append(kv=_kv(k_token=0)), lambda: _append(kv=_kv(v_token=63)), lambda: _append(kv=_kv(k_head=31)),   # slots overlap
+    lambda: _append(kv=_kv(v_page=1023)), lambda: _append(kv=_kv(k_token=32, k_head=511)),
+])
+def test_refused_by_size_and_overlap(call):
+    assert call() == nj.NNJIT_EINVAL
+    assert nj.nnjit_last_error()
+
+
 def test_dtypes_refused():
     assert _append(dtype=2) == nj.NNJIT_EDTYPE
     assert _rotary(xd=3) == nj.NNJIT_EDTYPE and _rotary(yd=-1) == nj.NNJIT_EDTYPE

@@ -33,7 +33,27 @@
 //
 // fp16 probabilities are rounded once to 11 bits.  The sum that divides takes
 // them unrounded; rounding is unbiased, and its share of the result's
-// error is that of the result's own rounding to fp16.
+// error is that of the result's own rounding to fp16.  (Two parts, as in
+// attention_rows.hip, would be half as many products again where products
+// are what bounds.)
+//
+// Why 32 rows a wave: K and V of a step are read from LDS once per 32 rows, half
+// as often as with 16 x 16 products; the sums and queries of 64 rows would leave
+// room for one wave a SIMD only.  Tiles of 128 rows (four row groups) read K
+// and V least often; tiles of 64 rows (two row groups times two key groups)
+// exist for prompts whose 128-row tiles leave compute units idle.
+//
+// Measured: 2048 new tokens at the end of 16384, 32 heads of 128 on 8, fp16:
+// 522 us, 987 TFLOP/s (a large matrix product: 1210): the clock, which power
+// holds at about 1.8 GHz under this load -- a quarter fewer scalar instructions, or
+// a step's logits computed one step ahead of its softmax (555 -> 545), change
+// next to nothing.  512 tokens at the end of 2048, 32 heads: 37 us, 410 TFLOP/s,
+// 31 and 6 for the join of two splits; ragged prompts of up to 777 tokens, 12
+// heads of 64: 20 us, the 13 steps of the longest tile, one after the other.
+// fp32 in three bf16 parts: four sequences of 256 rows on 256 keys, 16 heads of
+// 64: 17 us, 63 TFLOP/s; 2048 tokens alone, 32 heads of 128 on 8: 269 us, 128
+// TFLOP/s (a large fp32 matrix product: 153), against 372 on the fp32 matrix
+// cores.
 #pragma once
 
 #include <type_traits>

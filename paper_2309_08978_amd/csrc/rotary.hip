@@ -18,7 +18,14 @@
 // Bandwidth-bound: every element is read and written once.  A thread keeps
 // one place in the row (four pairs, or eight plain elements: two loads of
 // four elements, 16 bytes in fp32) and walks over heads of one token, so that
-// 16 lanes cover a head of 128 contiguously.
+// 16 lanes cover a head of 128 contiguously and cos and sin are read once a
+// token.  4096 tokens of 32 heads of 128, fp32 to fp16: 19 us, 5.4 TB/s (a
+// large copy: 5.2); ragged prompts of 16 + 32 heads of 64 appended in fp32:
+// 11.7 us, 5.0 TB/s; one token, or a decode step's append: 2.2 and 3.0 us on
+// the device, a launch.  Loads past the caches gain a tenth where the rows
+// come from memory, but lose as much or more where they are still in the last
+// level of cache (1000 tokens: 7.1 -> 8.4 us), as what a linear has just
+// written is.
 #include "kcommon.h"
 #include "serving.h"
 #include "nnjit.h"
@@ -210,6 +217,8 @@ hipError_t launch_rotary(const RotaryParams &in, bool append, int src_dtype, int
     const int rows = kThreads / units;
     // few tokens: their heads are spread over workgroups until about four
     // workgroups a compute unit are there; many tokens: one workgroup each
+    // (one, two, four or eight a compute unit: alike to 0.1 us from 1 to 4096 tokens;
+    // sixteen: 11.0 -> 11.9 for 2048 tokens appended)
     const int most = (heads + rows - 1) / rows;
     const int want = (1024 + p.tokens - 1) / p.tokens;
     const int blocks = want < most ? want : most;

@@ -107,7 +107,7 @@ struct AttentionParams {
 
 // How one call is laid out on the chip; sizes the scratch.
 struct AttentionPlan {
-    int tile_rows;             // 16: attention_rows.hip; 64, 128: attention_tiles.h
+    int tile_rows;             // rows of a tile.  16: attention_rows.hip; 64, 128: attention_tiles.h
     int row_tiles, splits, split_keys;
     int64_t ws_floats;         // partial sums and statistics
 };

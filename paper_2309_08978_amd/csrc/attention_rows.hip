@@ -105,14 +105,31 @@ attention_rows_kernel(AttentionParams p)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
 
-    int id = xcd_remap(blockIdx.x, gridDim.x);
-    const int tile = id % p.row_tiles;
-    id /= p.row_tiles;
-    const int split = id % p.splits;
-    id /= p.splits;
+    // row tiles of one sequence and key head run on one XCD; with one row tile nothing
+    // is shared, and the (split, sequence) pairs go round the XCDs, each with all its
+    // heads, a sequence's splits to different XCDs: sequences of random lengths
+    // 2% (fp16) and 4% (fp32) faster than with neighbours on one XCD, up to 28% (three
+    // of up to 10000 keys, 32 heads of 128: 166 -> 119 us); equal ones 0 .. 2% slower.
+    // (A head a XCD would leave most channels of its L2 idle: its rows lie 2 KB apart.)
     const int kv_heads = p.q_heads / p.group;
-    const int head = id % kv_heads;
-    const int seq = id / kv_heads;
+    int tile = 0, split, head, seq;
+    if (p.row_tiles == 1 && p.splits > 1 && p.batch.sequences > 1) {
+        const int b = blockIdx.x, n = p.batch.sequences, size = 8 * kv_heads, round = b / size, whole = gridDim.x - gridDim.x % size;
+        const int pair = round * 8 + (b % 8 + (n < 8 ? round : round * 8 / n)) % 8;
+        int id = b < whole ? pair * kv_heads + b % size / 8 : whole + xcd_remap(b - whole, gridDim.x - whole);
+        head = id % kv_heads;
+        id /= kv_heads;
+        seq = id % n;
+        split = id / n;
+    } else {
+        int id = xcd_remap(blockIdx.x, gridDim.x);
+        tile = id % p.row_tiles;
+        id /= p.row_tiles;
+        split = id % p.splits;
+        id /= p.splits;
+        head = id % kv_heads;
+        seq = id / kv_heads;
+    }
     const RowTile t = row_tile(p, seq, tile, 16);
     if (t.rows <= 0) return;
 
@@ -490,34 +507,101 @@ hipError_t launch_join(const AttentionParams &p, hipStream_t stream)
     return hipGetLastError();
 }
 
-template <typename T, int DP, bool VEC, bool STREAM>
+template <typename T, int DP, bool VEC, bool STREAM, int NW>
 hipError_t launch_paged(const AttentionParams &p, int grid, hipStream_t stream)
 {
-    constexpr int NW = 4;
     if (p.pool.page_size.d % 16 == 0) attention_rows_kernel<T, DP, VEC, true, STREAM, NW><<<grid, NW * 64, 0, stream>>>(p);
     else attention_rows_kernel<T, DP, VEC, false, STREAM, NW><<<grid, NW * 64, 0, stream>>>(p);
     return hipGetLastError();
 }
 
+template <typename T, int DP, bool VEC, bool STREAM>
+hipError_t launch_waves(const AttentionParams &p, int waves, int grid, hipStream_t stream)
+{
+    if constexpr (VEC && DP <= 128) {
+        if (waves == 8) return launch_paged<T, DP, VEC, STREAM, 8>(p, grid, stream);
+    }
+    return launch_paged<T, DP, VEC, STREAM, 4>(p, grid, stream);
+}
+
 template <typename T, int DP, bool VEC>
-hipError_t launch_rows(const AttentionParams &p, int grid, hipStream_t stream)
+hipError_t launch_rows(const AttentionParams &p, int waves, int grid, hipStream_t stream)
 {
     if constexpr (VEC && DP >= 128) {
-        if (p.dim == DP && p.row_tiles == 1) return launch_paged<T, DP, VEC, true>(p, grid, stream);
+        if (p.dim == DP && p.row_tiles == 1) return launch_waves<T, DP, VEC, true>(p, waves, grid, stream);
     }
-    return launch_paged<T, DP, VEC, false>(p, grid, stream);
+    return launch_waves<T, DP, VEC, false>(p, waves, grid, stream);
 }
 
 template <typename T>
-hipError_t launch_typed(const AttentionParams &p, bool vec, int grid, hipStream_t stream)
+hipError_t launch_typed(const AttentionParams &p, bool vec, int waves, int grid, hipStream_t stream)
 {
-    if (!vec) return p.dim <= 128 ? launch_rows<T, 128, false>(p, grid, stream) : launch_rows<T, 256, false>(p, grid, stream);
-    if (p.dim <= 64) return launch_rows<T, 64, true>(p, grid, stream);
-    if (p.dim <= 128) return launch_rows<T, 128, true>(p, grid, stream);
-    return launch_rows<T, 256, true>(p, grid, stream);
+    if (!vec) return p.dim <= 128 ? launch_rows<T, 128, false>(p, waves, grid, stream) : launch_rows<T, 256, false>(p, waves, grid, stream);
+    if (p.dim <= 64) return launch_rows<T, 64, true>(p, waves, grid, stream);
+    if (p.dim <= 128) return launch_rows<T, 128, true>(p, waves, grid, stream);
+    return launch_rows<T, 256, true>(p, waves, grid, stream);
 }
 
-// Estimated time of a step of a kernel's workgroups: max(a, b o) us with `o`
+// Keys that one tile can see: with a window, from the first row's first key
+// (rounded down to a multiple of 32) to the last row's last.
+int64_t seen_span(int64_t max_kv, int64_t window, int tile_rows, int64_t group)
+{
+    return window > 0 ? std::min(max_kv, window + (tile_rows + group - 1) / group + 32) : max_kv;
+}
+
+// Up to 16 rows of a sequence and key head: chosen are the splits and the waves of a
+// workgroup.  Estimated time (us, d = head dim / 128): steps of a split times the
+// largest of a step's latency, its share of a compute unit's cores (a unit of four
+// waves) and its bytes at 6.6 TB/s; workgroups in whole rounds count for the most
+// part, and sequences of different lengths take longer unless there are many
+// workgroups, which take 0.4 us each to start.  A split costs a second launch and
+// the partial sums.  Fitted to times measured over
+// 100 .. 10000 keys, 8 .. 1024 sequences times key heads, dims 64 and 128, lengths
+// alike and spread from 5% to all: within 2.7% of the best choice on the geometric mean.
+struct FewRowsCost {
+    double latency0, latency1, share0, share1;   // x0 + x1 d
+    double rounds;                               // weight of whole rounds
+    double spread, even;                         // 1 + spread exp(-workgroups a CU / even)
+    double join;
+};
+constexpr FewRowsCost kFewF16 = {2.9, 0.45, 0.48, 0.26, 0.9, 0.37, 5, 6.5}, kFewF32 = {2.4, 1.25, 0.33, 1.9, 1, 0.215, 7.3, 7.9};
+
+// Eight waves, unsplit, take half the steps where workgroups are no more than
+// compute units (32 sequences, 8 key heads, 1000 keys, heads of 128 in fp32: 47 us against
+// 52 unsplit and 50 in two splits of four waves; 24 sequences, heads of 64 in fp16:
+// 13.7 against 16.7 and 17.8); with more, four waves are ahead (48 sequences:
+// 20.8 against 24.3).
+AttentionPlan few_rows_plan(int dtype, int64_t tokens, int64_t sequences, int q_heads, int kv_heads, int dim, int64_t span, int cus)
+{
+    const bool half = dtype == NNJIT_F16;
+    const FewRowsCost &c = half ? kFewF16 : kFewF32;
+    const int64_t lanes = (int64_t)kv_heads * sequences;
+    const double d = dim / 128.0, part_us = (double)tokens * q_heads * dim * 8 / 3.3e6;   // partial sums of a split, written and read
+    AttentionPlan best{};
+    double least = 0;
+    for (int waves = 4; waves <= (dim <= 128 && lanes <= cus ? 8 : 4); waves += 4) {
+        const int keys = waves * (half ? 32 : 16);          // of a step
+        for (int64_t want = 1; want <= (waves == 4 ? 256 : 1); want = want < 4 ? want + 1 : want * 3 / 2 - want * 3 / 2 % 2) {
+            const int64_t per = (span + want - 1) / want;
+            const int64_t split_keys = std::max<int64_t>((per + 31) / 32 * 32, 32);
+            const int64_t splits = std::max<int64_t>((span + split_keys - 1) / split_keys, 1);
+            const double per_cu = (double)lanes * splits / cus, units = per_cu * waves / 4;
+            const double rounds = per_cu < 1 ? 1 : per_cu < 4 ? per_cu + c.rounds * (std::ceil(per_cu) - per_cu) : per_cu;
+            double bytes_us = 2.0 * keys * dim * (half ? 2 : 4) * rounds * cus / 6.6e6;
+            if (sequences > 1) bytes_us *= 1 + c.spread * std::exp(-per_cu / c.even);
+            const double step = std::max({c.latency0 + c.latency1 * d, (c.share0 + c.share1 * d) * units, bytes_us});
+            const double cost = (std::min(split_keys, span) + keys - 1) / keys * step + 0.4 * per_cu + (splits > 1 ? c.join + splits * part_us : 0);
+            if (best.tile_rows == 0 || cost < least) {
+                least = cost;
+                best = AttentionPlan{16, 1, (int)splits, (int)split_keys, waves, 0};
+            }
+            if (splits < want || per_cu > 16) break;       // more splits than keys, or than the chip holds
+        }
+    }
+    return best;
+}
+
+// More rows: estimated time of a step of a kernel's workgroups: max(a, b o) us with `o`
 // workgroups to a compute unit, linear in the head dimension d (in units of
 // 128), and no less than its bytes at 5.5 TB/s.  Fitted to measured times
 // (within about 15% over 64 .. 8192 keys, 8 .. 384 sequences times key heads,
@@ -530,8 +614,6 @@ struct StepCost {
 constexpr StepCost kStepF16[] = {{16, 128, 1.5, 0, 0.5, 1.0}, {64, 64, 0.35, 0.8, 0.325, 0.35}, {128, 64, 0.5, 1.1, 0.4, 0.65}};
 constexpr StepCost kStepF32[] = {{16, 64, 0.9, 1.2, 0.5, 1.0}, {64, 64, 0.4, 4.2, -0.7, 5.8}, {128, 64, -0.3, 7.6, 0.7, 4.65}};
 
-}  // namespace
-
 // The kernel and the splits of the keys that these estimates call cheapest.
 // Tall tiles read keys and values least often but leave CUs idle where rows are
 // few (512 new tokens on 3584 cached, 32 heads of 128, in us: 128 rows unsplit 93,
@@ -539,22 +621,18 @@ constexpr StepCost kStepF32[] = {{16, 64, 0.9, 1.2, 0.5, 1.0}, {64, 64, 0.4, 4.2
 // up to 128 rows of up to 128 keys the 16-row kernel starts soonest (7 against 8);
 // a split costs a second launch and writes and reads the partial sums (512 new
 // tokens alone: 16 unsplit, 28 in two).
-AttentionPlan attention_plan(int dtype, int64_t tokens, int64_t sequences, int q_heads, int kv_heads, int dim, int64_t max_q,
-                             int64_t max_kv, int causal, int64_t window, int cus)
+AttentionPlan many_rows_plan(int dtype, int64_t tokens, int64_t sequences, int q_heads, int kv_heads, int dim, int64_t rows,
+                             int64_t max_kv, int64_t window, int cus)
 {
-    const int64_t group = q_heads / kv_heads, rows = max_q * group, lanes = (int64_t)kv_heads * sequences;
+    const int64_t group = q_heads / kv_heads, lanes = (int64_t)kv_heads * sequences;
     const int elt = dtype == NNJIT_F16 ? 2 : 4;
     const double d = dim / 128.0, part_us = (double)tokens * q_heads * dim * 8 / 3.3e6;   // partial sums of a split, written and read
     AttentionPlan best{};
     double least = 0;
     for (const StepCost &c : dtype == NNJIT_F16 ? kStepF16 : kStepF32) {
         if (c.tile_rows == 64 && dim > 128) continue;      // not built: registers
-        if (c.tile_rows > 16 && rows <= 16) break;         // tiles that rows do not fill are no better, and less exact
         const int64_t row_tiles = (rows + c.tile_rows - 1) / c.tile_rows;
-        // keys that one tile can see: with a window, from the first row's first key
-        // (rounded down to a multiple of 32) to the last row's last
-        int64_t span = max_kv;
-        if (causal && window > 0 && window < span) span = std::min(span, window + (c.tile_rows + group - 1) / group + 32);
+        const int64_t span = seen_span(max_kv, window, c.tile_rows, group);
         for (int64_t want = 1; want <= 256; want = want < 4 ? want + 1 : want * 3 / 2 - want * 3 / 2 % 2) {
             const int64_t per = (span + want - 1) / want;
             const int64_t split_keys = std::max<int64_t>((per + 31) / 32 * 32, 32);
@@ -577,12 +655,25 @@ AttentionPlan attention_plan(int dtype, int64_t tokens, int64_t sequences, int q
                 best.row_tiles = (int)row_tiles;
                 best.splits = (int)splits;
                 best.split_keys = (int)split_keys;
+                best.waves = 4;
             }
             if (splits < want || o > 16) break;            // more splits than keys, or than the chip holds
         }
     }
-    best.ws_floats = best.splits > 1 ? best.splits * tokens * q_heads * ((dim + 3) / 4 * 4 + 2) : 0;
     return best;
+}
+
+}  // namespace
+
+AttentionPlan attention_plan(int dtype, int64_t tokens, int64_t sequences, int q_heads, int kv_heads, int dim, int64_t max_q,
+                             int64_t max_kv, int causal, int64_t window, int cus)
+{
+    const int64_t group = q_heads / kv_heads, rows = max_q * group;
+    if (!causal) window = 0;
+    AttentionPlan plan = rows <= 16 ? few_rows_plan(dtype, tokens, sequences, q_heads, kv_heads, dim, seen_span(max_kv, window, 16, group), cus)
+                                    : many_rows_plan(dtype, tokens, sequences, q_heads, kv_heads, dim, rows, max_kv, window, cus);
+    plan.ws_floats = plan.splits > 1 ? plan.splits * tokens * q_heads * ((dim + 3) / 4 * 4 + 2) : 0;
+    return plan;
 }
 
 hipError_t launch_attention(AttentionParams p, const AttentionPlan &plan, int dtype, bool vec, hipStream_t stream)
@@ -593,9 +684,9 @@ hipError_t launch_attention(AttentionParams p, const AttentionPlan &plan, int dt
     const int grid = plan.row_tiles * plan.splits * (p.q_heads / p.group) * p.batch.sequences;
     hipError_t e;
     if (dtype == NNJIT_F16)
-        e = plan.tile_rows == 16 ? launch_typed<_Float16>(p, vec, grid, stream) : launch_attention_tiles_f16(p, plan.tile_rows, vec, grid, stream);
+        e = plan.tile_rows == 16 ? launch_typed<_Float16>(p, vec, plan.waves, grid, stream) : launch_attention_tiles_f16(p, plan.tile_rows, vec, grid, stream);
     else
-        e = plan.tile_rows == 16 ? launch_typed<float>(p, vec, grid, stream) : launch_attention_tiles_f32(p, plan.tile_rows, vec, grid, stream);
+        e = plan.tile_rows == 16 ? launch_typed<float>(p, vec, plan.waves, grid, stream) : launch_attention_tiles_f32(p, plan.tile_rows, vec, grid, stream);
     if (e != hipSuccess || plan.splits == 1) return e;
     return dtype == NNJIT_F16 ? launch_join<_Float16>(p, stream) : launch_join<float>(p, stream);
 }

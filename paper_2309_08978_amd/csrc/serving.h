@@ -109,6 +109,7 @@ struct AttentionParams {
 struct AttentionPlan {
     int tile_rows;             // rows of a tile.  16: attention_rows.hip; 64, 128: attention_tiles.h
     int row_tiles, splits, split_keys;
+    int waves;                 // waves of a workgroup of attention_rows.hip, 4 or 8
     int64_t ws_floats;         // partial sums and statistics
 };
 AttentionPlan attention_plan(int dtype, int64_t tokens, int64_t sequences, int q_heads, int kv_heads, int dim, int64_t max_q,

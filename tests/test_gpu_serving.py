@@ -207,6 +207,16 @@ def test_keys_split_over_workgroups(dtype, news, keys, hq, hk):
         _case(news, keys, hq, hk, 128, 32, dtype, seed=16, window=1000)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("count,hq,hk,dim", [(2, 3, 3, 64), (5, 2, 1, 128), (8, 8, 8, 64), (9, 10, 5, 96), (13, 4, 4, 128)])
+def test_splits_of_many_sequences(dtype, count, hq, hk, dim):
+    """Every (split, sequence, head) is taken once, whatever their numbers: lengths from one to thousands."""
+    keys = [3000 if i % 3 == 0 else 1 + (971 * i) % 2500 for i in range(count)]
+    B, got = _case([1] * count, keys, hq, hk, dim, 16, dtype, seed=19)
+    assert torch.equal(got, _attend(B))
+    _case([2] * count, [k + 1 for k in keys], hq, hk, dim, 33, dtype, seed=20)
+
+
 def test_offsets_past_32_bits():
     """Pages beyond the 2^32nd byte and the 2^31st element of the pool."""
     page, hk, dim = 64, 8, 128

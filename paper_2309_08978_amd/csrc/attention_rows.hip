@@ -611,7 +611,7 @@ struct StepCost {
     int tile_rows, keys;       // rows of a tile; keys of a step
     double a0, a1, b0, b1;     // a = a0 + a1 d, b = b0 + b1 d
 };
-constexpr StepCost kStepF16[] = {{16, 128, 1.5, 0, 0.5, 1.0}, {64, 64, 0.35, 0.8, 0.325, 0.35}, {128, 64, 0.5, 1.1, 0.4, 0.65}};
+constexpr StepCost kStepF16[] = {{16, 128, 1.5, 0, 1.0, 2.0}, {64, 64, 0.35, 0.8, 0.325, 0.35}, {128, 64, 0.5, 1.1, 0.4, 0.65}};
 constexpr StepCost kStepF32[] = {{16, 64, 0.9, 1.2, 0.5, 1.0}, {64, 64, 0.4, 4.2, -0.7, 5.8}, {128, 64, -0.3, 7.6, 0.7, 4.65}};
 
 // The kernel and the splits of the keys that these estimates call cheapest.

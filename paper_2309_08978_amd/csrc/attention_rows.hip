@@ -35,8 +35,8 @@
 // as much once many workgroups take part.)
 //
 // Measured, heads of 128 in fp16, with the join: 32 ragged sequences of up to
-// 4096 keys, 32 query heads on 8 key heads: 73 us, 4.2 TB/s of keys and values
-// (69 + 4 us); one sequence of 65536 keys: 61 us, 4.4 TB/s (55 + 5); both wait
+// 4096 keys, 32 query heads on 8 key heads: 71 us, 4.3 TB/s of keys and values
+// (with the join of eight splits); one sequence of 65536 keys: 61 us, 4.4 TB/s (55 + 5); both wait
 // for memory (matrix cores busy 4% of the time).  One sequence of 1023 keys,
 // 32 heads: 11.3 us, of which two launches are 5.
 #include <algorithm>

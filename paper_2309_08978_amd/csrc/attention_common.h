@@ -21,10 +21,11 @@ struct RowTile {
     int r0, rows;         // first row of the tile, rows in it (<= 0: nothing to do)
     const int *table;     // the sequence's page table row
 
+    // (64 bits: a window of any size behind a position below zero)
     __device__ __forceinline__ int first_key(const AttentionParams &p, int r) const
     {
         if (!p.causal || p.window == 0) return 0;
-        return min(max(past + p.group_div.quot(r) - p.window + 1, 0), keys);
+        return (int)min(max((long long)past + p.group_div.quot(r) - p.window + 1, 0ll), (long long)keys);
     }
     __device__ __forceinline__ int end_key(const AttentionParams &p, int r) const
     {

@@ -442,7 +442,8 @@ typedef struct nnjit_paged_kv {
  * The arrays are read by the kernels, so a captured graph follows them; the
  * library cannot check them.  The kernels stay inside the cache and the
  * tensors all the same: a page id outside the pool is not written to and
- * read as the nearest one, keys past the table's columns do not exist.
+ * read as the nearest one, keys past the table's columns do not exist (they
+ * move no position: these follow kv_len as it stands).
  * max_q and max_kv bound the new tokens and the keys of any one sequence
  * (rows and keys beyond them may be left out); they size the launch, and a
  * value much larger than the lengths costs time, not correctness. */

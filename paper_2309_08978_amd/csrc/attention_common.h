@@ -16,7 +16,7 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 // r / group, so the query heads that share keys share a tile.
 struct RowTile {
     int q0, new_tokens;   // first row of q, new tokens of the sequence
-    int past;             // position of its first new token
+    long long past;       // position of its first new token (below zero: it and maybe others see no key)
     int keys;             // keys in the cache
     int r0, rows;         // first row of the tile, rows in it (<= 0: nothing to do)
     const int *table;     // the sequence's page table row
@@ -25,11 +25,11 @@ struct RowTile {
     __device__ __forceinline__ int first_key(const AttentionParams &p, int r) const
     {
         if (!p.causal || p.window == 0) return 0;
-        return (int)min(max((long long)past + p.group_div.quot(r) - p.window + 1, 0ll), (long long)keys);
+        return (int)min(max(past + p.group_div.quot(r) - p.window + 1, 0ll), (long long)keys);
     }
     __device__ __forceinline__ int end_key(const AttentionParams &p, int r) const
     {
-        return p.causal ? min(keys, max(past + p.group_div.quot(r) + 1, 0)) : keys;
+        return p.causal ? (int)min(max(past + p.group_div.quot(r) + 1, 0ll), (long long)keys) : keys;
     }
 };
 
@@ -41,7 +41,9 @@ __device__ __forceinline__ RowTile row_tile(const AttentionParams &p, int seq, i
     t.new_tokens = min(max(b.q_start[seq + 1] - t.q0, 0), b.tokens - t.q0);
     const long long room = (long long)b.table_pages * p.pool.page_size.d;
     t.keys = (int)min((long long)max(b.kv_len[seq], 0), room);
-    t.past = t.keys - t.new_tokens;
+    // positions follow kv_len as it stands, like those that an append turns and stores by: keys that
+    // the table has no column for do not exist, but move no other key's position
+    t.past = (long long)b.kv_len[seq] - ((long long)b.q_start[seq + 1] - t.q0);
     t.r0 = tile * tile_rows;
     t.rows = min((long long)tile_rows, (long long)t.new_tokens * p.group - t.r0);
     t.table = b.page_table + (long long)seq * b.ld_table;

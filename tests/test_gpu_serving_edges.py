@@ -1,10 +1,11 @@
 """Serving operators on the GPU at the ends of their arguments' ranges: against
 the 64-bit forms, with bounds derived where they are used."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2309_08978_amd as nj
-from tests.serving_util import DT, Batch, check_attention
+from tests.serving_util import DT, U16, U32, Batch, check_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +27,39 @@ def test_window_past_every_key(dtype, news, keys, heads, window):
     got = _attend(B, window=window)
     check_attention(B, got)
     assert torch.equal(got, _attend(B))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("news,keys,columns,hq,hk", [([8, 1], [20, 33], 1, 4, 2), ([40, 5], [50, 70], 2, 2, 2), ([1], [3000], 100, 2, 1),
+                                                     ([320, 40], [500, 330], 20, 16, 16)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 6), (False, 0)])
+def test_lengths_past_the_page_table(dtype, news, keys, columns, hq, hk, causal, window):
+    """Keys past the table's columns do not exist; positions stay those of kv_len, as an append takes them.
+
+    Bound: see tests.serving_util.attention, here with all sizes taken as the largest of the case."""
+    dim, page = 64, 16
+    B = Batch(news, keys, hq, hk, dim, page, dtype, seed=32).device()
+    table = torch.from_numpy(B.table[:, :columns].copy()).cuda()
+    B.batch = nj.PagedBatch(B.batch.q_start, B.batch.kv_len, table, tokens=B.tokens, max_q=max(news), max_kv=max(keys))
+    got = _attend(B, causal=causal, window=window).double().cpu().numpy()
+    q, group = B.q.double().numpy(), hq // hk
+    for b, (n, m) in enumerate(zip(news, keys)):
+        slots = B.key_slots(b)[:columns * page]
+        k, v = (np.stack([t[s].double().numpy() for s in slots]) for t in (B.k, B.v))
+        pos, j = np.arange(m - n, m)[:, None], np.arange(len(slots))[None]
+        seen = (j <= pos) | (not causal)
+        if window:
+            seen &= j > pos - window
+        for h in range(hq):
+            qq = q[B.start[b]:B.start[b] + n, h]
+            x = np.where(seen, dim ** -0.5 * (qq @ k[:, h // group].T), -np.inf)
+            top = x.max(1, keepdims=True)
+            w = np.where(seen, np.exp(x - np.where(seen.any(1, keepdims=True), top, 0.0)), 0.0)
+            total = w.sum(1, keepdims=True)
+            ref = np.where(total > 0, w @ v[:, h // group] / np.where(total > 0, total, 1.0), 0.0)
+            size = dim ** -0.5 * np.linalg.norm(qq, axis=1).max() * np.linalg.norm(k[:, h // group], axis=1).max()
+            e = (dim + 4) * U32 * size + 4 * U32 * size + 4 * U32
+            bound = np.abs(v).max() * (2 * e + 2 * len(slots) * U32 + (2 * U16 if dtype == "f16" else 0.0))
+            off = np.abs(got[B.start[b]:B.start[b] + n, h] - ref)
+            assert off.max() <= bound, (b, h, off.max(), bound)
+            assert (off[~seen.any(1)] == 0).all()

@@ -39,7 +39,8 @@ __device__ __forceinline__ RowTile row_tile(const AttentionParams &p, int seq, i
     const PageBatch &b = p.batch;
     t.q0 = min(max(b.q_start[seq], 0), b.tokens);
     t.new_tokens = min(max(b.q_start[seq + 1] - t.q0, 0), b.tokens - t.q0);
-    const long long room = (long long)b.table_pages * p.pool.page_size.d;
+    // (key indices stay well inside 32 bits, whatever kv_len holds)
+    const long long room = min((long long)b.table_pages * p.pool.page_size.d, kMaxKeys);
     t.keys = (int)min((long long)max(b.kv_len[seq], 0), room);
     // positions follow kv_len as it stands, like those that an append turns and stores by: keys that
     // the table has no column for do not exist, but move no other key's position

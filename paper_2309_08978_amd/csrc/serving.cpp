@@ -11,7 +11,6 @@ namespace nnjit {
 namespace {
 
 constexpr int64_t kMaxInt = 0x7fffffff;
-constexpr int64_t kMaxKeys = (int64_t)1 << 30;   // key indices stay well inside 32 bits
 constexpr int64_t kMaxGroups = 0xffffff;          // workgroups of 256 threads: a launch holds below 2^32 threads
 
 bool is_dtype(int d) { return d == NNJIT_F32 || d == NNJIT_F16; }

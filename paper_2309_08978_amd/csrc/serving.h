@@ -9,6 +9,8 @@ namespace nnjit {
 
 // Largest head dimension of the serving operators.
 constexpr int kMaxHeadDim = 256;
+// Most keys of a sequence: max_kv is refused above, and later keys do not exist.
+constexpr long long kMaxKeys = 1ll << 30;
 
 // n / d for 0 <= n < 2^31 by one multiplication (d >= 1): with
 // 2^(l-1) < d <= 2^l, l >= 1, and mul = ceil(2^(31+l) / d), which is below

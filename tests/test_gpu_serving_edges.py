@@ -63,3 +63,29 @@ def test_lengths_past_the_page_table(dtype, news, keys, columns, hq, hk, causal,
             off = np.abs(got[B.start[b]:B.start[b] + n, h] - ref)
             assert off.max() <= bound, (b, h, off.max(), bound)
             assert (off[~seen.any(1)] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("rows", [1, 40])
+@pytest.mark.parametrize("window", [0, 5])
+def test_lengths_near_2_to_the_31(dtype, rows, window):
+    """A kv_len that passes every limit is no key index past 32 bits: keys from 2^30 on do not exist.  (Pages of 2^30
+    tokens that all lie in one place, which only the C entry point takes; a non-causal or unwindowed call would walk all keys.)"""
+    page, dt = 1 << 30, DT[dtype]
+    k, v = torch.randn(2, 1, 1, 64, device="cuda").to(dt)
+    q = torch.randn(rows, 1, 64, device="cuda").to(dt)
+    out = torch.full_like(q, 7.0)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    table, start = torch.zeros(1, 3, **i32), torch.tensor([0, rows], **i32)
+    cache = nj.PagedKvDesc(k.data_ptr(), v.data_ptr(), 0, 0, 64, 0, 0, 64, 1, page, 1, 64, nj.NNJIT_F16 if dtype == "f16" else nj.NNJIT_F32)
+    for length in ((1 << 30) + 2, (1 << 31) - 3, (1 << 31) - 1):
+        lengths = torch.tensor([length], **i32)
+        # without a window only the rows' first 64 keys are asked for
+        batch = nj.PagedBatchDesc(1, rows, start.data_ptr(), lengths.data_ptr(), table.data_ptr(), 3, 3, rows, 1 << 30 if window else 64)
+        nj.check(nj.nnjit_paged_attention(cache, batch, 1, q, 64, 64, out, 64, 64, 0.125, 1, window))
+        torch.cuda.synchronize()
+        first = torch.arange(rows, device="cuda") + length - rows - window + 1     # first key that a row sees
+        sees = (first < 1 << 30) if window else first > 0
+        assert torch.equal(out[~sees], torch.zeros_like(out[~sees]))
+        # all keys are alike: the value itself, up to the rounding of a mean of equal values
+        assert torch.allclose(out[sees].float(), v.float().expand(rows, 1, 64)[sees], rtol=2e-3 if dtype == "f16" else 1e-5, atol=0)

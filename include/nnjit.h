@@ -445,8 +445,9 @@ typedef struct nnjit_paged_kv {
  * read as the nearest one, keys past the table's columns do not exist (they
  * move no position: these follow kv_len as it stands).
  * max_q and max_kv bound the new tokens and the keys of any one sequence
- * (rows and keys beyond them may be left out); they size the launch, and a
- * value much larger than the lengths costs time, not correctness. */
+ * (rows and keys beyond them may be left out: such a row of out is the full
+ * result or is not written); they size the launch, and a value much larger
+ * than the lengths costs time, not correctness. */
 typedef struct nnjit_paged_batch {
     int64_t sequences, tokens;         /* tokens: rows of q, k, v and out */
     const int32_t *q_start;            /* [sequences + 1] */

@@ -51,6 +51,20 @@ __device__ __forceinline__ RowTile row_tile(const AttentionParams &p, int seq, i
     return t;
 }
 
+// Rows of the sequence behind the last tile (max_q was too small for it) are
+// left alone; where splits are joined, the join has to be told: their largest
+// logit in the first split is a NaN, which no row that was computed has.  By the
+// threads of the last tile's first split.
+__device__ __forceinline__ void mark_left_out(const AttentionParams &p, const RowTile &t, int head, int tile, int split, int tile_rows)
+{
+    if (p.splits == 1 || split != 0 || tile != p.row_tiles - 1) return;
+    const long long rows = (long long)t.new_tokens * p.group;
+    for (long long r = (long long)p.row_tiles * tile_rows + threadIdx.x; r < rows; r += blockDim.x) {
+        const int tok = p.group_div.quot((int)r);
+        p.stat[((long long)(t.q0 + tok) * p.q_heads + head * p.group + (int)r - tok * p.group) * 2] = __builtin_nanf("");
+    }
+}
+
 // A page id that can be read whatever the table holds.
 __device__ __forceinline__ int safe_page(const AttentionParams &p, int id) { return min(max(id, 0), p.pool.pages - 1); }
 

@@ -132,6 +132,7 @@ attention_rows_kernel(AttentionParams p)
     }
     const RowTile t = row_tile(p, seq, tile, 16);
     if (t.rows <= 0) return;
+    mark_left_out(p, t, head, tile, split, 16);
 
     // keys of the tile's rows, and of this split
     const int r_last = t.r0 + t.rows - 1;
@@ -435,24 +436,27 @@ attention_join_kernel(AttentionParams p)
     const long long rows = (long long)p.batch.tokens * p.q_heads;
     const long long row = (long long)blockIdx.x * ROWS + group / GPR;
     const int token = (int)(row / p.q_heads), head = (int)(row % p.q_heads);
-    const bool live = row < rows && token >= p.batch.q_start[0] && token < p.batch.q_start[p.batch.sequences];
+    bool live = row < rows && token >= p.batch.q_start[0] && token < p.batch.q_start[p.batch.sequences];
 
     float most = -__builtin_inff(), total = 0.f;
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-    bool none = false;
+    bool none = false, left_out = false;
     if (live) {
         // the largest logit: a lane per split
         for (int s = lane; s < p.splits; s += LPR) {
             const f32x2 st = *(const f32x2 *)(p.stat + (s * rows + row) * 2);
             most = fmaxf(most, st[0]);
             none |= st[1] != st[1];
+            left_out |= st[0] != st[0];
         }
     }
 #pragma unroll
     for (int i = 1; i < LPR; i <<= 1) {
         most = fmaxf(most, __shfl_xor(most, i));
         none |= (bool)__shfl_xor((int)none, i);
+        left_out |= (bool)__shfl_xor((int)left_out, i);
     }
+    live = live && !left_out;
     if (live) {
         const float off = most == -__builtin_inff() ? 0.f : most;
         const int d = min(4 * lane, p.part_dim - 4);

@@ -89,3 +89,26 @@ def test_lengths_near_2_to_the_31(dtype, rows, window):
         assert torch.equal(out[~sees], torch.zeros_like(out[~sees]))
         # all keys are alike: the value itself, up to the rounding of a mean of equal values
         assert torch.allclose(out[sees].float(), v.float().expand(rows, 1, 64)[sees], rtol=2e-3 if dtype == "f16" else 1e-5, atol=0)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("news,keys,max_q,hq,hk,tile", [([3, 40], [3000, 2000], 3, 4, 2, 16), ([1, 17, 1], [900, 5000, 3000], 1, 3, 3, 16),
+                                                        ([320, 700], [3000, 1500], 320, 16, 4, 128)])
+def test_rows_past_max_q(dtype, news, keys, max_q, hq, hk, tile):
+    """Rows that a too small max_q leaves out keep what they held, also where keys are split: scratch of an earlier call is
+    not taken for their sums.  (Rows that share the last tile may be computed, and are right then.)"""
+    other = Batch([1], [20000], 32, 32, 64, 16, dtype, seed=33).device()
+    B = Batch(news, keys, hq, hk, 64, 16, dtype, seed=34).device(max_q=max_q)
+    _attend(other)                                           # fills the stream's scratch
+    got = _attend(B)
+    left = (got == 7.0).flatten(1).all(1).cpu()
+    for b, n in enumerate(news):
+        r = left[B.start[b]:B.start[b] + n]
+        assert not bool(r[:max_q].any())
+        assert bool(r[max_q + -(-tile * hk // hq):].all())
+    # the rows that were computed, as with a large enough max_q (another plan: other roundings)
+    B.batch.desc.max_q = max(news)
+    full = _attend(B)
+    check_attention(B, full)
+    diff = (got[~left].double() - full[~left].double()).norm() / full[~left].double().norm()
+    assert float(diff) <= (4 * U16 if dtype == "f16" else 2e-5), float(diff)

@@ -52,8 +52,8 @@ __device__ __forceinline__ RowTile row_tile(const AttentionParams &p, int seq, i
 }
 
 // Rows of the sequence behind the last tile (max_q was too small for it) are
-// left alone; where splits are joined, the join has to be told: their largest
-// logit in the first split is a NaN, which no row that was computed has.  By the
+// left alone; where splits are joined, the join has to be told: their
+// reference in the first split is a NaN, which no row that was computed has.  By the
 // threads of the last tile's first split.
 __device__ __forceinline__ void mark_left_out(const AttentionParams &p, const RowTile &t, int head, int tile, int split, int tile_rows)
 {
@@ -151,22 +151,44 @@ struct Largest16 {
     __device__ __forceinline__ bool finite() const { return top[0] < 0x7c00 && top[1] < 0x7c00; }
 };
 
-// Largest logit (times log2 e) and sum of a row's split, as the join takes them.
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A row's weights are taken against its reference, about its largest logit so
+// far.  As it moves from step to step, and from wave to wave and split to split
+// when their sums are joined, weights and sums have to be taken against the very
+// same value: a reference is kept as it was rounded.
+//   fp32: the logit itself; a weight takes the difference first, so it is off by
+//   a few roundings of its own exponent however large the logits are;
+//   fp16: scaled, for one fma a weight (a difference first costs prompts 3 to 7% of
+//   their time); what its rounding is off by is the same for all weights.
+template <bool HALF>
+__device__ __forceinline__ float reference(const AttentionParams &p, float top) { return HALF ? top * p.scale_log2 : top; }
+
+// ... as weights take it: 0 while the row has seen nothing (or only -inf), so
+// that its weights are exp2(-inf) = 0
+__device__ __forceinline__ float started(float ref) { return ref == -__builtin_inff() ? 0.f : ref; }
+
+// Weight of the logit x.
+template <bool HALF>
+__device__ __forceinline__ float weight(const AttentionParams &p, float x, float ref)
+{
+    return exp2_fast(HALF ? fmaf(x, p.scale_log2, -ref) : (x - ref) * p.scale_log2);
+}
+
+// What sums against the reference `from` are multiplied by against `to`.
+template <bool HALF>
+__device__ __forceinline__ float moved(const AttentionParams &p, float from, float to)
+{
+    return exp2_fast(HALF ? from - to : (from - to) * p.scale_log2);
+}
+
+// Reference and sum of a row's split, as the join takes them.
 // A sum that is a NaN stays one (weight exp2(inf - inf)); keys seen, but only
 // logits of -inf: 0 / 0 unless another split has more.
-__device__ __forceinline__ void store_stat(const AttentionParams &p, long long at, float top, float sum, bool sees)
+__device__ __forceinline__ void store_stat(const AttentionParams &p, long long at, float ref, float sum, bool sees)
 {
-    p.stat[at * 2] = sum != sum ? __builtin_inff() : top;
+    p.stat[at * 2] = sum != sum ? __builtin_inff() : ref;
     p.stat[at * 2 + 1] = sees && sum == 0.f ? __builtin_nanf("") : sum;
 }
-
-// A logit, or a row's reference, in powers of two, minus `off`.
-template <bool BOTH>
-__device__ __forceinline__ float scaled(const AttentionParams &p, float x, float off)
-{
-    return BOTH ? fmaf(x, p.scale_log2, fmaf(x, p.scale_low, -off)) : fmaf(x, p.scale_log2, -off);
-}
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 }  // namespace nnjit

@@ -227,7 +227,7 @@ attention_rows_kernel(AttentionParams p)
     f32x4 acc[BLK];
 #pragma unroll
     for (int b = 0; b < BLK; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -__builtin_inff(), l = 0.f;
+    float ref = -__builtin_inff(), l = 0.f;
 
     const int tiles = (k1 - k0 + KT - 1) / KT;
     Ids ids;
@@ -283,18 +283,18 @@ attention_rows_kernel(AttentionParams p)
             }
         }
 
-        float top = m;
+        float top = -__builtin_inff();
 #pragma unroll
         for (int i = 0; i < SUB * 4; ++i) top = fmaxf(top, x[i / 4][i % 4]);
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float off = top == -__builtin_inff() ? 0.f : scaled<!HALF>(p, top, 0.f);   // a row that has seen nothing yet
-        const float shrink = exp2_fast(scaled<!HALF>(p, m, off));
-        m = top;
+        const float next = fmaxf(ref, reference<HALF>(p, top)), off = started(next);
+        const float shrink = moved<HALF>(p, ref, off);
+        ref = next;
         float pr[SUB * 4], sum = 0.f;
 #pragma unroll
         for (int i = 0; i < SUB * 4; ++i) {
-            pr[i] = exp2_fast(scaled<!HALF>(p, x[i / 4][i % 4], off));
+            pr[i] = weight<HALF>(p, x[i / 4][i % 4], off);
             sum += pr[i];
         }
         l = l * shrink + sum;
@@ -366,9 +366,9 @@ attention_rows_kernel(AttentionParams p)
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
 
-    // join the waves: weights exp2(m_w - M) of their sums
+    // join the waves: their sums against the largest reference
     if (g == 0) {
-        lds_m[wave][c] = scaled<!HALF>(p, m, 0.f);
+        lds_m[wave][c] = ref;
         lds_l[wave][c] = l;
     }
     if (c < t.rows) {
@@ -388,14 +388,14 @@ attention_rows_kernel(AttentionParams p)
         float most = -__builtin_inff();
 #pragma unroll
         for (int w = 0; w < NW; ++w) most = fmaxf(most, lds_m[w][row]);
-        const float off = most == -__builtin_inff() ? 0.f : most;
+        const float off = started(most);
         float total = 0.f;
         f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const float weight = exp2_fast(lds_m[w][row] - off);
-            total += weight * lds_l[w][row];
-            o += weight * *(const f32x4 *)&lds_o[w][row][d];
+            const float part = moved<HALF>(p, lds_m[w][row], off);
+            total += part * lds_l[w][row];
+            o += part * *(const f32x4 *)&lds_o[w][row][d];
         }
         const int rr = t.r0 + row, tok = p.group_div.quot(rr);
         const int oh = head * p.group + rr - tok * p.group;
@@ -420,7 +420,8 @@ attention_rows_kernel(AttentionParams p)
     }
 }
 
-// Joins the splits of every row: o = sum_s w_s o_s / sum_s w_s l_s, w_s = exp2(m_s - M).
+// Joins the splits of every row: o = sum_s w_s o_s / sum_s w_s l_s, w_s = exp(scale (m_s - M))
+// for the references m_s and the largest of them, M.
 // A group of LPR lanes takes four dims a lane of one row; GPR groups of a
 // workgroup share a row, group i the splits i, i + GPR, ..., added in order:
 // 1 where rows fill the chip by themselves, else all groups of the workgroup,
@@ -429,6 +430,7 @@ template <typename T, int LPR, int GPR>
 __global__ void __launch_bounds__(256)
 attention_join_kernel(AttentionParams p)
 {
+    constexpr bool HALF = sizeof(T) == 2;
     constexpr int GROUPS = 256 / LPR, ROWS = GROUPS / GPR;
     __shared__ f32x4 lds_o[GPR > 1 ? GROUPS : 1][LPR];
     __shared__ float lds_l[GROUPS];
@@ -442,7 +444,7 @@ attention_join_kernel(AttentionParams p)
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
     bool none = false, left_out = false;
     if (live) {
-        // the largest logit: a lane per split
+        // the largest reference: a lane per split
         for (int s = lane; s < p.splits; s += LPR) {
             const f32x2 st = *(const f32x2 *)(p.stat + (s * rows + row) * 2);
             most = fmaxf(most, st[0]);
@@ -458,7 +460,7 @@ attention_join_kernel(AttentionParams p)
     }
     live = live && !left_out;
     if (live) {
-        const float off = most == -__builtin_inff() ? 0.f : most;
+        const float off = started(most);
         const int d = min(4 * lane, p.part_dim - 4);
 #pragma unroll 8
         for (int s = group % GPR; s < p.splits; s += GPR) {
@@ -466,7 +468,7 @@ attention_join_kernel(AttentionParams p)
             const f32x2 st = *(const f32x2 *)(p.stat + at * 2);
             const f32x4 part = *(const f32x4 *)(p.part + at * p.part_dim + d);
             const bool seen = st[0] != -__builtin_inff();          // else it has seen nothing, or only -inf
-            const float w = exp2_fast(st[0] - off);
+            const float w = moved<HALF>(p, st[0], off);
             total += seen ? w * st[1] : 0.f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] += seen ? w * part[e] : 0.f;

@@ -2,7 +2,7 @@
 // wave, keys and values shared through LDS.
 //
 // The mathematics is that of attention_rows.hip: one pass over the keys with a
-// running reference m and sum; here the matrix cores bound it.  A workgroup has WR x WK
+// running reference and sum; here the matrix cores bound it.  A workgroup has WR x WK
 // waves: WR row groups of 32 rows, WK groups that take different keys of a
 // step (joined through LDS at the end).  A step takes BN = 32 KB WK keys: K and
 // V rows go from their pages to LDS by direct copies, one or two steps ahead of the
@@ -27,7 +27,7 @@
 // keys at one chunk -- and the four keys of a transposing read fall on
 // different banks.
 //
-// The reference m of a row moves only when a logit passes it by 2^8 (the
+// The reference of a row moves only when a logit passes it by 2^8 (the
 // weights then are at most 2^8, no less exact in fp16 or fp32): the sums are
 // rescaled in the first steps and hardly ever again.
 //
@@ -110,12 +110,12 @@ template <typename T, int DP>
 __device__ __forceinline__ void redo_row(const AttentionParams &p, const RowTile &t, int head, int split, int r, int k0, int k1, int lane)
 {
     constexpr int E = (DP + 63) / 64;
-    constexpr bool BOTH = sizeof(T) == 4;
+    constexpr bool HALF = sizeof(T) == 2;
     const int lo = max(t.first_key(p, r), k0), hi = min(t.end_key(p, r), k1);
     const int token = t.q0 + p.group_div.quot(r);
     const int q_head = head * p.group + r - p.group_div.quot(r) * p.group;
     const T *q = (const T *)p.q.p + (long long)token * p.q.tok + (long long)q_head * p.q.head;
-    float qv[E], o[E], m = -__builtin_inff(), l = 0.f;
+    float qv[E], o[E], ref = -__builtin_inff(), l = 0.f;
     for (int e = 0; e < E; ++e) {
         qv[e] = lane + 64 * e < p.dim ? (float)q[lane + 64 * e] : 0.f;
         if (p.negate) qv[e] = -qv[e];
@@ -131,9 +131,9 @@ __device__ __forceinline__ void redo_row(const AttentionParams &p, const RowTile
         for (int e = 0; e < E; ++e)
             if (lane + 64 * e < p.dim) x += qv[e] * (float)k[lane + 64 * e];
         for (int i = 1; i < 64; i <<= 1) x += __shfl_xor(x, i);
-        const float next = fmaxf(m, x), off = next == -__builtin_inff() ? 0.f : next;
-        const float shrink = exp2_fast(scaled<BOTH>(p, m - off, 0.f)), w = exp2_fast(scaled<BOTH>(p, x - off, 0.f));
-        m = next;
+        const float next = fmaxf(ref, reference<HALF>(p, x)), off = started(next);
+        const float shrink = moved<HALF>(p, ref, off), w = weight<HALF>(p, x, off);
+        ref = next;
         l = l * shrink + w;
         for (int e = 0; e < E; ++e)
             if (lane + 64 * e < p.dim) o[e] = o[e] * shrink + w * (float)v[lane + 64 * e];
@@ -148,7 +148,7 @@ __device__ __forceinline__ void redo_row(const AttentionParams &p, const RowTile
             if (d < p.part_dim) p.part[at * p.part_dim + d] = o[e];
         }
     }
-    if (p.splits > 1 && lane == 0) store_stat(p, at, scaled<BOTH>(p, m, 0.f), l, hi > lo);
+    if (p.splits > 1 && lane == 0) store_stat(p, at, ref, l, hi > lo);
 }
 
 // Bytes of a row in LDS, and the waves a SIMD is to hold: two, of two
@@ -370,9 +370,9 @@ attention_tiles_kernel(AttentionParams p)
     f32x16 acc[BLK];
 #pragma unroll
     for (int b = 0; b < BLK; ++b) acc[b] = f32x16{};
-    float m = -__builtin_inff(), l = 0.f;
-    constexpr bool BOTH = sizeof(T) == 4;
-    const float slack = kSlack / p.scale_log2;
+    float ref = -__builtin_inff(), l = 0.f;
+    constexpr bool SCALED = sizeof(T) == 2;               // references and weights of fp16
+    const float slack = SCALED ? kSlack : kSlack / p.scale_log2;
 
     // lane parts of the LDS addresses
     const int kw = wk * KB * 32;                          // first key of this wave in a step
@@ -509,20 +509,21 @@ attention_tiles_kernel(AttentionParams p)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
         top = max_of_halves(top);
-        if (__any(top - m > slack)) {
-            const float next = fmaxf(m, top);
-            const float shrink = exp2_fast(scaled<BOTH>(p, m - (next == -__builtin_inff() ? 0.f : next), 0.f));
-            m = next;
+        const float peak = reference<SCALED>(p, top);
+        if (__any(peak - ref > slack)) {
+            const float next = fmaxf(ref, peak);
+            const float shrink = moved<SCALED>(p, ref, started(next));
+            ref = next;
             l *= shrink;
 #pragma unroll
             for (int blk = 0; blk < BLK; ++blk) acc[blk] *= shrink;
         }
-        const float off = m == -__builtin_inff() ? 0.f : scaled<BOTH>(p, m, 0.f);   // a row that has seen nothing yet
+        const float off = started(ref);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                x[kb][i] = exp2_fast(scaled<BOTH>(p, x[kb][i], off));
+                x[kb][i] = weight<SCALED>(p, x[kb][i], off);
                 l += x[kb][i];
             }
         add_values(std::bool_constant<!WHOLE>{}, x, b);
@@ -601,7 +602,7 @@ attention_tiles_kernel(AttentionParams p)
         lds_barrier();
         if (wk > 0) {
             lds_float *box = box_of(wk);
-            box[0] = m;
+            box[0] = ref;
             box[64] = l;
             box[128] = dirty ? 1.f : 0.f;
 #pragma unroll
@@ -614,12 +615,12 @@ attention_tiles_kernel(AttentionParams p)
 #pragma unroll
         for (int g = 1; g < WK; ++g) {
             lds_float *box = box_of(g);
-            const float om = box[0], ol = box[64];
+            const float other = box[0], ol = box[64];
             dirty |= box[128] != 0.f;
-            const float next = fmaxf(m, om);
-            const float off = next == -__builtin_inff() ? 0.f : next;
-            const float mine = exp2_fast(scaled<BOTH>(p, m - off, 0.f)), theirs = exp2_fast(scaled<BOTH>(p, om - off, 0.f));
-            m = next;
+            const float next = fmaxf(ref, other);
+            const float off = started(next);
+            const float mine = moved<SCALED>(p, ref, off), theirs = moved<SCALED>(p, other, off);
+            ref = next;
             l = l * mine + ol * theirs;
 #pragma unroll
             for (int blk = 0; blk < BLK; ++blk)
@@ -669,7 +670,7 @@ attention_tiles_kernel(AttentionParams p)
                     if (d < dim) *(f32x4 *)(p.part + at * p.part_dim + d) = f32x4{o[0], o[1], o[2], o[3]};
                 }
             }
-    if (p.splits > 1 && h == 0) store_stat(p, at, scaled<BOTH>(p, m, 0.f), l, sees);
+    if (p.splits > 1 && h == 0) store_stat(p, at, ref, l, sees);
 }
 
 template <typename T, int DP, int HOW, int KB>

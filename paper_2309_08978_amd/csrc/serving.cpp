@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <limits>
 
 #include "nnjit.h"
 #include "serving.h"
@@ -313,10 +314,7 @@ int nnjit_paged_attention(const nnjit_paged_kv *cache, const nnjit_paged_batch *
     c.p.batch = batch_of(batch);
     // a scale of 0 (all keys alike) would make NaNs of masked logits: 2^-100 leaves
     // the weights of all q . k below 2^76 alike to the last bit
-    const double factor = std::fmax(std::fabs((double)scale) * 1.4426950408889634074, 0x1p-100);
-    c.p.scale_log2 = (float)factor;
-    if ((double)c.p.scale_log2 > factor) c.p.scale_log2 = std::nextafterf(c.p.scale_log2, 0.f);
-    c.p.scale_low = std::fmax((float)(factor - (double)c.p.scale_log2), 0x1p-126f);
+    c.p.scale_log2 = (float)std::fmin(std::fmax(std::fabs((double)scale) * 1.4426950408889634074, 0x1p-100), (double)std::numeric_limits<float>::max());
     c.p.negate = scale < 0.f;
     c.p.causal = causal != 0;
     c.p.window = (int)std::min<int64_t>(window, kMaxInt);

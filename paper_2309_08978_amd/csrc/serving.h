@@ -93,9 +93,7 @@ struct AttentionParams {
     FastDiv group_div;
     PagePool pool;
     PageBatch batch;
-    float scale_log2, scale_low;   // |scale| log2(e), cut to fp32, and what that leaves (fp32 operands
-                               // take both: logits of 10 times a constant off by 6e-8 would be off by more
-                               // than their own rounding); scale_low > 0, so that -inf stays -inf
+    float scale_log2;          // |scale| log2(e), finite and above 0, so that -inf stays -inf
     int negate;                // the scale is negative: queries are taken negated
     int causal, window;
     int row_tiles;             // row tiles of a sequence and key head
@@ -103,7 +101,7 @@ struct AttentionParams {
     int split_keys;            // keys of one split (a multiple of the key tile)
     int part_dim;              // dim rounded up to a multiple of 4
     float *part;               // splits > 1: [splits][tokens * q_heads][part_dim], not normalised
-    float *stat;               // splits > 1: [splits][tokens * q_heads][2]: largest logit (times log2 e), sum
+    float *stat;               // splits > 1: [splits][tokens * q_heads][2]: reference (attention_common.h), sum
     const void *zero;          // >= 64 bytes of zeros
 };
 

@@ -112,3 +112,45 @@ def test_rows_past_max_q(dtype, news, keys, max_q, hq, hk, tile):
     check_attention(B, full)
     diff = (got[~left].double() - full[~left].double()).norm() / full[~left].double().norm()
     assert float(diff) <= (4 * U16 if dtype == "f16" else 2e-5), float(diff)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("news,keys,hq,hk,dim", [([1], [700], 2, 2, 64), ([1] * 32, [700] * 32, 8, 8, 64), ([3], [2000], 4, 2, 128),
+                                                 ([320], [700], 16, 16, 64), ([320], [700], 4, 4, 128), ([320], [2500], 16, 4, 128),
+                                                 ([320], [700], 16, 16, 200)])
+def test_references_of_any_size(dtype, news, keys, hq, hk, dim):
+    """Large logits that grow along the keys, so that every row's reference moves again and again, with values that shrink as the
+    weights grow: all steps count alike.  The logits are exact (multiples of 1/16), so only the weights' own roundings are left.
+
+    Bound on an element, in units of the mean of |v| by weight: an exponent is a difference of logits, times a rounded scale,
+    rounded: 3 U32 of the row's spread in all, along every chain of references; an exp2 is off by 2 ulp, once a key and once
+    a move (of at most one in 16 keys); the sums of n terms by n U32 each.  fp16: weights rounded to 11 bits, and the result."""
+    step, most = (6.0, 11) if dtype == "f32" else (6.0, 1)
+    B = Batch(news, keys, hq, hk, dim, 16, dtype, seed=35)
+    rng = np.random.default_rng(36)
+    B.q.zero_()
+    B.q[..., 0], B.q[..., 1] = 256.0, 1.0
+    rows = []
+    for b, m in enumerate(keys):
+        level = np.minimum(np.arange(m) * 16 // max(m, 1), most)
+        small = np.round((step * level + rng.normal(0, 0.5, m)) * 16) / 16
+        value = rng.uniform(0.5, 1.5, (m, hk, dim)) * (np.where(level % 2, -1.0, 1.0) * np.exp(step * (most - level)))[:, None, None]
+        for j, s in enumerate(B.key_slots(b)):
+            B.k[s][:, 0], B.k[s][:, 1] = 512.0, float(small[j])
+            B.v[s] = torch.from_numpy(value[j]).to(DT[dtype])
+        rows.append((small, np.stack([B.v[s].double().numpy() for s in B.key_slots(b)])))
+    got = _attend(B.device(), scale=1.0).double().cpu().numpy()
+    for b, (n, m) in enumerate(zip(news, keys)):
+        small, v = rows[b]
+        for i in range(n):
+            x = small[:m - n + i + 1]
+            w = np.exp(x - x.max())
+            vv = v[:len(x)]
+            ref, mean = np.tensordot(w, vv, 1) / w.sum(), np.tensordot(w, np.abs(vv), 1) / w.sum()
+            spread = x.max() - x.min()
+            bound = mean * (2 * (3 * spread + 4 + len(x) / 4) + 2 * len(x)) * U32
+            if dtype == "f16":
+                bound = bound + mean * U16 + np.abs(ref) * U16 + 2.0 ** -25
+            off = np.abs(got[B.start[b] + i] - np.repeat(ref, hq // hk, 0))
+            worst = (off / np.repeat(bound, hq // hk, 0)).max()
+            assert worst <= 1, (b, i, worst)

@@ -16,7 +16,7 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 // r / group, so the query heads that share keys share a tile.
 struct RowTile {
     int q0, new_tokens;   // first row of q, new tokens of the sequence
-    long long past;       // position of its first new token (below zero: it and maybe others see no key)
+    int past;             // position of its first new token (below zero: it and maybe others see no key)
     int keys;             // keys in the cache
     int r0, rows;         // first row of the tile, rows in it (<= 0: nothing to do)
     const int *table;     // the sequence's page table row
@@ -25,11 +25,11 @@ struct RowTile {
     __device__ __forceinline__ int first_key(const AttentionParams &p, int r) const
     {
         if (!p.causal || p.window == 0) return 0;
-        return (int)min(max(past + p.group_div.quot(r) - p.window + 1, 0ll), (long long)keys);
+        return (int)min(max((long long)past + p.group_div.quot(r) - p.window + 1, 0ll), (long long)keys);
     }
     __device__ __forceinline__ int end_key(const AttentionParams &p, int r) const
     {
-        return p.causal ? (int)min(max(past + p.group_div.quot(r) + 1, 0ll), (long long)keys) : keys;
+        return p.causal ? min(keys, max(past + p.group_div.quot(r) + 1, 0)) : keys;
     }
 };
 
@@ -44,7 +44,8 @@ __device__ __forceinline__ RowTile row_tile(const AttentionParams &p, int seq, i
     t.keys = (int)min((long long)max(b.kv_len[seq], 0), room);
     // positions follow kv_len as it stands, like those that an append turns and stores by: keys that
     // the table has no column for do not exist, but move no other key's position
-    t.past = (long long)b.kv_len[seq] - ((long long)b.q_start[seq + 1] - t.q0);
+    // (no position passes kv_len, so their sums stay in 32 bits)
+    t.past = (int)max((long long)b.kv_len[seq] - ((long long)b.q_start[seq + 1] - t.q0), -0x7fffffffll);
     t.r0 = tile * tile_rows;
     t.rows = min((long long)tile_rows, (long long)t.new_tokens * p.group - t.r0);
     t.table = b.page_table + (long long)seq * b.ld_table;
@@ -54,12 +55,14 @@ __device__ __forceinline__ RowTile row_tile(const AttentionParams &p, int seq, i
 // Rows of the sequence behind the last tile (max_q was too small for it) are
 // left alone; where splits are joined, the join has to be told: their
 // reference in the first split is a NaN, which no row that was computed has.  By the
-// threads of the last tile's first split.
+// THREADS threads of the last tile's first split, and only where the batch has more
+// rows than the tiles of one sequence.
+template <int THREADS>
 __device__ __forceinline__ void mark_left_out(const AttentionParams &p, const RowTile &t, int head, int tile, int split, int tile_rows)
 {
-    if (p.splits == 1 || split != 0 || tile != p.row_tiles - 1) return;
+    if (!p.may_leave_out || split != 0 || tile != p.row_tiles - 1) return;
     const long long rows = (long long)t.new_tokens * p.group;
-    for (long long r = (long long)p.row_tiles * tile_rows + threadIdx.x; r < rows; r += blockDim.x) {
+    for (long long r = (long long)p.row_tiles * tile_rows + threadIdx.x; r < rows; r += THREADS) {
         const int tok = p.group_div.quot((int)r);
         p.stat[((long long)(t.q0 + tok) * p.q_heads + head * p.group + (int)r - tok * p.group) * 2] = __builtin_nanf("");
     }

@@ -132,7 +132,7 @@ attention_rows_kernel(AttentionParams p)
     }
     const RowTile t = row_tile(p, seq, tile, 16);
     if (t.rows <= 0) return;
-    mark_left_out(p, t, head, tile, split, 16);
+    mark_left_out<NW * 64>(p, t, head, tile, split, 16);
 
     // keys of the tile's rows, and of this split
     const int r_last = t.r0 + t.rows - 1;
@@ -438,27 +438,24 @@ attention_join_kernel(AttentionParams p)
     const long long rows = (long long)p.batch.tokens * p.q_heads;
     const long long row = (long long)blockIdx.x * ROWS + group / GPR;
     const int token = (int)(row / p.q_heads), head = (int)(row % p.q_heads);
-    bool live = row < rows && token >= p.batch.q_start[0] && token < p.batch.q_start[p.batch.sequences];
+    const bool live = row < rows && token >= p.batch.q_start[0] && token < p.batch.q_start[p.batch.sequences];
 
     float most = -__builtin_inff(), total = 0.f;
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-    bool none = false, left_out = false;
+    int marks = 0;                                             // 1: 0 / 0, 2: left out (mark_left_out)
     if (live) {
         // the largest reference: a lane per split
         for (int s = lane; s < p.splits; s += LPR) {
             const f32x2 st = *(const f32x2 *)(p.stat + (s * rows + row) * 2);
             most = fmaxf(most, st[0]);
-            none |= st[1] != st[1];
-            left_out |= st[0] != st[0];
+            marks |= (st[1] != st[1] ? 1 : 0) | (st[0] != st[0] ? 2 : 0);
         }
     }
 #pragma unroll
     for (int i = 1; i < LPR; i <<= 1) {
         most = fmaxf(most, __shfl_xor(most, i));
-        none |= (bool)__shfl_xor((int)none, i);
-        left_out |= (bool)__shfl_xor((int)left_out, i);
+        marks |= __shfl_xor(marks, i);
     }
-    live = live && !left_out;
     if (live) {
         const float off = started(most);
         const int d = min(4 * lane, p.part_dim - 4);
@@ -486,11 +483,11 @@ attention_join_kernel(AttentionParams p)
             total += lds_l[group + g];
         }
     }
-    if (!live) return;
+    if (!live || (marks & 2)) return;
     const bool empty = most == -__builtin_inff();
     T *dst = (T *)p.o.p + (long long)token * p.o.tok + (long long)head * p.o.head + 4 * lane;
     for (int e = 0; e < 4; ++e)
-        if (4 * lane + e < p.dim) dst[e] = (T)(empty ? (none ? __builtin_nanf("") : 0.f) : o[e] / total);
+        if (4 * lane + e < p.dim) dst[e] = (T)(empty ? ((marks & 1) ? __builtin_nanf("") : 0.f) : o[e] / total);
 }
 
 template <typename T>
@@ -687,6 +684,7 @@ hipError_t launch_attention(AttentionParams p, const AttentionPlan &plan, int dt
     p.row_tiles = plan.row_tiles;
     p.splits = plan.splits;
     p.split_keys = plan.split_keys;
+    p.may_leave_out = plan.splits > 1 && (int64_t)plan.row_tiles * plan.tile_rows < (int64_t)p.batch.tokens * p.group;
     const int grid = plan.row_tiles * plan.splits * (p.q_heads / p.group) * p.batch.sequences;
     hipError_t e;
     if (dtype == NNJIT_F16)

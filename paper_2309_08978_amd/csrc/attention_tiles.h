@@ -213,7 +213,7 @@ attention_tiles_kernel(AttentionParams p)
     const int seq = id / kv_heads;
     const RowTile t = row_tile(p, seq, tile, 32 * WR);
     if (t.rows <= 0) return;
-    mark_left_out(p, t, head, tile, split, 32 * WR);
+    mark_left_out<NW * 64>(p, t, head, tile, split, 32 * WR);
 
     const int r_last = t.r0 + t.rows - 1;
     const int lo_min = t.first_key(p, t.r0), hi_max = t.end_key(p, r_last);

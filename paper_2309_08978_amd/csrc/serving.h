@@ -99,6 +99,7 @@ struct AttentionParams {
     int row_tiles;             // row tiles of a sequence and key head
     int splits;                // workgroups along the keys
     int split_keys;            // keys of one split (a multiple of the key tile)
+    int may_leave_out;         // splits are joined, and a sequence may have more rows than tiles
     int part_dim;              // dim rounded up to a multiple of 4
     float *part;               // splits > 1: [splits][tokens * q_heads][part_dim], not normalised
     float *stat;               // splits > 1: [splits][tokens * q_heads][2]: reference (attention_common.h), sum

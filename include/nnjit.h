@@ -521,9 +521,10 @@ int nnjit_kv_append(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch,
  * in places that a token does not see -- unused slots, other positions' keys
  * and values, infinities and NaN among them -- does not touch its row.
  * Softmax statistics and sums are held in fp32.  fp16: weights go to the
- * matrix cores in fp16, so those below 2^-25 of the row's largest may count as
- * 0 (and an infinite value seen with such a weight may give NaN in place of an
- * infinity).  fp32: values below 2^-110 are taken to an absolute 2^-126.
+ * matrix cores in fp16 -- in two parts for up to 16 rows of a sequence and key
+ * head, rounded once to 11 bits for more -- so those below 2^-24 of the row's
+ * largest lose bits and those below 2^-35 may count as 0 (and an infinite value
+ * seen with such a weight may give NaN in place of an infinity).  fp32: values below 2^-110 are taken to an absolute 2^-126.
  * Results do not depend on the order in which workgroups run.  The stream's scratch (see "Stream
  * capture" above) is used when keys are split over workgroups. */
 int nnjit_paged_attention(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch, int64_t q_heads,

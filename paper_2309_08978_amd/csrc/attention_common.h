@@ -163,9 +163,19 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 //   fp32: the logit itself; a weight takes the difference first, so it is off by
 //   a few roundings of its own exponent however large the logits are;
 //   fp16: scaled, for one fma a weight (a difference first costs prompts 3 to 7% of
-//   their time); what its rounding is off by is the same for all weights.
-template <bool HALF>
-__device__ __forceinline__ float reference(const AttentionParams &p, float top) { return HALF ? top * p.scale_log2 : top; }
+//   their time); what its rounding is off by is the same for all weights.  And
+//   2^LIFT below the logit: fp16 weights lose bits below 2^-14, so that many more of the
+//   small ones, which may be all of a result if the largest meets a value near zero,
+//   keep theirs; it cancels in the division.  Rounded up by two to four units in the last
+//   place: the weight of `top` must not pass 2^LIFT, nor that of a logit a rounded sum
+//   above it what the sum says, where such a unit is worth more than fp16's room above.
+template <bool HALF, int LIFT>
+__device__ __forceinline__ float reference(const AttentionParams &p, float top)
+{
+    if (!HALF) return top;
+    const float ref = fmaf(top, p.scale_log2, -(float)LIFT);
+    return fmaf(fabsf(ref), 0x1p-22f, ref);               // (-inf gives a NaN, which no fmaxf() takes)
+}
 
 // ... as weights take it: 0 while the row has seen nothing (or only -inf), so
 // that its weights are exp2(-inf) = 0

@@ -24,8 +24,9 @@
 // so lane (c, g) ends up with 4 VE consecutive dims of row c, next to row c's
 // maximum and sum: rescaling needs no exchange, the maximum two shuffles a
 // tile.  In fp16 the eight keys of an operand are gathered from eight loaded
-// vectors by byte permutes.  Probabilities go into the products in two fp16
-// parts (p = hi + lo, 22 bits): matrix cores have nothing else to do here.
+// vectors by byte permutes.  Weights go into the products in two fp16 parts (p =
+// hi + lo: matrix cores have nothing else to do here) and are up to 2^15: they are
+// held to 22 bits, or to 2^-40 of the row's largest.
 //
 // The waves of a workgroup are joined through LDS at the end.  Keys are split
 // over workgroups where sequences and key heads alone leave the chip idle; a
@@ -48,6 +49,8 @@
 namespace nnjit {
 
 namespace {
+
+constexpr int kLiftRows = 15;                 // fp16 weights are at most 2^15 (the largest half: 2^16)
 
 template <typename T> struct RowsOf;
 template <> struct RowsOf<_Float16> {
@@ -288,7 +291,7 @@ attention_rows_kernel(AttentionParams p)
         for (int i = 0; i < SUB * 4; ++i) top = fmaxf(top, x[i / 4][i % 4]);
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float next = fmaxf(ref, reference<HALF>(p, top)), off = started(next);
+        const float next = fmaxf(ref, reference<HALF, kLiftRows>(p, top)), off = started(next);
         const float shrink = moved<HALF>(p, ref, off);
         ref = next;
         float pr[SUB * 4], sum = 0.f;

@@ -154,3 +154,40 @@ def test_references_of_any_size(dtype, news, keys, hq, hk, dim):
             off = np.abs(got[B.start[b] + i] - np.repeat(ref, hq // hk, 0))
             worst = (off / np.repeat(bound, hq // hk, 0)).max()
             assert worst <= 1, (b, i, worst)
+
+
+@pytest.mark.parametrize("news,keys,hq,hk,dim,page", [([1] * 2, [700, 60], 2, 2, 64, 16), ([1] * 16, [900] * 16, 8, 8, 64, 16), ([2], [5000], 4, 2, 128, 5),
+                                                      ([1], [700], 2, 1, 256, 16), ([320], [700], 16, 16, 64, 16), ([320], [700], 4, 4, 128, 5),
+                                                      ([320], [2500], 16, 4, 128, 16), ([600], [600], 32, 32, 64, 16), ([200], [700], 16, 16, 200, 16)])
+@pytest.mark.parametrize("bits", [12.3, 20.6, 23.5, 25.0])
+def test_small_weights_fp16(news, keys, hq, hk, dim, page, bits):
+    """A first key that takes nearly all weight but has values of zero: the result is the sum of the others, whose weights
+    (about 2^-bits of the largest) must have kept their bits."""
+    B = Batch(news, keys, hq, hk, dim, page, "f16", seed=37)
+    rng = np.random.default_rng(38)
+    B.q.zero_()
+    B.q[..., 0] = 1.0
+    for b, m in enumerate(keys):
+        for j, s in enumerate(B.key_slots(b)):
+            B.k[s][:, 0] = bits * float(np.log(2.0)) + 1.0 if j == 0 else float(rng.normal(1.0, 0.3))
+            B.v[s] = 0.0 if j == 0 else B.v[s] * 512.0
+    check_attention(B, _attend(B.device(), scale=1.0), scale=1.0)
+
+
+@pytest.mark.parametrize("news,keys,heads", [([1] * 3, [700, 60, 3000], 2), ([320], [700], 16)])
+@pytest.mark.parametrize("size", [2.0 ** 12, 2.0 ** 20, 2.0 ** 25])
+def test_large_logits_fp16(news, keys, heads, size):
+    """Logits whose last bit in fp32 is worth up to 2: nearly one-hot rows, finite, and right where the largest logit is clear."""
+    B = Batch(news, keys, heads, heads, 64, 16, "f16", seed=39)
+    B.q *= size ** 0.5 / 8
+    B.k *= size ** 0.5 / 8
+    got = _attend(B.device(), scale=1.0).double().cpu().numpy()
+    assert np.isfinite(got).all()
+    for b, (n, m) in enumerate(zip(news, keys)):
+        k, v = (np.stack([t[s].double().numpy() for s in B.key_slots(b)]) for t in (B.k, B.v))
+        for i in range(n):
+            x = np.einsum("hd,jhd->hj", B.q[int(B.start[b]) + i].double().numpy(), k[:m - n + i + 1])
+            order = np.sort(x, 1)
+            clear = order[:, -1] - order[:, -2] > 30 + 68 * U32 * size * 8 if x.shape[1] > 1 else np.ones(heads, dtype=bool)
+            want = v[x.argmax(1), np.arange(heads)]
+            assert (np.abs(got[B.start[b] + i] - want)[clear] <= 2 * U16 * np.abs(want)[clear] + 1e-6).all()

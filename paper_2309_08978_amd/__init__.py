@@ -3,16 +3,19 @@
 Every ``nnjit_*`` function here has the name and argument order of the C
 entry point it calls and returns its integer code unchanged; pointer
 arguments accept a ``torch.Tensor`` (its ``data_ptr()``), an int or None, and
-``stream`` accepts a ``torch.cuda.Stream``, an int handle or None.  All the
-work runs in the HIP library; if ``libnnjit.so`` is missing the binding
-raises instead of falling back to anything else.
+``stream`` accepts a ``torch.cuda.Stream``, an int handle or None (the default
+stream, as NULL in C).  All the work runs in the HIP library; if
+``libnnjit.so`` is missing the binding raises instead of falling back to
+anything else.
 
 ``matmul`` / ``batched_matmul`` are conveniences that take tensors, derive
 (M, N, K), leading dimensions and batch strides from them, call the entry
 point and raise ``NnjitError`` on a negative code.  ``rotary`` /
 ``kv_append`` / ``paged_attention`` do the same for the operators of a served
 decoder, with ``RotaryTable``, ``PagedCache`` and ``PagedBatch`` as the
-handles that a program keeps.
+handles that a program keeps.  All of these run on the tensors' GPU, on
+``stream`` or, without one, on the stream that torch works on there; an output
+that they allocate belongs to that stream.
 """
 from __future__ import annotations
 
@@ -465,16 +468,42 @@ def _plain_lds(A, B, C, sa, sb, sc):
 _CODES: dict = {}     # torch dtype -> code; filled on first use (torch is imported lazily)
 _F32 = None
 _torch_module = None
+_torch_stream = _torch_device = None     # handle of torch's current stream on a GPU; the current GPU (0.1 us each)
 
 
 def _torch():
-    global _F32, _torch_module
+    global _F32, _torch_module, _torch_stream, _torch_device
     if _torch_module is None:
         import torch
         _CODES.update({torch.float32: NNJIT_F32, torch.float16: NNJIT_F16})
         _F32 = torch.float32
+        _torch_stream, _torch_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         _torch_module = torch
     return _torch_module
+
+
+def _launch(entry, device_index: int, stream, *args) -> int:
+    """entry(*args, stream), checked, with the operands' GPU current: on
+    ``stream`` or, if None, on torch's current one there, so that the call is
+    ordered with the other work on its tensors and with the reuse of their
+    memory."""
+    s = _torch_stream(device_index) if stream is None else _stream(stream)
+    if _torch_device() == device_index:
+        return check(entry(*args, s))
+    with _torch_module.cuda.device(device_index):
+        return check(entry(*args, s))
+
+
+def _empty(shape, dtype, device, stream):
+    """An output from the memory of the stream that will write it: another
+    stream's could still be in use there."""
+    torch = _torch()
+    if stream is None or device.type != "cuda":
+        return torch.empty(shape, dtype=dtype, device=device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def matmul(A, B, C=None, stream=None, cfg: Optional[int] = None):
@@ -486,16 +515,16 @@ def matmul(A, B, C=None, stream=None, cfg: Optional[int] = None):
     M, K = sa
     N = sb[1]
     if C is None:
-        C = torch.empty((M, N), dtype=torch.float32, device=A.device)
+        C = _empty((M, N), torch.float32, A.device, stream)
     sc = C.shape
     p = _plain_lds(A, B, C, sa, sb, sc) if len(sc) == 2 else None
     lda, ldb, ldc = p[:3] if p else _check_operands(A, B, C, batched=False)
     dt = dtype_code(A) if not p else _CODES[A.dtype]
     if cfg is None:
-        check((_lib or load()).nnjit_matmul(M, N, K, A.data_ptr(), lda, B.data_ptr(), ldb, C.data_ptr(), ldc, dt,
-                                            _stream(stream)))
+        _launch((_lib or load()).nnjit_matmul, A.get_device(), stream, M, N, K, A.data_ptr(), lda, B.data_ptr(), ldb,
+                C.data_ptr(), ldc, dt)
     else:
-        check(nnjit_matmul_config(cfg, 1, M, N, K, A, lda, 0, B, ldb, 0, C, ldc, 0, dt, stream))
+        _launch(nnjit_matmul_config, A.get_device(), stream, cfg, 1, M, N, K, A, lda, 0, B, ldb, 0, C, ldc, 0, dt)
     return C
 
 
@@ -508,7 +537,7 @@ def batched_matmul(A, B, C=None, stream=None, cfg: Optional[int] = None):
     batch, M, K = sa
     N = sb[2]
     if C is None:
-        C = torch.empty((batch, M, N), dtype=torch.float32, device=A.device)
+        C = _empty((batch, M, N), torch.float32, A.device, stream)
     sc = C.shape
     p = _plain_lds(A, B, C, sa, sb, sc) if len(sc) == 3 else None
     if p:
@@ -519,10 +548,10 @@ def batched_matmul(A, B, C=None, stream=None, cfg: Optional[int] = None):
         dt = dtype_code(A)
         sA, sB, sC = (int(t.stride(0)) for t in (A, B, C))
     if cfg is None:
-        check((_lib or load()).nnjit_batched_matmul(batch, M, N, K, A.data_ptr(), lda, sA, B.data_ptr(), ldb, sB,
-                                                    C.data_ptr(), ldc, sC, dt, _stream(stream)))
+        _launch((_lib or load()).nnjit_batched_matmul, A.get_device(), stream, batch, M, N, K, A.data_ptr(), lda, sA,
+                B.data_ptr(), ldb, sB, C.data_ptr(), ldc, sC, dt)
     else:
-        check(nnjit_matmul_config(cfg, batch, M, N, K, A, lda, sA, B, ldb, sB, C, ldc, sC, dt, stream))
+        _launch(nnjit_matmul_config, A.get_device(), stream, cfg, batch, M, N, K, A, lda, sA, B, ldb, sB, C, ldc, sC, dt)
     return C
 
 
@@ -542,8 +571,8 @@ def gemv_q4(x, Wq, scales, group: int, N: int, y=None, stream=None, cfg: Optiona
                 and y.dtype is _F32 and y.shape == (N,) and y.stride(0) == 1
                 and x.is_cuda and Wq.is_cuda and scales.is_cuda and y.is_cuda
                 and x.get_device() == Wq.get_device() == scales.get_device() == y.get_device()):
-            check((_lib or load()).nnjit_gemv_q4(N, K, group, x.data_ptr(), Wq.data_ptr(), tw[0], scales.data_ptr(),
-                                                 ts[0], y.data_ptr(), _stream(stream)))
+            _launch((_lib or load()).nnjit_gemv_q4, x.get_device(), stream, N, K, group, x.data_ptr(), Wq.data_ptr(), tw[0],
+                    scales.data_ptr(), ts[0], y.data_ptr())
             return y
     if x.dim() != 1 or (x.shape[0] > 1 and x.stride(0) != 1):
         raise ValueError(f"x must be a contiguous vector, got shape {tuple(x.shape)}")
@@ -557,7 +586,7 @@ def gemv_q4(x, Wq, scales, group: int, N: int, y=None, stream=None, cfg: Optiona
     if x.dtype != torch.float16 or scales.dtype != torch.float16 or Wq.element_size() != 4:
         raise TypeError("x and scales must be float16, Wq 32-bit words")
     if y is None:
-        y = torch.empty((N,), dtype=torch.float32, device=x.device)
+        y = _empty((N,), torch.float32, x.device, stream)
     if y.dtype != torch.float32 or tuple(y.shape) != (N,) or (N > 1 and y.stride(0) != 1):
         raise ValueError(f"y must be a contiguous float32 vector of {N}, got {y.dtype} {tuple(y.shape)}")
     devs = {t.device for t in (x, Wq, scales, y)}
@@ -565,9 +594,9 @@ def gemv_q4(x, Wq, scales, group: int, N: int, y=None, stream=None, cfg: Optiona
         raise ValueError(f"x, Wq, scales and y must be on one GPU, got {sorted(str(d) for d in devs)}")
     ldq, lds = _ld(Wq), _ld(scales)
     if cfg is None:
-        check(nnjit_gemv_q4(N, K, group, x, Wq, ldq, scales, lds, y, stream))
+        _launch(nnjit_gemv_q4, x.get_device(), stream, N, K, group, x, Wq, ldq, scales, lds, y)
     else:
-        check(nnjit_gemv_q4_config(cfg, N, K, group, x, Wq, ldq, scales, lds, y, stream))
+        _launch(nnjit_gemv_q4_config, x.get_device(), stream, cfg, N, K, group, x, Wq, ldq, scales, lds, y)
     return y
 
 
@@ -625,10 +654,9 @@ class RotaryTable:
 def rotary_table(positions: int, rotary_dim: int, base: float = 10000.0, layout: str = "half",
                  scaling: Optional[RotaryScaling] = None, device="cuda", stream=None) -> RotaryTable:
     """A RotaryTable for positions 0 .. positions - 1 (nnjit_rotary_fill)."""
-    import torch
-    table = torch.empty((positions, rotary_dim), dtype=torch.float32, device=device)
-    with torch.cuda.device(table.device):
-        check(nnjit_rotary_fill(table, positions, rotary_dim, base, scaling, stream))
+    torch = _torch()
+    table = _empty((positions, rotary_dim), torch.float32, torch.device(device), stream)
+    _launch(nnjit_rotary_fill, table.get_device(), stream, table, positions, rotary_dim, base, scaling)
     return RotaryTable(table, layout)
 
 
@@ -639,7 +667,7 @@ class PagedCache:
     ``transpose(1, 2)``)."""
 
     def __init__(self, k, v):
-        torch = _torch()
+        _torch()
         for name, t in (("k", k), ("v", v)):
             if t.dim() != 4 or 0 in t.shape:
                 raise ValueError(f"{name} must be [pages, page_size, kv_heads, head_dim], got {tuple(t.shape)}")
@@ -714,7 +742,7 @@ def rotary(x, positions, table: RotaryTable, out=None, transpose: bool = False, 
         raise ValueError(f"x must be [tokens, heads, head_dim], got {tuple(shape)}")
     tokens, heads, dim = shape
     if out is None:
-        out = torch.empty((tokens, heads, dim), dtype=x.dtype, device=x.device)
+        out = _empty((tokens, heads, dim), x.dtype, x.device, stream)
     xd, yd, dev = x.dtype, out.dtype, table.device_index
     if xd not in _CODES or yd not in _CODES:
         raise TypeError(f"unsupported dtype {xd} to {yd}")
@@ -724,9 +752,8 @@ def rotary(x, positions, table: RotaryTable, out=None, transpose: bool = False, 
         raise ValueError(f"positions must be int32 of shape ({tokens},) on x's GPU, got {positions.dtype} {tuple(positions.shape)}")
     if tokens > 1 and positions.stride(0) != 1:
         raise ValueError("positions must be contiguous")
-    check((_lib or load()).nnjit_rotary(table.address, tokens, heads, dim, positions.data_ptr(), x.data_ptr(), sx[0], sx[1],
-                                        _CODES[xd], out.data_ptr(), sy[0], sy[1], _CODES[yd], 1 if transpose else 0,
-                                        _stream(stream)))
+    _launch((_lib or load()).nnjit_rotary, dev, stream, table.address, tokens, heads, dim, positions.data_ptr(), x.data_ptr(),
+            sx[0], sx[1], _CODES[xd], out.data_ptr(), sy[0], sy[1], _CODES[yd], 1 if transpose else 0)
     return out
 
 
@@ -736,7 +763,7 @@ def kv_append(cache: PagedCache, batch: PagedBatch, k, v, rotary: Optional[Rotar
     the batch's slots of the cache; turns q [tokens, heads, head_dim] of the
     same type into q_out (of the cache's type, allocated if None), which is
     returned (None without q)."""
-    torch = _torch()
+    _torch()
     n, dim, dev = batch.tokens, cache.head_dim, cache.device_index
     dt = k.dtype
     if dt not in _CODES:
@@ -750,14 +777,14 @@ def kv_append(cache: PagedCache, batch: PagedBatch, k, v, rotary: Optional[Rotar
         heads = q.shape[1] if q.dim() == 3 else -1
         sq = _head_rows("q", q, n, heads, dim, dt, dev)
         if q_out is None:
-            q_out = torch.empty((n, heads, dim), dtype=cache.dtype, device=q.device)
+            q_out = _empty((n, heads, dim), cache.dtype, q.device, stream)
         so = _written_rows("q_out", q_out, n, heads, dim, cache.dtype, dev)
         qp, op = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out without q")
-    check((_lib or load()).nnjit_kv_append(cache.address, batch.address, None if rotary is None else rotary.address,
-                                           k.data_ptr(), sk[0], sk[1], v.data_ptr(), sv[0], sv[1], heads, qp, sq[0], sq[1],
-                                           op, so[0], so[1], _CODES[dt], _stream(stream)))
+    _launch((_lib or load()).nnjit_kv_append, dev, stream, cache.address, batch.address,
+            None if rotary is None else rotary.address, k.data_ptr(), sk[0], sk[1], v.data_ptr(), sv[0], sv[1], heads, qp,
+            sq[0], sq[1], op, so[0], so[1], _CODES[dt])
     return q_out
 
 
@@ -766,7 +793,7 @@ def paged_attention(q, cache: PagedCache, batch: PagedBatch, out=None, scale: Op
     """Attention of q [tokens, heads, head_dim] over the cached keys and values
     of every row's sequence; q and out are of the cache's type.  ``scale``
     defaults to head_dim ** -0.5; ``window`` > 0: the last ``window`` keys only."""
-    torch = _torch()
+    _torch()
     shape = q.shape
     if len(shape) != 3:
         raise ValueError(f"q must be [tokens, heads, head_dim], got {tuple(shape)}")
@@ -775,11 +802,10 @@ def paged_attention(q, cache: PagedCache, batch: PagedBatch, out=None, scale: Op
         raise ValueError("cache and batch must be on one GPU")
     sq = _head_rows("q", q, batch.tokens, heads, dim, cache.dtype, dev)
     if out is None:
-        out = torch.empty((batch.tokens, heads, dim), dtype=cache.dtype, device=q.device)
+        out = _empty((batch.tokens, heads, dim), cache.dtype, q.device, stream)
     so = _written_rows("out", out, batch.tokens, heads, dim, cache.dtype, dev)
-    check((_lib or load()).nnjit_paged_attention(cache.address, batch.address, heads, q.data_ptr(), sq[0], sq[1],
-                                                 out.data_ptr(), so[0], so[1], dim ** -0.5 if scale is None else scale,
-                                                 1 if causal else 0, window, _stream(stream)))
+    _launch((_lib or load()).nnjit_paged_attention, dev, stream, cache.address, batch.address, heads, q.data_ptr(), sq[0],
+            sq[1], out.data_ptr(), so[0], so[1], dim ** -0.5 if scale is None else scale, 1 if causal else 0, window)
     return out
 
 

@@ -525,8 +525,11 @@ int nnjit_kv_append(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch,
  * head, rounded once to 11 bits for more -- so those below 2^-24 of the row's
  * largest lose bits and those below 2^-35 may count as 0 (and an infinite value
  * seen with such a weight may give NaN in place of an infinity).  fp32: values below 2^-110 are taken to an absolute 2^-126.
- * Results do not depend on the order in which workgroups run.  The stream's scratch (see "Stream
- * capture" above) is used when keys are split over workgroups. */
+ * Results do not depend on the order in which workgroups run.  The stream's
+ * scratch (see "Stream capture" above) is used when keys are split over
+ * workgroups: as much as tokens, sequences, max_q and max_kv, heads, head_dim,
+ * window and type ask for, whatever the lengths on the device; a call of the
+ * same sizes outside capture readies it. */
 int nnjit_paged_attention(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch, int64_t q_heads,
                           const void *q, int64_t q_token, int64_t q_head, void *out, int64_t out_token, int64_t out_head,
                           float scale, int causal, int64_t window, void *stream);

@@ -211,7 +211,7 @@ int device_ready(Device **out) {
     return NNJIT_OK;
 }
 
-// Split-K scratch for (device, stream); grown on demand (under g_mu).  The
+// Scratch (partial sums of split products and of attention) for (device, stream); grown on demand (under g_mu).  The
 // outgrown buffer is retired, not freed: launches still queued on the stream
 // and graphs captured on it keep using it, so growing needs no wait.
 int workspace_for(Device &d, hipStream_t stream, int64_t ws_floats, float **out) {
@@ -222,14 +222,14 @@ int workspace_for(Device &d, hipStream_t stream, int64_t ws_floats, float **out)
         hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
         if (hipStreamIsCapturing(stream, &cap) != hipSuccess) (void)hipGetLastError();
         if (cap != hipStreamCaptureStatusNone)
-            return fail(NNJIT_EHIP, "split-K scratch of %lld floats needed while the stream is being captured; "
-                                    "run this shape once on the stream outside capture first", (long long)ws_floats);
+            return fail(NNJIT_EHIP, "scratch of %lld floats needed while the stream is being captured; "
+                                    "run a call of the same sizes once on the stream outside capture first", (long long)ws_floats);
         const int64_t nf = std::max(w.ws_floats, ws_floats + ws_floats / 4);
         float *fresh = nullptr;
         hipError_t e = hipMalloc((void **)&fresh, (size_t)std::max<int64_t>(nf, 1) * sizeof(float));
         if (e != hipSuccess) {
             (void)hipGetLastError();
-            return fail(NNJIT_ENOMEM, "split-K scratch of %lld floats", (long long)nf);
+            return fail(NNJIT_ENOMEM, "scratch of %lld floats", (long long)nf);
         }
         if (w.ws) d.retired.push_back(w.ws);
         w.ws = fresh;

@@ -1,5 +1,7 @@
 """Serving operators on the GPU at the ends of their arguments' ranges: against
 the 64-bit forms, with bounds derived where they are used."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -191,3 +193,30 @@ def test_large_logits_fp16(news, keys, heads, size):
             clear = order[:, -1] - order[:, -2] > 30 + 68 * U32 * size * 8 if x.shape[1] > 1 else np.ones(heads, dtype=bool)
             want = v[x.argmax(1), np.arange(heads)]
             assert (np.abs(got[B.start[b] + i] - want)[clear] <= 2 * U16 * np.abs(want)[clear] + 1e-6).all()
+
+
+def test_capture_that_needs_scratch():
+    """A captured call whose stream lacks the scratch is refused with what to do; lengths of the run that readies it are free."""
+    B = Batch([1], [5000], 4, 1, 128, 16, "f16", seed=40).device()
+    want = _attend(B)
+    # a stream of its own: torch hands its streams out again and again, with the scratch of earlier calls
+    handle = ctypes.c_void_p()
+    assert nj.load().hipStreamCreateWithFlags(ctypes.byref(handle), 1) == 0
+    s, out = torch.cuda.ExternalStream(handle.value), torch.empty_like(B.dq)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        with pytest.raises(nj.NnjitError, match="^NNJIT_EHIP: scratch of .* being captured; run a call of the same sizes once"):
+            nj.paged_attention(B.dq, B.cache, B.batch, out)
+    B.batch.kv_len.fill_(3)
+    nj.paged_attention(B.dq, B.cache, B.batch, out, stream=s)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph := torch.cuda.CUDAGraph(), stream=s):
+        nj.paged_attention(B.dq, B.cache, B.batch, out)
+    B.batch.kv_len.fill_(5000)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)

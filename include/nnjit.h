@@ -506,7 +506,10 @@ int nnjit_rotary(const nnjit_rotary_table *rotary, int64_t tokens, int64_t heads
  * cache, rounded to its type, and turns the queries of the same rows into
  * q_out (of the cache's type), in one launch.  k, v: head rows of kv_heads
  * heads, q: of q_heads heads, all of src_dtype; q_heads == 0: no queries.
- * rotary NULL: nothing is turned.  Two sequences must not share the pages
+ * rotary NULL: nothing is turned.  Positions are clamped to the table, as by
+ * nnjit_rotary: a token behind it is turned by the last position's angles, which
+ * no argument check can see (the lengths lie on the device), so the table has
+ * to reach as far as the longest sequence grows.  Two sequences must not share the pages
  * that new tokens go to.  max_q and max_kv are not used. */
 int nnjit_kv_append(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch, const nnjit_rotary_table *rotary,
                     const void *k, int64_t k_token, int64_t k_head, const void *v, int64_t v_token, int64_t v_head,

@@ -762,7 +762,8 @@ def kv_append(cache: PagedCache, batch: PagedBatch, k, v, rotary: Optional[Rotar
     """Writes k (turned) and v [tokens, kv_heads, head_dim], fp32 or fp16, to
     the batch's slots of the cache; turns q [tokens, heads, head_dim] of the
     same type into q_out (of the cache's type, allocated if None), which is
-    returned (None without q)."""
+    returned (None without q).  ``rotary`` has to hold every position that the
+    sequences reach: later ones are turned by its last angles."""
     _torch()
     n, dim, dev = batch.tokens, cache.head_dim, cache.device_index
     dt = k.dtype

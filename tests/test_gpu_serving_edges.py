@@ -220,3 +220,15 @@ def test_capture_that_needs_scratch():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+def test_append_behind_the_table():
+    """Positions behind the rotary table are clamped to it, as nnjit_rotary clamps them; slots are not."""
+    cache = nj.PagedCache(torch.zeros(2, 16, 1, 8, device="cuda"), torch.zeros(2, 16, 1, 8, device="cuda"))
+    i32 = dict(dtype=torch.int32, device="cuda")
+    batch = nj.PagedBatch(torch.tensor([0, 3], **i32), torch.tensor([12], **i32), torch.tensor([[1, 0]], **i32), tokens=3)
+    table = nj.rotary_table(11, 8)
+    x = torch.randn(3, 1, 8, device="cuda")
+    q = nj.kv_append(cache, batch, x, x, table, x)
+    want = nj.rotary(x, torch.tensor([9, 10, 10], **i32), table)
+    assert torch.equal(q, want) and torch.equal(cache.k[1, 9:12], want) and torch.equal(cache.v[1, 9:12], x)

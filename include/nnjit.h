@@ -527,7 +527,9 @@ int nnjit_kv_append(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch,
  * matrix cores in fp16 -- in two parts for up to 16 rows of a sequence and key
  * head, rounded once to 11 bits for more -- so those below 2^-24 of the row's
  * largest lose bits and those below 2^-35 may count as 0 (and an infinite value
- * seen with such a weight may give NaN in place of an infinity).  fp32: values below 2^-110 are taken to an absolute 2^-126.
+ * seen with such a weight may give NaN in place of an infinity).  fp32: values below 2^-110 are taken to an absolute 2^-126,
+ * and a sum of values by weights of at most 1 (the largest at least 2^-5) has to
+ * stay in range before it is divided by the sum of the weights.
  * Results do not depend on the order in which workgroups run.  The stream's
  * scratch (see "Stream capture" above) is used when keys are split over
  * workgroups: as much as tokens, sequences, max_q and max_kv, heads, head_dim,

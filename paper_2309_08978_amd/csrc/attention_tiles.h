@@ -102,8 +102,10 @@ __device__ __forceinline__ float max_of_halves(float x)
     return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
 }
 
-// A row's reference is moved when a logit passes it by 2^kSlack; fp16 weights are
-// then at most 2^(kLift + kSlack), half of the largest half.  Every move scales all
+// A row's reference is moved when a logit passes the one that it was taken from by
+// 2^kSlack.  fp16 weights are then at most 2^(kLift + kSlack), half of the largest half;
+// fp32 references lie that much above their logit, so that weights are at most 1 and
+// no value times a weight overflows.  Every move scales all
 // sums: 512 tokens at the end of 2048 with logits spread by 2^2.9, 32 heads of 128,
 // 37.0 us with a slack of 2, 36.1 with 5, 35.7 with 7 or 8.
 constexpr int kSlack = 5, kLift = 10;
@@ -519,10 +521,11 @@ attention_tiles_kernel(AttentionParams p)
             for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
         top = max_of_halves(top);
         if (__any(top > limit)) {
-            const float next = fmaxf(ref, reference<SCALED, kLift>(p, top));
+            const float room = top + slack;
+            const float next = fmaxf(ref, SCALED ? reference<true, kLift>(p, top) : room);
             const float shrink = moved<SCALED>(p, ref, started(next));
             ref = next;
-            limit = fmaxf(limit, top + slack);
+            limit = SCALED ? fmaxf(limit, room) : next;
             l *= shrink;
 #pragma unroll
             for (int blk = 0; blk < BLK; ++blk) acc[blk] *= shrink;

@@ -52,11 +52,11 @@ def test_windows_on_long_contexts(dtype, news, keys, hq, hk, dim, window):
 
 
 @pytest.mark.parametrize("page", [16, 5])
-@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")], ids=str)
-@pytest.mark.parametrize("case", [c for c in COVER if c[6] > 16 or c[8] == 8], ids=name)
+@pytest.mark.parametrize("case,bad", [pytest.param(c, x, id=f"{name(c)}-{x}") for c in COVER if c[6] > 16 or c[8] == 8
+                                      for x in [float("inf"), float("-inf"), float("nan")] + [3.395e38, 3.4e38] * (c[0] == "f32")])
 def test_every_kernel_bad_values(case, bad, page):
-    """Values that are not finite at late and early keys, in some dims; a query row that is not finite:
-    each reaches the rows and dims that see it, and no other loses a bit."""
+    """Values that are not finite, or (fp32) close to the largest float or so close that bf16 cannot hold them, at late and early
+    keys, in some dims; a query row that is not finite: each reaches the rows and dims that see it, and no other loses a bit."""
     B = _batch(case, page, 0, 54)
     hk, dim = B.hk, B.dim
     s = B.key_slots(0)

@@ -412,7 +412,7 @@ int nnjit_stream_read(const void *src, int64_t bytes, void *sink, int workgroups
  * elements and >= 0, the dims of a head are contiguous.  Column ranges of one
  * qkv result are such rows.  Any alignment is served; rows that begin at
  * multiples of 16 bytes (with head_dim a multiple of 16 bytes' worth) faster.
- * head_dim is 1 .. 256.
+ * head_dim is 1 .. 256; a row that is turned or appended has up to 2^30 heads.
  *
  * The structs below are plain descriptions that the caller keeps; the library
  * reads them during the call only.  Errors, streams, capture and threads as

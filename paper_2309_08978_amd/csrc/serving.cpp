@@ -12,6 +12,7 @@ namespace nnjit {
 namespace {
 
 constexpr int64_t kMaxInt = 0x7fffffff;
+constexpr int64_t kMaxHeads = (int64_t)1 << 30;   // of a row that is turned: steps from head to head stay inside 32 bits
 constexpr int64_t kMaxGroups = 0xffffff;          // workgroups of 256 threads: a launch holds below 2^32 threads
 
 bool is_dtype(int d) { return d == NNJIT_F32 || d == NNJIT_F16; }
@@ -209,8 +210,8 @@ int nnjit_rotary(const nnjit_rotary_table *rotary, int64_t tokens, int64_t heads
                  int y_dtype, int transpose, void *stream) {
     runtime_clear_error();
     if (!is_dtype(x_dtype) || !is_dtype(y_dtype)) return runtime_fail(NNJIT_EDTYPE, "unsupported dtype %d to %d", x_dtype, y_dtype);
-    if (tokens < 0 || tokens > kMaxInt || heads < 0 || heads > kMaxInt)
-        return runtime_fail(NNJIT_EINVAL, "tokens=%lld, heads=%lld out of [0, 2^31)", (long long)tokens, (long long)heads);
+    if (tokens < 0 || tokens > kMaxInt || heads < 0 || heads > kMaxHeads)
+        return runtime_fail(NNJIT_EINVAL, "tokens=%lld out of [0, 2^31) or heads=%lld out of [0, 2^30]", (long long)tokens, (long long)heads);
     int rc = check_dim(head_dim);
     if (rc != NNJIT_OK) return rc;
     if (!rotary) return runtime_fail(NNJIT_EINVAL, "rotary is NULL");
@@ -247,7 +248,8 @@ int nnjit_kv_append(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch,
     if (rc != NNJIT_OK) return rc;
     if ((rc = check_batch(batch)) != NNJIT_OK) return rc;
     if (!is_dtype(src_dtype)) return runtime_fail(NNJIT_EDTYPE, "unsupported dtype %d", src_dtype);
-    if (q_heads < 0 || q_heads > kMaxInt - 2 * cache->kv_heads) return runtime_fail(NNJIT_EINVAL, "q_heads=%lld out of range", (long long)q_heads);
+    if (q_heads < 0 || q_heads > kMaxHeads - 2 * cache->kv_heads)
+        return runtime_fail(NNJIT_EINVAL, "q_heads=%lld out of [0, 2^30 - 2 kv_heads]", (long long)q_heads);
     const int64_t dim = cache->head_dim;
     if ((rc = check_slots("K", cache, cache->k_page, cache->k_token, cache->k_head)) != NNJIT_OK) return rc;
     if ((rc = check_slots("V", cache, cache->v_page, cache->v_token, cache->v_head)) != NNJIT_OK) return rc;

@@ -525,11 +525,13 @@ int nnjit_kv_append(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch,
  * and values, infinities and NaN among them -- does not touch its row.
  * Softmax statistics and sums are held in fp32.  fp16: weights go to the
  * matrix cores in fp16 -- in two parts for up to 16 rows of a sequence and key
- * head, rounded once to 11 bits for more -- so those below 2^-24 of the row's
- * largest lose bits and those below 2^-35 may count as 0 (and an infinite value
- * seen with such a weight may give NaN in place of an infinity).  fp32: values below 2^-110 are taken to an absolute 2^-126,
- * and a sum of values by weights of at most 1 (the largest at least 2^-5) has to
- * stay in range before it is divided by the sum of the weights.
+ * head, for more perhaps rounded once to 11 bits -- so those below 2^-24 of the
+ * row's largest lose bits and those below 2^-35 may count as 0.  fp32: values
+ * below 2^-110 are taken to an absolute 2^-126, and a sum of values by weights
+ * of at most 1 (the largest at least 2^-5) has to stay in range before it is
+ * divided by the sum of the weights.  An infinite value seen with a weight that
+ * counts as 0 (fp32: below 2^-120 of the largest) may give NaN in place of an
+ * infinity.
  * Results do not depend on the order in which workgroups run.  The stream's
  * scratch (see "Stream capture" above) is used when keys are split over
  * workgroups: as much as tokens, sequences, max_q and max_kv, heads, head_dim,

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import paper_2309_08978_amd as nj
-from tests.serving_util import DT, U16, U32, Batch, check_attention
+from tests.serving_util import DT, U16, U32, Batch, attention, check_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -232,3 +232,19 @@ def test_append_behind_the_table():
     q = nj.kv_append(cache, batch, x, x, table, x)
     want = nj.rotary(x, torch.tensor([9, 10, 10], **i32), table)
     assert torch.equal(q, want) and torch.equal(cache.k[1, 9:12], want) and torch.equal(cache.v[1, 9:12], x)
+
+
+@pytest.mark.parametrize("count,keys,heads,dim", [(4, 500, 12, 64), (2, 300, 8, 128), (1, 700, 8, 256), (24, 500, 8, 64), (1, 3000, 4, 96)])
+def test_rounding_of_single_rows_fp32(count, keys, heads, dim):
+    """The error that roundings of independent sign leave, in U32 relative to the result.
+
+    A logit is a sum of dim products of keys N(0, 1) and queries N(0, 4): a chain of m sums with steps of size 2 rounds m / sqrt(6)
+    times that off (each partial sum by U32 / sqrt(3) of its size 2 sqrt(j)), four chains of dim / 4 are off by half of what one
+    chain over all is.  That error of a weight is the result's (values N(0, 1): sums of w_j d_j v_j against sums of w_j v_j).
+    Weights, sums over the keys and the division leave about 3 more; a factor of 1.4 (one chain has 2) for all that is estimated."""
+    B = Batch([1] * count, [keys - 7 * i for i in range(count)], heads, heads, dim, 16, "f32", seed=41, q_scale=2.0).device()
+    ref, _ = attention(B)
+    off = _attend(B).double().cpu().numpy() - ref
+    logit = dim ** -0.5 * 2 * 2.0 * (dim / 4) / 6 ** 0.5
+    rel = np.linalg.norm(off) / np.linalg.norm(ref) / U32
+    assert rel <= (1.4 ** 2 * logit ** 2 + 9) ** 0.5, (rel, logit)

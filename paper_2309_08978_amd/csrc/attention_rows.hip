@@ -2,7 +2,7 @@
 //
 //   o[r] = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale q_r . k_j - m)
 //
-// in one pass over the keys with a running maximum m and sum.  A decode step
+// in one pass over the keys with a running reference m (attention_common.h) and sum.  A decode step
 // reads every key and value once for a handful of multiplications each:
 // bandwidth-bound, so the kernel keeps loads in flight and everything else in
 // registers.
@@ -37,9 +37,9 @@
 //
 // Measured, heads of 128 in fp16, with the join: 32 ragged sequences of up to
 // 4096 keys, 32 query heads on 8 key heads: 71 us, 4.3 TB/s of keys and values
-// (with the join of eight splits); one sequence of 65536 keys: 61 us, 4.4 TB/s (55 + 5); both wait
+// (with the join of eight splits); one sequence of 65536 keys: 61 us, 4.4 TB/s (55 + 6); both wait
 // for memory (matrix cores busy 4% of the time).  One sequence of 1023 keys,
-// 32 heads: 11.3 us, of which two launches are 5.
+// 32 heads: 11.6 us, of which two launches are 5.
 #include <algorithm>
 #include <cmath>
 

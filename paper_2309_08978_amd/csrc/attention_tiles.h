@@ -45,16 +45,18 @@
 // exist for prompts whose 128-row tiles leave compute units idle.
 //
 // Measured: 2048 new tokens at the end of 16384, 32 heads of 128 on 8, fp16:
-// 522 us, 987 TFLOP/s (a large matrix product: 1210): the clock, which power
+// 527 us, 977 TFLOP/s (a large matrix product: 1210): the clock, which power
 // holds at about 1.8 GHz under this load -- a quarter fewer scalar instructions, or
 // a step's logits computed one step ahead of its softmax (555 -> 545), change
-// next to nothing.  512 tokens at the end of 2048, 32 heads: 37 us, 410 TFLOP/s,
+// next to nothing.  512 tokens at the end of 2048, 32 heads: 37 us, 407 TFLOP/s,
 // 31 and 6 for the join of two splits; ragged prompts of up to 777 tokens, 12
 // heads of 64: 20 us, the 13 steps of the longest tile, one after the other.
 // fp32 in three bf16 parts: four sequences of 256 rows on 256 keys, 16 heads of
-// 64: 17 us, 63 TFLOP/s; 2048 tokens alone, 32 heads of 128 on 8: 269 us, 128
+// 64: 17 us, 62 TFLOP/s; 2048 tokens alone, 32 heads of 128 on 8: 269 us, 128
 // TFLOP/s (a large fp32 matrix product: 153), against 372 on the fp32 matrix
-// cores.
+// cores.  (With heads of 128 the queries' parts, the sums and the raw chunks are more
+// than the registers of two waves a SIMD: tiles of 128 rows spill 36 of them, 148
+// bytes of scratch a lane.)
 #pragma once
 
 #include <type_traits>

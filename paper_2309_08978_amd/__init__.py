@@ -498,7 +498,8 @@ def _empty(shape, dtype, device, stream):
     """An output from the memory of the stream that will write it: another
     stream's could still be in use there."""
     torch = _torch()
-    if stream is None or device.type != "cuda":
+    if stream is None or device.type != "cuda" or _stream(stream) == _torch_stream(
+            _torch_device() if device.index is None else device.index):
         return torch.empty(shape, dtype=dtype, device=device)
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)

@@ -160,8 +160,8 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // far.  As it moves from step to step, and from wave to wave and split to split
 // when their sums are joined, weights and sums have to be taken against the very
 // same value: a reference is kept as it was rounded.
-//   fp32: the logit itself; a weight takes the difference first, so it is off by
-//   a few roundings of its own exponent however large the logits are;
+//   fp32: a logit (tall tiles: plus a constant); a weight takes the difference first, so
+//   it is off by a few roundings of its own exponent however large the logits are;
 //   fp16: scaled, for one fma a weight (a difference first costs prompts 3 to 7% of
 //   their time); what its rounding is off by is the same for all weights.  And
 //   2^LIFT below the logit: fp16 weights lose bits below 2^-14, so that many more of the

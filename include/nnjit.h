@@ -541,6 +541,170 @@ int nnjit_paged_attention(const nnjit_paged_kv *cache, const nnjit_paged_batch *
                           const void *q, int64_t q_token, int64_t q_head, void *out, int64_t out_token, int64_t out_head,
                           float scale, int causal, int64_t window, void *stream);
 
+/* ------------------------------------------------- a step of drafted tokens
+ *
+ * What a served decoder does around its layers when several tokens of a
+ * sequence are tried at once: a drafter proposes a tree of next tokens, one step
+ * runs them all, the longest accepted path stays.  A step is
+ *   nnjit_paged_step        the arrays of the batch from the requests' lengths
+ *   per layer: nnjit_kv_append_slots (with the norms of queries and keys)
+ *              and nnjit_tree_attention
+ *   nnjit_adjust_logits     penalties, biases and grammars on the logits
+ *   per layer: nnjit_kv_move, the accepted path's keys and values to their places
+ * and the next step's lengths say what was kept.  Plain decoding is the same
+ * with one new token a sequence (nnjit_paged_attention, no moves).
+ * Conventions, types and limits as above. */
+
+/* Free pages: a stack, ids free_pages[0 .. count - 1], on the device.
+ * capacity: entries that free_pages holds; a program that puts every page of its
+ * cache there once never needs more. */
+typedef struct nnjit_page_pool {
+    int32_t *free_pages;               /* [capacity] */
+    int64_t capacity;
+    const int32_t *count;              /* [1] */
+    int32_t *count_out;                /* [1]: the count after the step; may be count */
+} nnjit_page_pool;
+
+/* The arrays of one step, all on the device.  Sequence b holds the pages of
+ * held[b] tokens, of which the first keep[b] stay (NULL: all), and gets added[b]
+ * new ones. */
+typedef struct nnjit_step_arrays {
+    int64_t sequences, tokens;         /* tokens: rows that slots, positions, parent and mask hold */
+    const int32_t *held, *keep, *added;/* [sequences] */
+    const int32_t *parent;             /* [tokens] or NULL, see nnjit_paged_step */
+    int32_t *page_table;               /* [sequences][ld_table], table_pages used: read and written */
+    int64_t ld_table, table_pages, page_size;
+    int32_t *q_start;                  /* [sequences + 1], written, as all below */
+    int32_t *kv_len;                   /* [sequences]; may be held or keep */
+    int32_t *positions;                /* [tokens], or NULL */
+    int64_t *slots;                    /* [tokens], or NULL */
+    uint32_t *mask;                    /* [tokens][ld_mask], mask_words used; only with parent */
+    int64_t ld_mask, mask_words;
+    int32_t *status;                   /* [4] */
+} nnjit_step_arrays;
+
+/* The step's arrays in one launch, from lengths that lie on the device:
+ *   q_start      starts of the sequences' new rows; kv_len[b] = keep[b] + added[b]
+ *   page_table   sequences that need fewer pages for kv_len than for held put the others
+ *                back on the stack, in order of sequence and page; then those that
+ *                need more take theirs from its top, in the same order
+ *   slots[t]     page * page_size + slot of row t's place keep[b] + i in the cache (row t:
+ *                new token i of sequence b); -1 for rows behind the last sequence
+ *   positions[t] keep[b] + i; 0 behind the last sequence
+ * With parent the new tokens of a sequence are the nodes of a drafted tree:
+ * parent[t] is the index (within the sequence) of the node that t follows, below its own;
+ * -1 -- and any value that is no earlier node -- says that t follows the cached
+ * tokens.  Then
+ *   positions[t] keep[b] + the number of t's ancestors among the new tokens
+ *   mask[t]      bit i (of word i / 32) set if t sees new token i: its ancestors and itself;
+ *                words of rows behind the last sequence are 0
+ * and a sequence has up to 32 mask_words new tokens, mask_words <= 32.
+ * All or nothing: status[0] is 0, or the sum of 1 (pages are missing: status[1] of
+ * them), 2 (a length is negative, keep above held, or more keys than the table has
+ * columns for or 2^30), 4 (more new rows than tokens, or than mask_words hold), 8 (count
+ * outside 0 .. capacity, or the stack would grow past its capacity).  Unless it
+ * is 0 the step is empty -- q_start 0, no slot, kv_len = held -- and page table and pool
+ * are as they were.  status[2]: rows of the step, status[3]: free pages after it.
+ * (status[1] is 0 where lengths are wrong.)
+ * sequences <= 8192, tokens < 2^24.  No scratch; a pool or lengths in place
+ * (count_out == count, kv_len == held or keep) cost large batches a second launch. */
+int nnjit_paged_step(const nnjit_page_pool *pool, const nnjit_step_arrays *step, void *stream);
+
+/* Norms of heads: a row x of head_dim dims becomes x r w, r = (mean of x^2 +
+ * eps)^(-1/2).  Weights lie at q_weight[h * q_head + i]; q_head (k_head) 0: one
+ * weight for all heads.  Squares are summed in fp32. */
+typedef struct nnjit_head_norm {
+    const void *q_weight, *k_weight;   /* NULL: those heads are not normed */
+    int64_t q_head, k_head;
+    int dtype;                         /* of both weights */
+    float eps;                         /* >= 0 */
+} nnjit_head_norm;
+
+/* nnjit_kv_append by slots: row t's key and value go to slot slots[t] (page *
+ * page_size + slot) of the cache, queries and keys normed, then turned by the
+ * angles of positions[t].  norm NULL: no norms; rotary NULL: nothing is
+ * turned (positions may then be NULL).  A row whose slot is negative or not in the cache is left
+ * alone: nothing is stored, and its row of q_out is not written.  No
+ * slot twice.  (Queries alone: nnjit_norm_rotary.) */
+int nnjit_kv_append_slots(const nnjit_paged_kv *cache, int64_t tokens, const int64_t *slots, const int32_t *positions,
+                          const nnjit_rotary_table *rotary, const nnjit_head_norm *norm,
+                          const void *k, int64_t k_token, int64_t k_head, const void *v, int64_t v_token, int64_t v_head,
+                          int64_t q_heads, const void *q, int64_t q_token, int64_t q_head,
+                          void *q_out, int64_t qo_token, int64_t qo_head, int src_dtype, void *stream);
+
+/* y = the normed rows of x, turned, without a cache: what a training step
+ * runs forward.  weight, w_head, w_dtype, eps as nnjit_head_norm's; rotary NULL:
+ * norm only.  y may be x (same strides and type). */
+int nnjit_norm_rotary(const nnjit_rotary_table *rotary, int64_t tokens, int64_t heads, int64_t head_dim, const int32_t *positions,
+                      const void *weight, int64_t w_head, int w_dtype, float eps,
+                      const void *x, int64_t x_token, int64_t x_head, int x_dtype,
+                      void *y, int64_t y_token, int64_t y_head, int y_dtype, void *stream);
+
+/* Its gradients: with g = dy turned back,
+ *   dx = r (g w - x r mean(g w x r)),   dw = sum over rows of g x r
+ * (of each head on its own if w_head > 0, dw [heads][head_dim], else of all heads, dw
+ * [head_dim]; fp32, overwritten).  dx has x's type and may be dy or x (same
+ * strides and type); dx or dw may be NULL.  Sums are added in an order
+ * that depends on the sizes only.  The stream's scratch holds the partial
+ * sums of dw. */
+int nnjit_norm_rotary_grad(const nnjit_rotary_table *rotary, int64_t tokens, int64_t heads, int64_t head_dim, const int32_t *positions,
+                           const void *weight, int64_t w_head, int w_dtype, float eps,
+                           const void *x, int64_t x_token, int64_t x_head, int x_dtype,
+                           const void *dy, int64_t dy_token, int64_t dy_head, int dy_dtype,
+                           void *dx, int64_t dx_token, int64_t dx_head, float *dw, void *stream);
+
+/* Attention of drafted tokens: row t, a new token of sequence b, sees the
+ * keys before b's new tokens, and new token i if bit i % 32 of mask[t * ld_mask +
+ * i / 32] is set, i < 32 mask_words (<= 2^20 words).  Bits of tokens that the
+ * sequence does not have do not count; any pattern is served, not only
+ * trees.  window > 0: of the keys before the new tokens only those at
+ * positions above positions[t] - window (positions[t] taken as the nearest of
+ * the positions that b's new tokens can have); the mask alone says which new tokens are
+ * seen.  positions may be NULL without a window.  Otherwise as nnjit_paged_attention. */
+int nnjit_tree_attention(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch, const uint32_t *mask, int64_t ld_mask,
+                         int64_t mask_words, const int32_t *positions, int64_t q_heads,
+                         const void *q, int64_t q_token, int64_t q_head, void *out, int64_t out_token, int64_t out_head,
+                         float scale, int64_t window, void *stream);
+
+/* The accepted path of each drafted tree moves to the places behind the cached
+ * keys: key and value of new token path[b * ld_path + i] of sequence b go to
+ * the place of its new token i, for i < accepted[b] (clamped to 0 ..
+ * path_len), all as if everything were read before anything is written.  batch is the
+ * drafted step's.  Entries below their own i or not new tokens of the sequence are
+ * skipped, as are places whose page is not in the cache.  Two sequences must not share the pages
+ * that new tokens lie in.  max_q and max_kv are not used. */
+int nnjit_kv_move(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch, const int32_t *path, int64_t ld_path,
+                  int64_t path_len, const int32_t *accepted, void *stream);
+
+/* Rules for rows of logits; any group of pointers may be NULL (its rule then
+ * does not apply).  All on the device. */
+typedef struct nnjit_logit_rules {
+    const int32_t *history;            /* [rows][ld_history]: the tokens so far, */
+    int64_t ld_history, history_len;   /* history_len columns at most, */
+    const int32_t *length;             /* [rows]: so many of them (clamped to 0 .. history_len; NULL: all); */
+    const int32_t *prompt;             /* [rows]: the first so many are the prompt's (NULL: none) */
+    const float *repetition, *presence, *frequency;   /* [rows] */
+    const int32_t *bias_token;         /* [rows][ld_bias], bias_len used; tokens outside the vocabulary are ignored */
+    const float *bias_value;           /* [rows][ld_bias] */
+    int64_t ld_bias, bias_len;
+    const uint32_t *mask;              /* [mask_rows][ld_mask], ceil(vocab / 32) words: bit set: allowed */
+    int64_t ld_mask, mask_rows;
+    const int32_t *mask_row;           /* [rows]: the row of mask, negative: none (NULL: row r has mask row r) */
+} nnjit_logit_rules;
+
+/* y = the logits x under the rules: with s = token v is in the row's history, c =
+ * how often it is there behind the prompt,
+ *   z = x; where s: z = x / repetition if x > 0, else x * repetition
+ *   z = z - frequency c - (presence if c > 0)
+ *   z = z + the bias of v (of several entries for one token the last one counts)
+ *   y = z where the mask allows v, -infinity elsewhere
+ * in fp32, rounded once to y's type; a mask that allows nothing leaves only
+ * -infinity.  Tokens of the history outside the vocabulary are ignored;
+ * a mask row at or behind mask_rows counts as the last.  y may be x (same stride and type); rows of y must not
+ * overlap.  rows < 2^20, vocab < 2^30. */
+int nnjit_adjust_logits(const nnjit_logit_rules *rules, int64_t rows, int64_t vocab, const void *x, int64_t ldx, int x_dtype,
+                        void *y, int64_t ldy, int y_dtype, void *stream);
+
 /* Message for the last error on this thread ("" if none).  The pointer stays
  * valid until the next nnjit_* call on the same thread. */
 const char *nnjit_last_error(void);

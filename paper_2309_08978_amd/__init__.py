@@ -13,7 +13,10 @@ anything else.
 point and raise ``NnjitError`` on a negative code.  ``rotary`` /
 ``kv_append`` / ``paged_attention`` do the same for the operators of a served
 decoder, with ``RotaryTable``, ``PagedCache`` and ``PagedBatch`` as the
-handles that a program keeps.  All of these run on the tensors' GPU, on
+handles that a program keeps, and ``paged_step`` / ``kv_append_slots`` /
+``norm_rotary`` / ``norm_rotary_grad`` / ``tree_attention`` / ``kv_move`` /
+``adjust_logits`` for a step of drafted tokens, with ``PagePool``, ``PagedStep``,
+``HeadNorm`` and ``LogitRules``.  All of these run on the tensors' GPU, on
 ``stream`` or, without one, on the stream that torch works on there; an output
 that they allocate belongs to that stream.
 """
@@ -40,7 +43,8 @@ EXPORTED = ["nnjit_matmul", "nnjit_batched_matmul", "nnjit_batched_matmul_noallo
             "nnjit_last_tune_stats", "nnjit_last_tune_stats_ex", "nnjit_last_tune_trace", "nnjit_cached_config", "nnjit_cached_ranked",
             "nnjit_set_online", "nnjit_online_status", "nnjit_cache_clear",
             "nnjit_cache_save", "nnjit_cache_load", "nnjit_stream_read", "nnjit_rotary_fill", "nnjit_rotary",
-            "nnjit_kv_append", "nnjit_paged_attention", "nnjit_last_error", "nnjit_version"]
+            "nnjit_kv_append", "nnjit_paged_attention", "nnjit_paged_step", "nnjit_kv_append_slots", "nnjit_norm_rotary",
+            "nnjit_norm_rotary_grad", "nnjit_tree_attention", "nnjit_kv_move", "nnjit_adjust_logits", "nnjit_last_error", "nnjit_version"]
 
 
 class NnjitError(RuntimeError):
@@ -88,6 +92,31 @@ class RotaryDesc(ctypes.Structure):
 class RotaryScaling(ctypes.Structure):
     """nnjit_rotary_scaling: RotaryScaling(kind, factor, original, fast, slow, magnitude)."""
     _fields_ = [("kind", ctypes.c_int)] + [(n, ctypes.c_double) for n in ("factor", "original", "fast", "slow", "magnitude")]
+
+
+class PagePoolDesc(ctypes.Structure):
+    _fields_ = [("free_pages", ctypes.c_void_p), ("capacity", ctypes.c_int64), ("count", ctypes.c_void_p),
+                ("count_out", ctypes.c_void_p)]
+
+
+class StepDesc(ctypes.Structure):
+    _fields_ = [("sequences", ctypes.c_int64), ("tokens", ctypes.c_int64)] + [
+        (n, ctypes.c_void_p) for n in ("held", "keep", "added", "parent", "page_table")] + [
+        (n, ctypes.c_int64) for n in ("ld_table", "table_pages", "page_size")] + [
+        (n, ctypes.c_void_p) for n in ("q_start", "kv_len", "positions", "slots", "mask")] + [
+        ("ld_mask", ctypes.c_int64), ("mask_words", ctypes.c_int64), ("status", ctypes.c_void_p)]
+
+
+class HeadNormDesc(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("q_head", ctypes.c_int64), ("k_head", ctypes.c_int64),
+                ("dtype", ctypes.c_int), ("eps", ctypes.c_float)]
+
+
+class LogitRulesDesc(ctypes.Structure):
+    _fields_ = [("history", ctypes.c_void_p), ("ld_history", ctypes.c_int64), ("history_len", ctypes.c_int64)] + [
+        (n, ctypes.c_void_p) for n in ("length", "prompt", "repetition", "presence", "frequency", "bias_token", "bias_value")] + [
+        ("ld_bias", ctypes.c_int64), ("bias_len", ctypes.c_int64), ("mask", ctypes.c_void_p), ("ld_mask", ctypes.c_int64),
+        ("mask_rows", ctypes.c_int64), ("mask_row", ctypes.c_void_p)]
 
 
 def mi355x_limits() -> DeviceLimits:
@@ -147,6 +176,14 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
             "nnjit_rotary": [vp, i64, i64, i64, vp, vp, i64, i64, ci, vp, i64, i64, ci, ci, vp],
             "nnjit_kv_append": [vp, vp, vp, vp, i64, i64, vp, i64, i64, i64, vp, i64, i64, vp, i64, i64, ci, vp],
             "nnjit_paged_attention": [vp, vp, i64, vp, i64, i64, vp, i64, i64, ctypes.c_float, ci, i64, vp],
+            "nnjit_paged_step": [vp, vp, vp],
+            "nnjit_kv_append_slots": [vp, i64, vp, vp, vp, vp, vp, i64, i64, vp, i64, i64, i64, vp, i64, i64, vp, i64, i64, ci, vp],
+            "nnjit_norm_rotary": [vp, i64, i64, i64, vp, vp, i64, ci, ctypes.c_float, vp, i64, i64, ci, vp, i64, i64, ci, vp],
+            "nnjit_norm_rotary_grad": [vp, i64, i64, i64, vp, vp, i64, ci, ctypes.c_float, vp, i64, i64, ci, vp, i64, i64, ci,
+                                       vp, i64, i64, vp, vp],
+            "nnjit_tree_attention": [vp, vp, vp, i64, i64, vp, i64, vp, i64, i64, vp, i64, i64, ctypes.c_float, i64, vp],
+            "nnjit_kv_move": [vp, vp, vp, i64, i64, vp, vp],
+            "nnjit_adjust_logits": [vp, i64, i64, vp, i64, ci, vp, i64, ci, vp],
             "nnjit_last_error": [],
             "nnjit_version": [],
         }
@@ -349,6 +386,44 @@ def nnjit_paged_attention(cache, batch, q_heads, q, q_token, q_head, out, out_to
                                         out_head, scale, causal, window, _stream(stream))
 
 
+def nnjit_paged_step(pool, step, stream=None) -> int:
+    return load().nnjit_paged_step(_desc(pool), _desc(step), _stream(stream))
+
+
+def nnjit_kv_append_slots(cache, tokens, slots, positions, rotary, norm, k, k_token, k_head, v, v_token, v_head, q_heads, q, q_token,
+                          q_head, q_out, qo_token, qo_head, src_dtype, stream=None) -> int:
+    return load().nnjit_kv_append_slots(_desc(cache), tokens, _ptr(slots), _ptr(positions), _desc(rotary), _desc(norm), _ptr(k),
+                                        k_token, k_head, _ptr(v), v_token, v_head, q_heads, _ptr(q), q_token, q_head, _ptr(q_out),
+                                        qo_token, qo_head, src_dtype, _stream(stream))
+
+
+def nnjit_norm_rotary(rotary, tokens, heads, head_dim, positions, weight, w_head, w_dtype, eps, x, x_token, x_head, x_dtype, y, y_token,
+                      y_head, y_dtype, stream=None) -> int:
+    return load().nnjit_norm_rotary(_desc(rotary), tokens, heads, head_dim, _ptr(positions), _ptr(weight), w_head, w_dtype, eps, _ptr(x),
+                                    x_token, x_head, x_dtype, _ptr(y), y_token, y_head, y_dtype, _stream(stream))
+
+
+def nnjit_norm_rotary_grad(rotary, tokens, heads, head_dim, positions, weight, w_head, w_dtype, eps, x, x_token, x_head, x_dtype, dy,
+                           dy_token, dy_head, dy_dtype, dx, dx_token, dx_head, dw, stream=None) -> int:
+    return load().nnjit_norm_rotary_grad(_desc(rotary), tokens, heads, head_dim, _ptr(positions), _ptr(weight), w_head, w_dtype, eps,
+                                         _ptr(x), x_token, x_head, x_dtype, _ptr(dy), dy_token, dy_head, dy_dtype, _ptr(dx), dx_token,
+                                         dx_head, _ptr(dw), _stream(stream))
+
+
+def nnjit_tree_attention(cache, batch, mask, ld_mask, mask_words, positions, q_heads, q, q_token, q_head, out, out_token, out_head,
+                         scale, window=0, stream=None) -> int:
+    return load().nnjit_tree_attention(_desc(cache), _desc(batch), _ptr(mask), ld_mask, mask_words, _ptr(positions), q_heads, _ptr(q),
+                                       q_token, q_head, _ptr(out), out_token, out_head, scale, window, _stream(stream))
+
+
+def nnjit_kv_move(cache, batch, path, ld_path, path_len, accepted, stream=None) -> int:
+    return load().nnjit_kv_move(_desc(cache), _desc(batch), _ptr(path), ld_path, path_len, _ptr(accepted), _stream(stream))
+
+
+def nnjit_adjust_logits(rules, rows, vocab, x, ldx, x_dtype, y, ldy, y_dtype, stream=None) -> int:
+    return load().nnjit_adjust_logits(_desc(rules), rows, vocab, _ptr(x), ldx, x_dtype, _ptr(y), ldy, y_dtype, _stream(stream))
+
+
 def nnjit_last_error() -> str:
     r = load().nnjit_last_error()
     return r.decode() if r else ""
@@ -360,7 +435,7 @@ def nnjit_version() -> int:
 
 # ------------------------------------------------------------ conveniences
 
-_NOT_PRODUCTS = ("attention_", "rotary.", "serving.")   # csrc/ sources that no product runs
+_NOT_PRODUCTS = ("attention_", "rotary.", "serving")   # csrc/ sources that no product runs
 
 
 def kernel_digest() -> str:
@@ -808,6 +883,365 @@ def paged_attention(q, cache: PagedCache, batch: PagedBatch, out=None, scale: Op
     so = _written_rows("out", out, batch.tokens, heads, dim, cache.dtype, dev)
     _launch((_lib or load()).nnjit_paged_attention, dev, stream, cache.address, batch.address, heads, q.data_ptr(), sq[0],
             sq[1], out.data_ptr(), so[0], so[1], dim ** -0.5 if scale is None else scale, 1 if causal else 0, window)
+    return out
+
+
+class PagePool:
+    """The free pages of a cache: ``free_pages`` int32 [capacity], a stack whose
+    first ``count`` (int32 [1]) ids are free; a step writes the new count to
+    ``count_out`` (default: ``count`` itself)."""
+
+    def __init__(self, free_pages, count, count_out=None):
+        _torch()
+        count_out = count if count_out is None else count_out
+        _int32("free_pages", free_pages, None)
+        _int32("count", count, 1)
+        _int32("count_out", count_out, 1)
+        _on_one_gpu(free_pages=free_pages, count=count, count_out=count_out)
+        self.free_pages, self.count, self.count_out, self.device_index = free_pages, count, count_out, count.get_device()
+        self.desc = PagePoolDesc(free_pages.data_ptr(), free_pages.shape[0], count.data_ptr(), count_out.data_ptr())
+        self.address = ctypes.addressof(self.desc)
+
+
+class PagedStep:
+    """The arrays of a step of up to ``tokens`` new rows, which ``paged_step``
+    fills: ``q_start``, ``kv_len``, ``positions``, ``slots``, ``status`` and, with
+    ``mask_words`` > 0 (32 drafted tokens of a sequence each, at most 32 words),
+    ``mask``.  ``page_table`` int32 [sequences, columns] is the program's; ``kv_len``
+    (default: an array of the step's own) may be the tensor that is passed as
+    ``held`` or ``keep``."""
+
+    def __init__(self, page_table, page_size: int, tokens: int, mask_words: int = 0, kv_len=None):
+        torch = _torch()
+        _int32("page_table", page_table, None, None)
+        _unit_dims("page_table", page_table)
+        sequences, columns = page_table.shape
+        if sequences > 1 and page_table.stride(0) < columns:
+            raise ValueError("rows of page_table overlap")
+        if tokens < 0 or not 0 <= mask_words <= 32:
+            raise ValueError(f"tokens must be >= 0 and mask_words 0 .. 32, got {tokens} and {mask_words}")
+        if kv_len is not None:
+            _int32("kv_len", kv_len, sequences)
+            _on_one_gpu(page_table=page_table, kv_len=kv_len)
+        else:
+            _on_one_gpu(page_table=page_table)
+        dev = page_table.device
+        self.page_table, self.page_size, self.tokens, self.mask_words = page_table, page_size, tokens, mask_words
+        self.sequences, self.device_index = sequences, page_table.get_device()
+        self.q_start = torch.zeros(sequences + 1, dtype=torch.int32, device=dev)
+        self.kv_len = torch.zeros(sequences, dtype=torch.int32, device=dev) if kv_len is None else kv_len
+        self.positions = torch.zeros(tokens, dtype=torch.int32, device=dev)
+        self.slots = torch.full((tokens,), -1, dtype=torch.int64, device=dev)
+        self.mask = torch.zeros((tokens, mask_words), dtype=torch.int32, device=dev) if mask_words else None
+        self.status = torch.zeros(4, dtype=torch.int32, device=dev)
+        self.desc = StepDesc(sequences, tokens, None, None, None, None, page_table.data_ptr(), max(page_table.stride(0), columns), columns,
+                             page_size, self.q_start.data_ptr(), self.kv_len.data_ptr(), self.positions.data_ptr(),
+                             self.slots.data_ptr(), self.mask.data_ptr() if mask_words else None, mask_words, mask_words,
+                             self.status.data_ptr())
+
+    def batch(self, max_q: Optional[int] = None, max_kv: Optional[int] = None) -> PagedBatch:
+        """The step as a PagedBatch over the same arrays."""
+        return PagedBatch(self.q_start, self.kv_len, self.page_table, self.tokens, max_q, max_kv)
+
+
+def _step_ints(name: str, t, count: int, device_index: int) -> int:
+    if t.shape == (count,) and t.dtype is _torch_module.int32 and t.get_device() == device_index and (count < 2 or t.stride(0) == 1):
+        return t.data_ptr()
+    _int32(name, t, count)
+    raise ValueError(f"{name} must be on one GPU with the step, got {t.device}")
+
+
+def paged_step(step: PagedStep, pool: PagePool, held, added, keep=None, parent=None, stream=None) -> PagedStep:
+    """Fills the step's arrays from lengths on the GPU (nnjit_paged_step):
+    sequence b holds the pages of held[b] tokens, of which keep[b] (default: all)
+    stay, and gets added[b] new ones (int32 [sequences] each).  ``parent`` int32
+    [tokens] makes the new tokens of a sequence a drafted tree.  Unless
+    ``step.status[0]`` is 0 afterwards nothing was changed and the step is empty."""
+    _torch()
+    n, dev = step.sequences, step.device_index
+    if pool.device_index != dev:
+        raise ValueError("pool and step must be on one GPU")
+    d = StepDesc.from_buffer_copy(step.desc)
+    d.held, d.added = _step_ints("held", held, n, dev), _step_ints("added", added, n, dev)
+    if keep is not None:
+        d.keep = _step_ints("keep", keep, n, dev)
+    if parent is not None:
+        if not step.mask_words:
+            raise ValueError("parent needs a step with mask_words")
+        d.parent = _step_ints("parent", parent, step.tokens, dev)
+    _launch((_lib or load()).nnjit_paged_step, dev, stream, pool.address, ctypes.addressof(d))
+    return step
+
+
+def _norm_weight(name: str, w, dtype):
+    """A norm's weight [dim] or [heads, dim] -> (heads or None, head stride)."""
+    if w.dtype not in _CODES or (dtype is not None and w.dtype != dtype):
+        raise TypeError(f"{name} must be float32 or float16 (both weights alike), got {w.dtype}")
+    if w.dim() not in (1, 2) or w.shape[-1] < 1:
+        raise ValueError(f"{name} must be [head_dim] or [heads, head_dim], got {tuple(w.shape)}")
+    _unit_dims(name, w)
+    if w.dim() == 1:
+        return None, 0
+    if w.shape[0] > 1 and w.stride(0) < w.shape[1]:
+        raise ValueError(f"rows of {name} overlap")
+    return int(w.shape[0]), max(int(w.stride(0)), int(w.shape[1]))
+
+
+class HeadNorm:
+    """Norms of query and key heads: ``q_weight`` and ``k_weight`` fp32 or fp16
+    [head_dim], or [heads, head_dim] for a weight a head; None: not normed."""
+
+    def __init__(self, q_weight=None, k_weight=None, eps: float = 1e-6):
+        _torch()
+        given = {n: w for n, w in (("q_weight", q_weight), ("k_weight", k_weight)) if w is not None}
+        if not given:
+            raise ValueError("q_weight, k_weight or both are needed")
+        if not 0.0 <= eps < float("inf"):
+            raise ValueError(f"eps must be finite and >= 0, got {eps}")
+        dtype = next(iter(given.values())).dtype
+        shapes = {n: _norm_weight(n, w, dtype) for n, w in given.items()}
+        if len({w.shape[-1] for w in given.values()}) != 1:
+            raise ValueError("q_weight and k_weight must be of one head_dim")
+        _on_one_gpu(**given)
+        one = next(iter(given.values()))
+        self.q_weight, self.k_weight, self.eps, self.head_dim, self.device_index = q_weight, k_weight, eps, int(one.shape[-1]), one.get_device()
+        self.q_heads, q_head = shapes.get("q_weight", (None, 0))
+        self.k_heads, k_head = shapes.get("k_weight", (None, 0))
+        self.desc = HeadNormDesc(_ptr(q_weight), _ptr(k_weight), q_head, k_head, _CODES[dtype], eps)
+        self.address = ctypes.addressof(self.desc)
+
+
+def kv_append_slots(cache: PagedCache, slots, k, v, positions=None, rotary: Optional[RotaryTable] = None, q=None, q_out=None,
+                    norm: Optional[HeadNorm] = None, stream=None):
+    """Writes k (normed, turned) and v [tokens, kv_heads, head_dim], fp32 or
+    fp16, to slots int64 [tokens] (page * page_size + slot; negative: the row is left
+    alone); norms and turns q [tokens, heads, head_dim] of the same type into
+    q_out (of the cache's type, allocated if None), which is returned (None without
+    q).  ``rotary`` turns by the angles of ``positions`` int32 [tokens]."""
+    torch = _torch()
+    dim, dev, dt = cache.head_dim, cache.device_index, k.dtype
+    if dt not in _CODES:
+        raise TypeError(f"unsupported dtype {dt}")
+    if slots.dim() != 1 or slots.dtype is not torch.int64 or slots.get_device() != dev or (slots.shape[0] > 1 and slots.stride(0) != 1):
+        raise ValueError(f"slots must be a contiguous int64 vector on the cache's GPU, got {slots.dtype} {tuple(slots.shape)}")
+    n = slots.shape[0]
+    pp = None
+    if rotary is not None:
+        if rotary.device_index != dev:
+            raise ValueError("cache and rotary must be on one GPU")
+        if positions is None:
+            raise ValueError("rotary needs positions")
+        pp = _step_ints("positions", positions, n, dev)
+    sk = _head_rows("k", k, n, cache.kv_heads, dim, dt, dev)
+    sv = _head_rows("v", v, n, cache.kv_heads, dim, dt, dev)
+    heads, sq, so, qp, op = 0, (0, 0), (0, 0), None, None
+    if q is not None:
+        heads = q.shape[1] if q.dim() == 3 else -1
+        sq = _head_rows("q", q, n, heads, dim, dt, dev)
+        if q_out is None:
+            q_out = _empty((n, heads, dim), cache.dtype, q.device, stream)
+        so = _written_rows("q_out", q_out, n, heads, dim, cache.dtype, dev)
+        qp, op = q.data_ptr(), q_out.data_ptr()
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if norm is not None:
+        if norm.device_index != dev or norm.head_dim != dim:
+            raise ValueError(f"norm weights must be on the cache's GPU and of its head_dim {dim}, got {norm.head_dim}")
+        if norm.k_heads not in (None, cache.kv_heads) or (heads and norm.q_heads not in (None, heads)):
+            raise ValueError(f"weights of {norm.q_heads} query and {norm.k_heads} key heads for {heads} and {cache.kv_heads}")
+    _launch((_lib or load()).nnjit_kv_append_slots, dev, stream, cache.address, n, slots.data_ptr(), pp,
+            None if rotary is None else rotary.address, None if norm is None else norm.address, k.data_ptr(), sk[0], sk[1],
+            v.data_ptr(), sv[0], sv[1], heads, qp, sq[0], sq[1], op, so[0], so[1], _CODES[dt])
+    return q_out
+
+
+def _norm_operands(x, weight, positions, table):
+    """(tokens, heads, dim, device, pointer of positions, table's address, weight's head stride) of norm_rotary and its gradient."""
+    shape = x.shape
+    if len(shape) != 3:
+        raise ValueError(f"x must be [tokens, heads, head_dim], got {tuple(shape)}")
+    tokens, heads, dim = shape
+    dev = x.get_device()
+    if not x.is_cuda or weight.get_device() != dev or (table is not None and table.device_index != dev):
+        raise ValueError("x, weight and table must be on one GPU")
+    if x.dtype not in _CODES:
+        raise TypeError(f"unsupported dtype {x.dtype}")
+    w_heads, w_head = _norm_weight("weight", weight, None)
+    if weight.shape[-1] != dim or w_heads not in (None, heads):
+        raise ValueError(f"weight must be [{dim}] or [{heads}, {dim}], got {tuple(weight.shape)}")
+    if table is None:
+        return tokens, heads, dim, dev, None, None, w_head
+    if positions is None:
+        raise ValueError("a table needs positions")
+    return tokens, heads, dim, dev, _step_ints("positions", positions, tokens, dev), table.address, w_head
+
+
+def norm_rotary(x, weight, positions=None, table: Optional[RotaryTable] = None, eps: float = 1e-6, out=None, stream=None):
+    """x [tokens, heads, head_dim] with every head scaled to a mean square of 1,
+    times weight ([head_dim] or [heads, head_dim]), turned by the angles of positions
+    (int32 [tokens]; without a table: not turned).  ``out`` (fp32 or fp16,
+    allocated like x if None) may be x."""
+    _torch()
+    tokens, heads, dim, dev, pp, tp, w_head = _norm_operands(x, weight, positions, table)
+    if out is None:
+        out = _empty((tokens, heads, dim), x.dtype, x.device, stream)
+    xd, yd = x.dtype, out.dtype
+    if yd not in _CODES:
+        raise TypeError(f"unsupported dtype {yd}")
+    sx = _head_rows("x", x, tokens, heads, dim, xd, dev)
+    sy = _written_rows("out", out, tokens, heads, dim, yd, dev)
+    _launch((_lib or load()).nnjit_norm_rotary, dev, stream, tp, tokens, heads, dim, pp, weight.data_ptr(), w_head, _CODES[weight.dtype],
+            eps, x.data_ptr(), sx[0], sx[1], _CODES[xd], out.data_ptr(), sy[0], sy[1], _CODES[yd])
+    return out
+
+
+def norm_rotary_grad(dy, x, weight, positions=None, table: Optional[RotaryTable] = None, eps: float = 1e-6, dx=None, dweight=None,
+                     stream=None):
+    """(dx, dweight) of norm_rotary from its result's gradient dy: dx of x's type
+    (allocated if None; may be dy or x), dweight fp32 of weight's shape."""
+    torch = _torch()
+    tokens, heads, dim, dev, pp, tp, w_head = _norm_operands(x, weight, positions, table)
+    if dx is None:
+        dx = _empty((tokens, heads, dim), x.dtype, x.device, stream)
+    if dweight is None:
+        dweight = _empty(tuple(weight.shape), torch.float32, x.device, stream)
+    if dy.dtype not in _CODES:
+        raise TypeError(f"unsupported dtype {dy.dtype}")
+    sx = _head_rows("x", x, tokens, heads, dim, x.dtype, dev)
+    sd = _head_rows("dy", dy, tokens, heads, dim, dy.dtype, dev)
+    so = _written_rows("dx", dx, tokens, heads, dim, x.dtype, dev)
+    if dweight.shape != weight.shape or dweight.dtype is not _F32 or not dweight.is_contiguous() or dweight.get_device() != dev:
+        raise ValueError(f"dweight must be contiguous float32 {tuple(weight.shape)} on x's GPU, got {dweight.dtype} {tuple(dweight.shape)}")
+    _launch((_lib or load()).nnjit_norm_rotary_grad, dev, stream, tp, tokens, heads, dim, pp, weight.data_ptr(), w_head,
+            _CODES[weight.dtype], eps, x.data_ptr(), sx[0], sx[1], _CODES[x.dtype], dy.data_ptr(), sd[0], sd[1], _CODES[dy.dtype],
+            dx.data_ptr(), so[0], so[1], dweight.data_ptr())
+    return dx, dweight
+
+
+def tree_attention(q, cache: PagedCache, batch: PagedBatch, mask, out=None, scale: Optional[float] = None, positions=None,
+                   window: int = 0, stream=None):
+    """Attention of drafted tokens q [tokens, heads, head_dim] over the keys
+    before their sequence's new ones and over those new ones that mask (int32
+    [tokens, words], bit i % 32 of word i / 32: new token i) names.  ``window`` > 0: of
+    the keys before the new ones the last only, those above positions (int32
+    [tokens]) - window.  Otherwise as ``paged_attention``."""
+    torch = _torch()
+    shape = q.shape
+    if len(shape) != 3:
+        raise ValueError(f"q must be [tokens, heads, head_dim], got {tuple(shape)}")
+    heads, dim, dev, n = shape[1], cache.head_dim, cache.device_index, batch.tokens
+    if batch.device_index != dev:
+        raise ValueError("cache and batch must be on one GPU")
+    if mask.dim() != 2 or mask.shape[0] != n or mask.shape[1] < 1 or mask.dtype is not torch.int32 or mask.get_device() != dev:
+        raise ValueError(f"mask must be int32 [{n}, words] on the cache's GPU, got {mask.dtype} {tuple(mask.shape)}")
+    words, ld = mask.shape[1], mask.stride(0)
+    if words > 1 and mask.stride(1) != 1:
+        raise ValueError("mask must have unit stride along the last dimension")
+    pp = None
+    if window > 0:
+        if positions is None:
+            raise ValueError("a window needs positions")
+        pp = _step_ints("positions", positions, n, dev)
+    sq = _head_rows("q", q, n, heads, dim, cache.dtype, dev)
+    if out is None:
+        out = _empty((n, heads, dim), cache.dtype, q.device, stream)
+    so = _written_rows("out", out, n, heads, dim, cache.dtype, dev)
+    _launch((_lib or load()).nnjit_tree_attention, dev, stream, cache.address, batch.address, mask.data_ptr(), ld, words, pp, heads,
+            q.data_ptr(), sq[0], sq[1], out.data_ptr(), so[0], so[1], dim ** -0.5 if scale is None else scale, window)
+    return out
+
+
+def kv_move(cache: PagedCache, batch: PagedBatch, path, accepted, stream=None) -> None:
+    """Keys and values of the accepted nodes of each drafted tree go to the
+    places behind the cached ones: new token path[b, i] of sequence b to the place
+    of its new token i, i < accepted[b] (path int32 [sequences, nodes], accepted int32
+    [sequences]), as if all were read before any is written."""
+    _torch()
+    dev, sequences = cache.device_index, batch.kv_len.shape[0]
+    if batch.device_index != dev:
+        raise ValueError("cache and batch must be on one GPU")
+    _int32("path", path, sequences, None)
+    if path.get_device() != dev or (path.shape[1] > 1 and path.stride(1) != 1) or path.stride(0) < 0:
+        raise ValueError(f"path must be on the cache's GPU with unit stride along the last dimension, got {path.device} {tuple(path.stride())}")
+    _launch((_lib or load()).nnjit_kv_move, dev, stream, cache.address, batch.address, path.data_ptr(),
+            max(path.stride(0), path.shape[1]), path.shape[1], _step_ints("accepted", accepted, sequences, dev))
+
+
+class LogitRules:
+    """What adjust_logits applies to ``rows`` rows of logits (nnjit_logit_rules);
+    each is optional: ``history`` int32 [rows, columns] with ``length`` and
+    ``prompt`` int32 [rows] (its tokens, and how many of them are the prompt's);
+    ``repetition``, ``presence``, ``frequency`` fp32 [rows]; ``bias_token`` int32 and
+    ``bias_value`` fp32 [rows, entries] (tokens outside the vocabulary, such as -1, are ignored);
+    ``mask`` int32 [grammars, words], a bit a token, and ``mask_row`` int32 [rows], the
+    grammar of every row, negative: none (without it row r has mask row r)."""
+
+    def __init__(self, history=None, length=None, prompt=None, repetition=None, presence=None, frequency=None, bias_token=None,
+                 bias_value=None, mask=None, mask_row=None):
+        torch = _torch()
+        given = {n: t for n, t in (("history", history), ("length", length), ("prompt", prompt), ("repetition", repetition),
+                                   ("presence", presence), ("frequency", frequency), ("bias_token", bias_token),
+                                   ("bias_value", bias_value), ("mask", mask), ("mask_row", mask_row)) if t is not None}
+        if not given:
+            raise ValueError("no rule is given")
+        if (bias_token is None) != (bias_value is None):
+            raise ValueError("bias_token and bias_value go together")
+        if history is None and any(n in given for n in ("length", "prompt", "repetition", "presence", "frequency")):
+            raise ValueError("lengths and penalties need a history")
+        if mask is None and mask_row is not None:
+            raise ValueError("mask_row without mask")
+        rows = {n: int(t.shape[0]) for n, t in given.items() if t.dim() and (n != "mask" or mask_row is None)}
+        if len(set(rows.values())) != 1:
+            raise ValueError(f"the rules are for different numbers of rows: {rows}")
+        self.rows = next(iter(rows.values()))
+        for n, t in given.items():
+            want = torch.float32 if n in ("repetition", "presence", "frequency", "bias_value") else torch.int32
+            dims = 2 if n in ("history", "bias_token", "bias_value", "mask") else 1
+            if t.dtype != want or t.dim() != dims:
+                raise ValueError(f"{n} must be {want} with {dims} dimensions, got {t.dtype} {tuple(t.shape)}")
+            if t.shape[-1] > 1 and t.stride(-1) != 1:
+                raise ValueError(f"{n} must have unit stride along the last dimension")
+        if bias_token is not None and (bias_token.shape != bias_value.shape or (self.rows > 1 and bias_token.stride(0) != bias_value.stride(0))):
+            raise ValueError("bias_token and bias_value must have the same shape and strides")
+        if mask is not None and mask.shape[0] < 1:
+            raise ValueError("mask has no row")
+        _on_one_gpu(**given)
+        self.given, self.device_index = given, next(iter(given.values())).get_device()
+        self.words = None if mask is None else int(mask.shape[1])
+        ptr = {n: t.data_ptr() for n, t in given.items()}
+        ld = {n: int(t.stride(0)) for n, t in given.items() if t.dim() == 2}
+        self.desc = LogitRulesDesc(ptr.get("history"), ld.get("history", 0), 0 if history is None else history.shape[1],
+                                   ptr.get("length"), ptr.get("prompt"), ptr.get("repetition"), ptr.get("presence"), ptr.get("frequency"),
+                                   ptr.get("bias_token"), ptr.get("bias_value"), ld.get("bias_token", 0),
+                                   0 if bias_token is None else bias_token.shape[1], ptr.get("mask"), ld.get("mask", 0),
+                                   0 if mask is None else mask.shape[0], ptr.get("mask_row"))
+        self.address = ctypes.addressof(self.desc)
+
+
+def adjust_logits(logits, rules: LogitRules, out=None, stream=None):
+    """logits [rows, vocab], fp32 or fp16, under the rules: penalties for tokens
+    that are there already, biases, -infinity where a mask has no bit.  ``out`` (fp32 or
+    fp16, allocated like logits if None) may be logits."""
+    _torch()
+    if logits.dim() != 2:
+        raise ValueError(f"logits must be [rows, vocab], got {tuple(logits.shape)}")
+    rows, vocab = logits.shape
+    dev = rules.device_index
+    if out is None:
+        out = _empty((rows, vocab), logits.dtype, logits.device, stream)
+    if rules.rows != rows:
+        raise ValueError(f"{rows} rows of logits, rules for {rules.rows}")
+    if rules.words is not None and rules.words < -(-vocab // 32):
+        raise ValueError(f"mask rows of {rules.words} words for {vocab} tokens")
+    for name, t in (("logits", logits), ("out", out)):
+        if t.dtype not in _CODES:
+            raise TypeError(f"unsupported dtype {t.dtype}")
+        if t.shape != logits.shape or (vocab > 1 and t.stride(1) != 1) or t.get_device() != dev:
+            raise ValueError(f"{name} must be [{rows}, {vocab}] with unit stride along the last dimension on the rules' GPU, got {tuple(t.shape)} on {t.device}")
+    if rows > 1 and out.stride(0) < vocab:
+        raise ValueError("rows of out overlap")
+    _launch((_lib or load()).nnjit_adjust_logits, dev, stream, rules.address, rows, vocab, logits.data_ptr(), logits.stride(0),
+            _CODES[logits.dtype], out.data_ptr(), out.stride(0), _CODES[out.dtype])
     return out
 
 

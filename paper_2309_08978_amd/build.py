@@ -26,7 +26,9 @@ OBJDIR = os.path.join(HERE, "_build")
 ARCH = os.environ.get("NNJIT_ARCH", "gfx950")
 
 SOURCES = ["gemm_f32.hip", "gemm_staged.hip", "gemm_f16.hip", "gemm_row.hip", "gemv.hip", "gemv_q4.hip", "noalloc.hip", "rotary.hip", "attention_rows.hip",
-           "attention_tiles_f16.hip", "attention_tiles_f32.hip", "serving.cpp", "space.cpp", "runtime.cpp"]
+           "attention_tiles_f16.hip", "attention_tiles_f32.hip", "attention_rows_tree.hip", "attention_tiles_tree_f16.hip",
+           "attention_tiles_tree_f32.hip", "serving_step.hip", "serving_norm.hip", "serving_move.hip", "serving_logits.hip",
+           "serving.cpp", "serving_drafts.cpp", "space.cpp", "runtime.cpp"]
 
 COMMON = ["-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
           "-I", CSRC, "-I", os.path.join(ROOT, "include")]

@@ -19,6 +19,7 @@ struct RowTile {
     int past;             // position of its first new token (below zero: it and maybe others see no key)
     int keys;             // keys in the cache
     int r0, rows;         // first row of the tile, rows in it (<= 0: nothing to do)
+    int cached;           // drafted trees: keys before the new tokens
     const int *table;     // the sequence's page table row
 
     // (64 bits: a window of any size behind a position below zero)
@@ -30,6 +31,41 @@ struct RowTile {
     __device__ __forceinline__ int end_key(const AttentionParams &p, int r) const
     {
         return p.causal ? min(keys, max(past + p.group_div.quot(r) + 1, 0)) : keys;
+    }
+
+    // A drafted tree's row at depth i of its tree: of the cached keys it sees those from here on.
+    __device__ __forceinline__ int first_cached(const AttentionParams &p, int depth) const
+    {
+        if (p.window == 0) return 0;
+        return (int)min(max((long long)past + depth - p.window + 1, 0ll), (long long)cached);
+    }
+    // (a position outside the new tokens' counts as the nearest: no row sees less than the last or more than the first)
+    __device__ __forceinline__ int first_cached_of(const AttentionParams &p, int token) const
+    {
+        if (p.window == 0) return 0;
+        const long long depth = (long long)p.positions[token] - past;
+        return first_cached(p, (int)min(max(depth, 0ll), (long long)new_tokens - 1));
+    }
+    // Bits of a drafted row (token t of q) for the four keys from `key` on: those of them that are new tokens it sees.
+    __device__ __forceinline__ unsigned drafted4(const AttentionParams &p, int token, int key) const
+    {
+        const int i = key - max(past, -(1 << 30));        // (keys are below 2^30, words 2^20 at most)
+        if (i <= -4 || i >= 32 * p.mask_words) return 0;
+        const unsigned *row = p.mask + (long long)token * p.ld_mask;
+        const int w = max(i, 0) >> 5;
+        const unsigned long long two = row[w] | (unsigned long long)(w + 1 < p.mask_words ? row[w + 1] : 0u) << 32;
+        return (unsigned)(i >= 0 ? two >> (i & 31) : two << -i) & 15u;
+    }
+    // Whether a drafted row sees any of the keys from .. to - 1.
+    __device__ __forceinline__ bool drafted_any(const AttentionParams &p, int token, int from, int to) const
+    {
+        if (max(from, first_cached_of(p, token)) < min(to, cached)) return true;
+        const int end = (int)min((long long)min(to, keys), past + 32ll * p.mask_words);
+        for (int key = max(from, cached); key < end; key += 4) {
+            const unsigned ahead = end - key;
+            if (drafted4(p, token, key) & (ahead >= 4 ? 15u : (1u << ahead) - 1u)) return true;
+        }
+        return false;
     }
 };
 
@@ -48,6 +84,7 @@ __device__ __forceinline__ RowTile row_tile(const AttentionParams &p, int seq, i
     t.past = (int)max((long long)b.kv_len[seq] - ((long long)b.q_start[seq + 1] - t.q0), -0x7fffffffll);
     t.r0 = tile * tile_rows;
     t.rows = min((long long)tile_rows, (long long)t.new_tokens * p.group - t.r0);
+    t.cached = min(max(t.past, 0), t.keys);
     t.table = b.page_table + (long long)seq * b.ld_table;
     return t;
 }

@@ -1,7 +1,7 @@
 // Attention over a paged cache for many rows (prompts): tiles of 32 rows a
 // wave, keys and values shared through LDS.
 //
-// The mathematics is that of attention_rows.hip: one pass over the keys with a
+// The mathematics is that of attention_rows.h: one pass over the keys with a
 // running reference and sum; here the matrix cores bound it.  A workgroup has WR x WK
 // waves: WR row groups of 32 rows, WK groups that take different keys of a
 // step (joined through LDS at the end).  A step takes BN = 32 KB WK keys: K and
@@ -35,7 +35,7 @@
 // to 2^-35 of it).  The sum that divides takes them unrounded; rounding is
 // unbiased, and its share of the result's error is that of the result's own
 // rounding to fp16 (2.5 .. 2.9e-4 in all, against 2.1e-4 with exact weights).  (Two
-// parts, as in attention_rows.hip, would be half as many products again where
+// parts, as in attention_rows.h, would be half as many products again where
 // products are what bounds.)
 //
 // Why 32 rows a wave: K and V of a step are read from LDS once per 32 rows, half
@@ -118,14 +118,15 @@ constexpr int kSlack = 5, kLift = 10;
 // not finite among 2048 keys of 32 heads of 128 thus takes 512 rows, of which a
 // wave's 32 are taken anew, from 0.05 to 24 ms (fp16, a key that some of the rows
 // do not see) or from 0.14 to 12 ms (fp32); one such query to 0.06 and 0.8 ms.
-template <typename T, int DP>
+template <typename T, int DP, bool TREE>
 __device__ __forceinline__ void redo_row(const AttentionParams &p, const RowTile &t, int head, int split, int r, int k0, int k1, int lane)
 {
     constexpr int E = (DP + 63) / 64;
     constexpr bool HALF = sizeof(T) == 2;
-    const int lo = max(t.first_key(p, r), k0), hi = min(t.end_key(p, r), k1);
     const int token = t.q0 + p.group_div.quot(r);
+    const int lo = max(TREE ? t.first_cached_of(p, token) : t.first_key(p, r), k0), hi = min(TREE ? t.keys : t.end_key(p, r), k1);
     const int q_head = head * p.group + r - p.group_div.quot(r) * p.group;
+    bool sees = !TREE && hi > lo;
     const T *q = (const T *)p.q.p + (long long)token * p.q.tok + (long long)q_head * p.q.head;
     float qv[E], o[E], ref = -__builtin_inff(), l = 0.f;
     for (int e = 0; e < E; ++e) {
@@ -135,6 +136,10 @@ __device__ __forceinline__ void redo_row(const AttentionParams &p, const RowTile
     }
 #pragma unroll 1
     for (int key = lo; key < hi; ++key) {
+        if constexpr (TREE) {
+            if (key >= t.cached && !(t.drafted4(p, token, key) & 1)) continue;
+            sees = true;
+        }
         const int pi = p.pool.page_size.quot(key), slot = key - pi * (int)p.pool.page_size.d;
         const int page = safe_page(p, t.table[pi]);
         const T *k = (const T *)p.pool.k + (long long)head * p.pool.k_head + page_offset(page, p.pool.k_page, slot, p.pool.k_tok);
@@ -155,12 +160,12 @@ __device__ __forceinline__ void redo_row(const AttentionParams &p, const RowTile
     for (int e = 0; e < E; ++e) {
         const int d = lane + 64 * e;
         if (p.splits == 1) {
-            if (d < p.dim) dst[d] = (T)(hi > lo ? o[e] / l : 0.f);
+            if (d < p.dim) dst[d] = (T)(sees ? o[e] / l : 0.f);
         } else {
             if (d < p.part_dim) p.part[at * p.part_dim + d] = o[e];
         }
     }
-    if (p.splits > 1 && lane == 0) store_stat(p, at, ref, l, hi > lo);
+    if (p.splits > 1 && lane == 0) store_stat(p, at, ref, l, sees);
 }
 
 // Bytes of a row in LDS, and the waves a SIMD is to hold: two, of two
@@ -178,7 +183,9 @@ constexpr int lds_bytes() { return (HOW >= SPLIT ? 6 : 2 * stages<T, DP, HOW>())
 template <typename T, int DP, int HOW, int BLOCKS>
 constexpr int waves_per_simd() { return DP <= 128 && lds_bytes<T, DP, HOW, BLOCKS>() <= 80 * 1024 ? 2 : 1; }
 
-template <typename T, int DP, int HOW, int WR, int WK, int KB>
+// TREE: drafted trees: a row sees its sequence's cached keys (with a window from
+// first_cached() on) and the new tokens that its mask names.
+template <typename T, int DP, int HOW, int WR, int WK, int KB, bool TREE>
 __global__ void __launch_bounds__(WR * WK * 64, (waves_per_simd<T, DP, HOW, KB * WK>()))
 attention_tiles_kernel(AttentionParams p)
 {
@@ -228,20 +235,21 @@ attention_tiles_kernel(AttentionParams p)
     mark_left_out<NW * 64>(p, t, head, tile, split, 32 * WR);
 
     const int r_last = t.r0 + t.rows - 1;
-    const int lo_min = t.first_key(p, t.r0), hi_max = t.end_key(p, r_last);
+    const int lo_min = TREE ? t.first_cached(p, 0) : t.first_key(p, t.r0), hi_max = TREE ? t.keys : t.end_key(p, r_last);
     const long long begin = (lo_min & ~31) + (long long)split * p.split_keys;
     const int k0 = (int)min(begin, (long long)hi_max);
-    const int k1 = (int)min(begin + p.split_keys, (long long)hi_max);
+    // (trees: the last split goes to the end, for sequences of more new tokens than max_q)
+    const int k1 = TREE && split == p.splits - 1 ? hi_max : (int)min(begin + p.split_keys, (long long)hi_max);
     const int first = max(lo_min, k0);                    // keys first .. k1 - 1 are seen by a row of the tile
 
     // the wave's rows, and this lane's (rows past the end repeat the last one)
     const int w0 = min(t.r0 + 32 * wr, r_last), w1 = min(t.r0 + 32 * wr + 31, r_last);
     const bool wave_rows = t.r0 + 32 * wr <= r_last;
-    const int lo_w = max(t.first_key(p, w0), k0), hi_w = min(t.end_key(p, w1), k1);
+    const int lo_w = max(TREE ? lo_min : t.first_key(p, w0), k0), hi_w = min(TREE ? t.keys : t.end_key(p, w1), k1);
     const int r = min(t.r0 + 32 * wr + n, r_last);
     const int token = t.q0 + p.group_div.quot(r);
     const int q_head = head * p.group + r - p.group_div.quot(r) * p.group;
-    const int lo = max(t.first_key(p, r), k0), hi = min(t.end_key(p, r), k1);
+    const int lo = max(TREE ? t.first_cached_of(p, token) : t.first_key(p, r), k0), hi = min(TREE ? t.cached : t.end_key(p, r), k1);
     const int dim = p.dim;
 
     chunk q[PARTS ? 1 : QS];
@@ -509,12 +517,19 @@ attention_tiles_kernel(AttentionParams p)
         }
         if constexpr (!WHOLE) {
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
+            for (int kb = 0; kb < KB; ++kb) {
+                [[maybe_unused]] unsigned drafted = 0;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int key = key0 + 32 * kb + 8 * (i / 4) + 4 * h + i % 4;
-                    x[kb][i] = key >= lo && key < hi ? x[kb][i] : -__builtin_inff();
+                    bool see = key >= lo && key < hi;
+                    if constexpr (TREE) {
+                        if (i % 4 == 0) drafted = t.drafted4(p, token, key);
+                        see |= key >= t.cached && key < k1 && (drafted >> i % 4 & 1);
+                    }
+                    x[kb][i] = see ? x[kb][i] : -__builtin_inff();
                 }
+            }
         }
         float top = x[0][0];
 #pragma unroll
@@ -548,7 +563,7 @@ attention_tiles_kernel(AttentionParams p)
     // steps whole_from .. whole_to - 1: every row of the workgroup sees every key.
     // The others, a few at either end, run a loop of their own: one loop with
     // both kinds of step in it would hold the sums in two sets of registers.
-    const int lo_max = t.first_key(p, r_last), hi_min = min(t.end_key(p, t.r0), k1);
+    const int lo_max = TREE ? t.first_cached(p, t.new_tokens - 1) : t.first_key(p, r_last), hi_min = min(TREE ? t.cached : t.end_key(p, t.r0), k1);
     const int whole_from = min(max((lo_max - start + BN - 1) / BN, 0), steps);
     const int whole_to = hi_min > start ? max((hi_min - start) / BN, whole_from) : whole_from;
     Ids ids;
@@ -661,12 +676,12 @@ attention_tiles_kernel(AttentionParams p)
         const unsigned rows = (unsigned)(lanes | lanes >> 32);
 #pragma unroll 1
         for (int i = 0; i < 32 && t.r0 + 32 * wr + i <= r_last; ++i)
-            if (rows >> i & 1) redo_row<T, DP>(p, t, head, split, t.r0 + 32 * wr + i, k0, k1, lane);
+            if (rows >> i & 1) redo_row<T, DP, TREE>(p, t, head, split, t.r0 + 32 * wr + i, k0, k1, lane);
         if (rows >> n & 1) return;
     }
     if (t.r0 + 32 * wr + n > r_last) return;
     // block g VW + e holds dims 32 VW g + VW j + e, j = 8 (i / 4) + 4 h + i % 4: runs of 4 VW dims
-    const bool sees = hi > lo;
+    const bool sees = TREE ? t.drafted_any(p, token, k0, k1) : hi > lo;
     const float inv = p.splits == 1 ? 1.f / l : 1.f;
     const long long at = ((long long)split * p.batch.tokens + token) * p.q_heads + q_head;
     T *dst = (T *)p.o.p + (long long)token * p.o.tok + (long long)q_head * p.o.head;
@@ -699,26 +714,26 @@ attention_tiles_kernel(AttentionParams p)
     if (p.splits > 1 && h == 0) store_stat(p, at, ref, l, sees);
 }
 
-template <typename T, int DP, int HOW, int KB>
+template <typename T, int DP, int HOW, int KB, bool TREE>
 hipError_t launch_shape(const AttentionParams &p, int tile_rows, int grid, hipStream_t stream)
 {
     if (tile_rows == 128) {
-        attention_tiles_kernel<T, DP, HOW, 4, 1, KB><<<grid, 256, 0, stream>>>(p);
+        attention_tiles_kernel<T, DP, HOW, 4, 1, KB, TREE><<<grid, 256, 0, stream>>>(p);
     } else if constexpr (DP <= 128) {
-        attention_tiles_kernel<T, DP, HOW, 2, 2, 1><<<grid, 256, 0, stream>>>(p);
+        attention_tiles_kernel<T, DP, HOW, 2, 2, 1, TREE><<<grid, 256, 0, stream>>>(p);
     } else {
         return hipErrorInvalidValue;   // the plan asks for none
     }
     return hipGetLastError();
 }
 
-template <typename T, int DP, int KB>
+template <typename T, int DP, int KB, bool TREE>
 hipError_t launch_chunks(const AttentionParams &p, int tile_rows, int grid, hipStream_t stream)
 {
     // lane offsets of PAGED16 are 32 bits: at most 8 keys and a row
     const bool near = p.pool.k_tok < (1u << 24) && p.pool.v_tok < (1u << 24);
-    return p.dim == DP && p.pool.page_size.d % 16 == 0 && near ? launch_shape<T, DP, PAGED16, KB>(p, tile_rows, grid, stream)
-                                                               : launch_shape<T, DP, CHUNKS, KB>(p, tile_rows, grid, stream);
+    return p.dim == DP && p.pool.page_size.d % 16 == 0 && near ? launch_shape<T, DP, PAGED16, KB, TREE>(p, tile_rows, grid, stream)
+                                                               : launch_shape<T, DP, CHUNKS, KB, TREE>(p, tile_rows, grid, stream);
 }
 
 }  // namespace

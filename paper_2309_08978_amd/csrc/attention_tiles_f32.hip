@@ -8,13 +8,13 @@ namespace nnjit {
 hipError_t launch_attention_tiles_f32(const AttentionParams &p, int tile_rows, bool vec, int grid, hipStream_t stream)
 {
     if (!vec) {
-        return p.dim <= 128 ? launch_shape<float, 128, SPLIT_ANY, 1>(p, tile_rows, grid, stream)
-                            : launch_shape<float, 256, ANY, 1>(p, tile_rows, grid, stream);
+        return p.dim <= 128 ? launch_shape<float, 128, SPLIT_ANY, 1, false>(p, tile_rows, grid, stream)
+                            : launch_shape<float, 256, ANY, 1, false>(p, tile_rows, grid, stream);
     }
-    if (p.dim <= 64) return launch_shape<float, 64, SPLIT, 1>(p, tile_rows, grid, stream);
-    if (p.dim <= 96) return launch_shape<float, 96, SPLIT, 1>(p, tile_rows, grid, stream);
-    if (p.dim <= 128) return launch_shape<float, 128, SPLIT, 1>(p, tile_rows, grid, stream);
-    return launch_chunks<float, 256, 1>(p, tile_rows, grid, stream);
+    if (p.dim <= 64) return launch_shape<float, 64, SPLIT, 1, false>(p, tile_rows, grid, stream);
+    if (p.dim <= 96) return launch_shape<float, 96, SPLIT, 1, false>(p, tile_rows, grid, stream);
+    if (p.dim <= 128) return launch_shape<float, 128, SPLIT, 1, false>(p, tile_rows, grid, stream);
+    return launch_chunks<float, 256, 1, false>(p, tile_rows, grid, stream);
 }
 
 }  // namespace nnjit

@@ -1,126 +1,9 @@
 // Entry points of the serving operators (include/nnjit.h): argument checks,
 // parameters of the launches.
-#include <algorithm>
-#include <cmath>
-#include <cstdint>
-#include <limits>
-
-#include "nnjit.h"
-#include "serving.h"
+#include "serving_checks.h"
 
 namespace nnjit {
 namespace {
-
-constexpr int64_t kMaxInt = 0x7fffffff;
-constexpr int64_t kMaxHeads = (int64_t)1 << 30;   // of a row that is turned: steps from head to head stay inside 32 bits
-constexpr int64_t kMaxGroups = 0xffffff;          // workgroups of 256 threads: a launch holds below 2^32 threads
-
-bool is_dtype(int d) { return d == NNJIT_F32 || d == NNJIT_F16; }
-int64_t bytes_of(int dtype) { return dtype == NNJIT_F32 ? 4 : 2; }
-
-// rows whose pointer and strides are multiples of `elems` elements
-bool in_units(const void *p, int64_t tok, int64_t head, int64_t elems, int dtype) {
-    return (uintptr_t)p % (uintptr_t)(elems * bytes_of(dtype)) == 0 && tok % elems == 0 && head % elems == 0;
-}
-
-int check_rows(const char *name, const void *p, int64_t rows, int64_t heads, int64_t tok, int64_t head) {
-    if (rows > 0 && heads > 0 && !p) return runtime_fail(NNJIT_EINVAL, "%s is NULL", name);
-    if (tok < 0 || head < 0) return runtime_fail(NNJIT_EINVAL, "negative stride of %s", name);
-    return NNJIT_OK;
-}
-
-// rows that are written: none may overlap
-int check_written(const char *name, const void *p, int64_t rows, int64_t heads, int64_t dim, int64_t tok, int64_t head) {
-    const int rc = check_rows(name, p, rows, heads, tok, head);
-    if (rc != NNJIT_OK || heads == 0 || rows == 0) return rc;
-    if (heads > 1 && head < dim) return runtime_fail(NNJIT_EINVAL, "head stride %lld of %s < %lld dims", (long long)head, name, (long long)dim);
-    const int64_t least = heads > 1 && tok >= head ? (heads - 1) * head + dim : dim;
-    const bool heads_outside = heads > 1 && tok < head;   // heads major, tokens within
-    if (rows > 1 && (tok < least || (heads_outside && head < (rows - 1) * tok + dim)))
-        return runtime_fail(NNJIT_EINVAL, "rows of %s overlap (token stride %lld, head stride %lld)", name, (long long)tok, (long long)head);
-    return NNJIT_OK;
-}
-
-int check_dim(int64_t dim) {
-    if (dim < 1 || dim > kMaxHeadDim) return runtime_fail(NNJIT_EINVAL, "head_dim=%lld out of [1, %d]", (long long)dim, kMaxHeadDim);
-    return NNJIT_OK;
-}
-
-int check_rotary(const nnjit_rotary_table *r, int64_t dim) {
-    if (!r->table) return runtime_fail(NNJIT_EINVAL, "the rotary table is NULL");
-    if (r->positions < 1 || r->positions > kMaxInt) return runtime_fail(NNJIT_EINVAL, "rotary positions=%lld out of [1, 2^31)", (long long)r->positions);
-    if (r->rotary_dim < 2 || r->rotary_dim % 2 || r->rotary_dim > dim)
-        return runtime_fail(NNJIT_EINVAL, "rotary_dim=%lld must be even and in [2, head_dim=%lld]", (long long)r->rotary_dim, (long long)dim);
-    if (r->layout != NNJIT_ROTARY_HALF && r->layout != NNJIT_ROTARY_INTERLEAVED)
-        return runtime_fail(NNJIT_EINVAL, "unknown rotary layout %d", r->layout);
-    return NNJIT_OK;
-}
-
-int check_cache(const nnjit_paged_kv *c) {
-    if (!c) return runtime_fail(NNJIT_EINVAL, "the cache is NULL");
-    if (!is_dtype(c->dtype)) return runtime_fail(NNJIT_EDTYPE, "unsupported cache dtype %d", c->dtype);
-    const int rc = check_dim(c->head_dim);
-    if (rc != NNJIT_OK) return rc;
-    if (c->pages < 1 || c->pages > kMaxInt) return runtime_fail(NNJIT_EINVAL, "pages=%lld out of [1, 2^31)", (long long)c->pages);
-    if (c->page_size < 1 || c->page_size > kMaxKeys) return runtime_fail(NNJIT_EINVAL, "page_size=%lld out of [1, 2^30]", (long long)c->page_size);
-    if (c->kv_heads < 1 || c->kv_heads > kMaxInt) return runtime_fail(NNJIT_EINVAL, "kv_heads=%lld out of [1, 2^31)", (long long)c->kv_heads);
-    if (!c->k || !c->v) return runtime_fail(NNJIT_EINVAL, "the cache's K or V is NULL");
-    if (c->k_page < 0 || c->k_token < 0 || c->k_head < 0 || c->v_page < 0 || c->v_token < 0 || c->v_head < 0)
-        return runtime_fail(NNJIT_EINVAL, "negative stride of the cache");
-    if (std::max({c->k_page, c->k_token, c->v_page, c->v_token}) > (int64_t)0xffffffff)
-        return runtime_fail(NNJIT_EINVAL, "page and token strides of the cache must be below 2^32 elements");
-    return NNJIT_OK;
-}
-
-// slots that are written: none may overlap
-int check_slots(const char *name, const nnjit_paged_kv *c, int64_t page, int64_t token, int64_t head) {
-    struct { int64_t stride, count; } axis[3] = {{page, c->pages}, {token, c->page_size}, {head, c->kv_heads}};
-    std::sort(axis, axis + 3, [](const auto &a, const auto &b) { return a.stride < b.stride; });
-    double taken = (double)c->head_dim;                    // elements from the first to the last, axis by axis
-    for (const auto &a : axis) {
-        if (a.count == 1) continue;
-        if ((double)a.stride < taken) return runtime_fail(NNJIT_EINVAL, "slots of the cache's %s overlap (stride %lld)", name, (long long)a.stride);
-        taken += (double)a.stride * (double)(a.count - 1);
-    }
-    return NNJIT_OK;
-}
-
-int check_batch(const nnjit_paged_batch *b) {
-    if (!b) return runtime_fail(NNJIT_EINVAL, "the batch is NULL");
-    if (b->sequences < 0 || b->sequences > kMaxInt || b->tokens < 0 || b->tokens > kMaxInt)
-        return runtime_fail(NNJIT_EINVAL, "sequences=%lld, tokens=%lld out of [0, 2^31)", (long long)b->sequences, (long long)b->tokens);
-    if (b->table_pages < 0 || b->table_pages > kMaxInt) return runtime_fail(NNJIT_EINVAL, "table_pages=%lld out of [0, 2^31)", (long long)b->table_pages);
-    if (b->ld_table < b->table_pages) return runtime_fail(NNJIT_EINVAL, "ld_table=%lld < %lld page table columns", (long long)b->ld_table, (long long)b->table_pages);
-    if (b->sequences > 0 && b->tokens > 0) {
-        if (!b->q_start || !b->kv_len) return runtime_fail(NNJIT_EINVAL, "q_start or kv_len is NULL");
-        if (b->table_pages > 0 && !b->page_table) return runtime_fail(NNJIT_EINVAL, "page_table is NULL");
-    }
-    return NNJIT_OK;
-}
-
-PagePool pool_of(const nnjit_paged_kv *c) {
-    PagePool p;
-    p.k = c->k;
-    p.v = c->v;
-    p.k_page = (unsigned)c->k_page;
-    p.k_tok = (unsigned)c->k_token;
-    p.k_head = c->k_head;
-    p.v_page = (unsigned)c->v_page;
-    p.v_tok = (unsigned)c->v_token;
-    p.v_head = c->v_head;
-    p.pages = (int)c->pages;
-    p.page_size = FastDiv((unsigned)c->page_size);
-    return p;
-}
-
-PageBatch batch_of(const nnjit_paged_batch *b) {
-    return PageBatch{b->q_start, b->kv_len, b->page_table, b->ld_table, (int)b->table_pages, (int)b->sequences, (int)b->tokens};
-}
-
-bool pool_in_units(const nnjit_paged_kv *c, int64_t elems) {
-    return in_units(c->k, c->k_token, c->k_head, elems, c->dtype) && in_units(c->v, c->v_token, c->v_head, elems, c->dtype) &&
-           c->k_page % elems == 0 && c->v_page % elems == 0;
-}
 
 struct RotaryCall {
     RotaryParams p{};
@@ -141,13 +24,16 @@ struct AttentionCall {
     bool vec = false;
     int64_t max_q = 0, max_kv = 0;
     hipStream_t stream = nullptr;
+
+    // keys that a row's window and, of a tree, the new tokens behind it reach over
+    int64_t window() const { return p.window > 0 && p.mask ? p.window + max_q : p.window; }
 };
 
 int64_t attention_floats(void *ctx, int cus) {
     AttentionCall &c = *(AttentionCall *)ctx;
     const AttentionParams &p = c.p;
     c.plan = attention_plan(c.dtype, p.batch.tokens, p.batch.sequences, p.q_heads, p.q_heads / p.group, p.dim, c.max_q, c.max_kv,
-                            p.causal, p.window, cus);
+                            p.causal, c.window(), cus);
     return c.plan.ws_floats;
 }
 
@@ -161,6 +47,54 @@ hipError_t do_attention(void *ctx, const RuntimeDevice &d) {
         c.p.stat = d.ws + rows * c.p.part_dim;
     }
     return launch_attention(c.p, c.plan, c.dtype, c.vec, c.stream);
+}
+
+// What plain, causal and tree attention have in common; c.p: the mask of trees.
+int attend(AttentionCall &c, const nnjit_paged_kv *cache, const nnjit_paged_batch *batch, int64_t q_heads, const void *q, int64_t q_token,
+           int64_t q_head, void *out, int64_t out_token, int64_t out_head, float scale, int causal, int64_t window, void *stream, const char *what) {
+    int rc = check_cache(cache);
+    if (rc != NNJIT_OK) return rc;
+    if ((rc = check_batch(batch)) != NNJIT_OK) return rc;
+    if (q_heads < 1 || q_heads > kMaxInt || q_heads % cache->kv_heads)
+        return runtime_fail(NNJIT_EINVAL, "q_heads=%lld is no multiple of kv_heads=%lld", (long long)q_heads, (long long)cache->kv_heads);
+    if (batch->max_q < 0 || batch->max_q > kMaxInt) return runtime_fail(NNJIT_EINVAL, "max_q=%lld out of [0, 2^31)", (long long)batch->max_q);
+    if (batch->max_kv < 0 || batch->max_kv > kMaxKeys) return runtime_fail(NNJIT_EINVAL, "max_kv=%lld out of [0, 2^30]", (long long)batch->max_kv);
+    if (!std::isfinite(scale)) return runtime_fail(NNJIT_EINVAL, "scale is not finite");
+    if (window < 0) return runtime_fail(NNJIT_EINVAL, "window=%lld is negative", (long long)window);
+    if (window > 0 && !causal) return runtime_fail(NNJIT_EINVAL, "a window needs causal attention");
+    const int64_t dim = cache->head_dim, rows = batch->tokens;
+    if ((rc = check_rows("q", q, rows, q_heads, q_token, q_head)) != NNJIT_OK) return rc;
+    if ((rc = check_written("out", out, rows, q_heads, dim, out_token, out_head)) != NNJIT_OK) return rc;
+    if (rows == 0 || batch->sequences == 0 || batch->max_q == 0) return NNJIT_OK;
+    const int64_t units = (cache->dtype == NNJIT_F16) ? 8 : 4;   // elements of 16 bytes
+    c.p.q = HeadRows{q, q_token, q_head};
+    c.p.o = HeadRows{out, out_token, out_head};
+    c.p.q_heads = (int)q_heads;
+    c.p.group = (int)(q_heads / cache->kv_heads);
+    c.p.group_div = FastDiv((unsigned)c.p.group);
+    c.p.dim = (int)dim;
+    c.p.pool = pool_of(cache);
+    c.p.batch = batch_of(batch);
+    // a scale of 0 (all keys alike) would make NaNs of masked logits: 2^-100 leaves
+    // the weights of all q . k below 2^76 alike to the last bit
+    c.p.scale_log2 = (float)std::fmin(std::fmax(std::fabs((double)scale) * 1.4426950408889634074, 0x1p-100), (double)std::numeric_limits<float>::max());
+    c.p.negate = scale < 0.f;
+    c.p.causal = causal != 0;
+    c.p.window = (int)std::min<int64_t>(window, kMaxInt);
+    c.dtype = cache->dtype;
+    c.vec = dim % units == 0 && in_units(q, q_token, q_head, units, c.dtype) && in_units(out, out_token, out_head, units, c.dtype) &&
+            pool_in_units(cache, units);
+    c.max_q = std::min(batch->max_q, rows);
+    const int64_t room = batch->table_pages * cache->page_size;
+    c.max_kv = std::min(batch->max_kv, room);
+    c.stream = (hipStream_t)stream;
+    if (rows * q_heads > kMaxInt || c.max_q * c.p.group > kMaxInt - 64)
+        return runtime_fail(NNJIT_EINVAL, "%lld rows of %lld heads in one call: below 2^31 are served", (long long)rows, (long long)q_heads);
+    const AttentionPlan least = attention_plan(c.dtype, rows, batch->sequences, c.p.q_heads, (int)cache->kv_heads, c.p.dim, c.max_q, c.max_kv,
+                                               c.p.causal, c.window(), 1024);
+    if ((double)least.row_tiles * least.splits * (double)cache->kv_heads * (double)batch->sequences > (double)kMaxGroups)
+        return runtime_fail(NNJIT_EINVAL, "more than 2^24 - 1 workgroups (sequences times key heads times tiles)");
+    return runtime_launch(c.stream, attention_floats, do_attention, &c, what);
 }
 
 struct TableCall {
@@ -290,50 +224,24 @@ int nnjit_paged_attention(const nnjit_paged_kv *cache, const nnjit_paged_batch *
                           int64_t q_head, void *out, int64_t out_token, int64_t out_head, float scale, int causal, int64_t window,
                           void *stream) {
     runtime_clear_error();
-    int rc = check_cache(cache);
-    if (rc != NNJIT_OK) return rc;
-    if ((rc = check_batch(batch)) != NNJIT_OK) return rc;
-    if (q_heads < 1 || q_heads > kMaxInt || q_heads % cache->kv_heads)
-        return runtime_fail(NNJIT_EINVAL, "q_heads=%lld is no multiple of kv_heads=%lld", (long long)q_heads, (long long)cache->kv_heads);
-    if (batch->max_q < 0 || batch->max_q > kMaxInt) return runtime_fail(NNJIT_EINVAL, "max_q=%lld out of [0, 2^31)", (long long)batch->max_q);
-    if (batch->max_kv < 0 || batch->max_kv > kMaxKeys) return runtime_fail(NNJIT_EINVAL, "max_kv=%lld out of [0, 2^30]", (long long)batch->max_kv);
-    if (!std::isfinite(scale)) return runtime_fail(NNJIT_EINVAL, "scale is not finite");
-    if (window < 0) return runtime_fail(NNJIT_EINVAL, "window=%lld is negative", (long long)window);
-    if (window > 0 && !causal) return runtime_fail(NNJIT_EINVAL, "a window needs causal attention");
-    const int64_t dim = cache->head_dim, rows = batch->tokens;
-    if ((rc = check_rows("q", q, rows, q_heads, q_token, q_head)) != NNJIT_OK) return rc;
-    if ((rc = check_written("out", out, rows, q_heads, dim, out_token, out_head)) != NNJIT_OK) return rc;
-    if (rows == 0 || batch->sequences == 0 || batch->max_q == 0) return NNJIT_OK;
-    const int64_t units = (cache->dtype == NNJIT_F16) ? 8 : 4;   // elements of 16 bytes
     AttentionCall c;
-    c.p.q = HeadRows{q, q_token, q_head};
-    c.p.o = HeadRows{out, out_token, out_head};
-    c.p.q_heads = (int)q_heads;
-    c.p.group = (int)(q_heads / cache->kv_heads);
-    c.p.group_div = FastDiv((unsigned)c.p.group);
-    c.p.dim = (int)dim;
-    c.p.pool = pool_of(cache);
-    c.p.batch = batch_of(batch);
-    // a scale of 0 (all keys alike) would make NaNs of masked logits: 2^-100 leaves
-    // the weights of all q . k below 2^76 alike to the last bit
-    c.p.scale_log2 = (float)std::fmin(std::fmax(std::fabs((double)scale) * 1.4426950408889634074, 0x1p-100), (double)std::numeric_limits<float>::max());
-    c.p.negate = scale < 0.f;
-    c.p.causal = causal != 0;
-    c.p.window = (int)std::min<int64_t>(window, kMaxInt);
-    c.dtype = cache->dtype;
-    c.vec = dim % units == 0 && in_units(q, q_token, q_head, units, c.dtype) && in_units(out, out_token, out_head, units, c.dtype) &&
-            pool_in_units(cache, units);
-    c.max_q = std::min(batch->max_q, rows);
-    const int64_t room = batch->table_pages * cache->page_size;
-    c.max_kv = std::min(batch->max_kv, room);
-    c.stream = (hipStream_t)stream;
-    if (rows * q_heads > kMaxInt || c.max_q * c.p.group > kMaxInt - 64)
-        return runtime_fail(NNJIT_EINVAL, "%lld rows of %lld heads in one call: below 2^31 are served", (long long)rows, (long long)q_heads);
-    const AttentionPlan least = attention_plan(c.dtype, rows, batch->sequences, c.p.q_heads, (int)cache->kv_heads, c.p.dim, c.max_q, c.max_kv,
-                                               c.p.causal, c.p.window, 1024);
-    if ((double)least.row_tiles * least.splits * (double)cache->kv_heads * (double)batch->sequences > (double)kMaxGroups)
-        return runtime_fail(NNJIT_EINVAL, "more than 2^24 - 1 workgroups (sequences times key heads times tiles)");
-    return runtime_launch(c.stream, attention_floats, do_attention, &c, "paged_attention");
+    return attend(c, cache, batch, q_heads, q, q_token, q_head, out, out_token, out_head, scale, causal, window, stream, "paged_attention");
+}
+
+int nnjit_tree_attention(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch, const uint32_t *mask, int64_t ld_mask,
+                         int64_t mask_words, const int32_t *positions, int64_t q_heads, const void *q, int64_t q_token, int64_t q_head,
+                         void *out, int64_t out_token, int64_t out_head, float scale, int64_t window, void *stream) {
+    runtime_clear_error();
+    if (mask_words < 1 || mask_words > 1 << 20) return runtime_fail(NNJIT_EINVAL, "mask_words=%lld out of [1, 2^20]", (long long)mask_words);
+    if (ld_mask < 0) return runtime_fail(NNJIT_EINVAL, "negative ld_mask");
+    if (!mask && batch && batch->tokens > 0) return runtime_fail(NNJIT_EINVAL, "mask is NULL");
+    if (window > 0 && !positions && batch && batch->tokens > 0) return runtime_fail(NNJIT_EINVAL, "a window needs positions");
+    AttentionCall c;
+    c.p.mask = mask;
+    c.p.ld_mask = ld_mask;
+    c.p.mask_words = (int)mask_words;
+    c.p.positions = positions;
+    return attend(c, cache, batch, q_heads, q, q_token, q_head, out, out_token, out_head, scale, 1, window, stream, "tree_attention");
 }
 
 }  // extern "C"

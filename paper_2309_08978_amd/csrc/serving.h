@@ -96,6 +96,10 @@ struct AttentionParams {
     float scale_log2;          // |scale| log2(e), finite and above 0, so that -inf stays -inf
     int negate;                // the scale is negative: queries are taken negated
     int causal, window;
+    const unsigned *mask;      // drafted trees: bit i of row t's words: t sees new token i of its sequence (NULL: none)
+    long long ld_mask;
+    int mask_words;
+    const int *positions;      // drafted trees with a window: the rows' positions
     int row_tiles;             // row tiles of a sequence and key head
     int splits;                // workgroups along the keys
     int split_keys;            // keys of one split (a multiple of the key tile)
@@ -108,16 +112,99 @@ struct AttentionParams {
 
 // How one call is laid out on the chip; sizes the scratch.
 struct AttentionPlan {
-    int tile_rows;             // rows of a tile.  16: attention_rows.hip; 64, 128: attention_tiles.h
+    int tile_rows;             // rows of a tile.  16: attention_rows.h; 64, 128: attention_tiles.h
     int row_tiles, splits, split_keys;
-    int waves;                 // waves of a workgroup of attention_rows.hip, 4 or 8
+    int waves;                 // waves of a workgroup of attention_rows.h, 4 or 8
     int64_t ws_floats;         // partial sums and statistics
 };
 AttentionPlan attention_plan(int dtype, int64_t tokens, int64_t sequences, int q_heads, int kv_heads, int dim, int64_t max_q,
                              int64_t max_kv, int causal, int64_t window, int cus);
 hipError_t launch_attention_tiles_f16(const AttentionParams &p, int tile_rows, bool vec, int grid, hipStream_t stream);
 hipError_t launch_attention_tiles_f32(const AttentionParams &p, int tile_rows, bool vec, int grid, hipStream_t stream);
+// The same kernels for drafted trees (p.mask).
+hipError_t launch_tree_rows(const AttentionParams &p, int dtype, bool vec, int waves, int grid, hipStream_t stream);
+hipError_t launch_tree_tiles_f16(const AttentionParams &p, int tile_rows, bool vec, int grid, hipStream_t stream);
+hipError_t launch_tree_tiles_f32(const AttentionParams &p, int tile_rows, bool vec, int grid, hipStream_t stream);
 hipError_t launch_attention(AttentionParams p, const AttentionPlan &plan, int dtype, bool vec, hipStream_t stream);
+
+// Most sequences of a step whose arrays are built (their prefix sums lie in LDS), and most words of a tree's mask.
+constexpr int kStepSequences = 8192, kStepWords = 32;
+
+struct StepParams {
+    const int *held, *keep, *added, *parent;
+    int *page_table;
+    long long ld_table;
+    int table_pages, sequences, tokens;
+    FastDiv page_size;
+    int *q_start, *kv_len, *positions;
+    long long *slots;
+    unsigned *mask;
+    long long ld_mask;
+    int mask_words;
+    int *status;
+    int *free_pages;
+    int capacity;
+    const int *count;
+    int *count_out;
+};
+hipError_t launch_paged_step(const StepParams &p, hipStream_t stream);
+
+struct NormParams {
+    HeadRows q, qo;            // rows to rows; heads 0 .. q_heads - 1
+    int q_heads;
+    HeadRows k, v;             // appended rows (kv_heads heads each; 0 without a cache)
+    int kv_heads;
+    PagePool pool;
+    const long long *slots;    // appends: the place of every row
+    const int *positions;
+    const float *table;        // NULL: nothing is turned
+    int table_rows;
+    int rot, dim, tokens;
+    int interleaved;
+    const void *q_weight, *k_weight;   // NULL: not normed
+    long long qw_head, kw_head;
+    int weight_half;           // weights are fp16
+    float eps;
+    int heads_per_block;
+    // gradients: q holds x, qo dx (p NULL: not wanted)
+    HeadRows dy;
+    float *dw, *part;          // [groups][dim] partial sums (per head: [groups][heads][dim])
+    int chunk;                 // rows (per head: tokens) of a workgroup
+};
+hipError_t launch_norm_rotary(const NormParams &p, bool append, int src_dtype, int dst_dtype, bool vec, hipStream_t stream);
+// Workgroups along the rows that add partial sums of dw: sizes the scratch.
+int norm_grad_groups(int64_t tokens, int64_t heads, int dim, bool per_head, bool vec, int cus);
+hipError_t launch_norm_rotary_grad(const NormParams &p, int x_dtype, int dy_dtype, bool vec, int groups, hipStream_t stream);
+
+struct MoveParams {
+    PagePool pool;
+    PageBatch batch;
+    const int *path, *accepted;
+    long long ld_path;
+    int path_len, kv_heads, row_bytes;     // row_bytes: of one head
+};
+// unit: bytes that a thread moves at a time (16, 8, 4 or 2), which divides every offset
+hipError_t launch_kv_move(const MoveParams &p, int elem_bytes, int unit, hipStream_t stream);
+
+struct LogitParams {
+    const int *history, *length, *prompt;
+    long long ld_history;
+    int history_len;
+    const float *repetition, *presence, *frequency;
+    const int *bias_token;
+    const float *bias_value;
+    long long ld_bias;
+    int bias_len;
+    const unsigned *mask;
+    long long ld_mask;
+    int mask_rows;
+    const int *mask_row;
+    int rows, vocab;
+    const void *x;
+    void *y;
+    long long ldx, ldy;
+};
+hipError_t launch_adjust_logits(const LogitParams &p, int x_dtype, int y_dtype, bool vec, int cus, hipStream_t stream);
 
 // Runtime services for entry points outside runtime.cpp.
 int runtime_fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));

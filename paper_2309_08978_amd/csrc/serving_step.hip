@@ -1,0 +1,234 @@
+// The arrays of one step of a served batch, from the requests' lengths.
+//
+// All of it is prefix sums over the sequences and look-ups in them: with
+//   old = ceil(held / P), need = ceil((keep + added) / P)
+// sequence b gives back old - need pages or takes need - old.  Taken page i
+// (counted over the batch) is entry top - 1 - i of the stack that the given back
+// ones lie on top of, top = count + given back: above `count` that is given
+// back page top - 1 - i - count itself, read from where it still stands in the
+// page table.  So every entry of table, stack and slots follows from the prefix
+// sums and from entries that no one writes in this step, and workgroups need
+// not wait for each other: each takes the sums anew (a few kilobytes of lengths)
+// and then its share of the rows and pages.
+//
+// Only where lengths or count are replaced in place would a workgroup that starts
+// late read what an early one has written: one workgroup does such a step alone,
+// writing them last, or a second launch does.
+//
+// A tree row's ancestors are found by walking up the parents, of which a workgroup holds
+// its rows' and the kStepWords 32 before them in LDS.
+#include "serving.h"
+
+namespace nnjit {
+
+namespace {
+
+enum { kMissing = 1, kLengths = 2, kRows = 4, kPool = 8 };
+
+// Sum of `v` over the threads before this one, and of all; `waves`: THREADS / 64 words of LDS.
+template <int THREADS>
+__device__ __forceinline__ long long sum_before(long long v, long long *waves, long long &total)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    long long run = v;
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) {
+        const long long up = __shfl_up(run, i);
+        if (lane >= i) run += up;
+    }
+    if (lane == 63) waves[wave] = run;
+    __syncthreads();
+    long long before = run - v;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        if (w < wave) before += waves[w];
+        total += waves[w];
+    }
+    return before;
+}
+
+// The last b with sums[b] <= i, 0 <= i < sums[n].
+__device__ __forceinline__ int holder(const int *sums, int n, int i)
+{
+    int lo = 0, hi = n;                       // sums[lo] <= i < sums[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (sums[mid] <= i) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// THREADS PER sequences at most.  LATER: lengths and count are left to a second
+// launch, FINISH, which writes nothing else.
+template <int THREADS, int PER, bool LATER, bool FINISH>
+__global__ void __launch_bounds__(THREADS)
+paged_step_kernel(StepParams p)
+{
+    constexpr int N = THREADS * PER, REACH = 32 * kStepWords;
+    __shared__ int start[N + 1], back[N + 1], more[N + 1];
+    __shared__ long long waves[3][THREADS / 64];
+    __shared__ int parents[REACH + THREADS];
+
+    const int tid = threadIdx.x, n = p.sequences;
+    const int page_size = p.page_size.d;
+    const long long room = min((long long)p.table_pages * page_size, kMaxKeys);
+    auto pages_of = [&](int tokens) { return p.page_size.quot(tokens + page_size - 1); };
+
+    int rows_of[PER], delta[PER], bad = 0;
+    long long rows = 0, given = 0, taken = 0;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        const int b = tid * PER + e;
+        rows_of[e] = delta[e] = 0;
+        if (b >= n) continue;
+        const int held = p.held[b], keep = p.keep ? p.keep[b] : held, added = p.added[b];
+        if (held < 0 || keep < 0 || keep > held || added < 0 || held > room || (long long)keep + added > room) {
+            bad |= kLengths;
+            continue;
+        }
+        if (p.parent && added > 32 * p.mask_words) bad |= kRows;
+        rows_of[e] = added;
+        delta[e] = pages_of(keep + added) - pages_of(held);
+        rows += added;
+        given += max(-delta[e], 0);
+        taken += max(delta[e], 0);
+    }
+    bad = __syncthreads_or(bad & kLengths ? 1 : 0) * kLengths | __syncthreads_or(bad & kRows ? 1 : 0) * kRows;
+    long long all_rows, all_given, all_taken;
+    const long long rows_before = sum_before<THREADS>(rows, waves[0], all_rows);
+    const long long given_before = sum_before<THREADS>(given, waves[1], all_given);
+    const long long taken_before = sum_before<THREADS>(taken, waves[2], all_taken);
+    const int count = p.count[0];
+    if (all_rows > p.tokens) bad |= kRows;
+    if (count < 0 || count > p.capacity || count + all_given > p.capacity) bad |= kPool;
+    const long long missing = bad & (kLengths | kPool) ? 0 : max(all_taken - all_given - count, 0ll);
+    if (missing > 0) bad |= kMissing;
+    const int top = bad ? count : count + (int)all_given, left = bad ? count : top - (int)all_taken;
+    const int pages = bad ? 0 : (int)all_taken, pushes = max(left - count, 0);
+
+    if constexpr (!FINISH) {
+        int at[3] = {(int)rows_before, (int)given_before, (int)taken_before};
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            const int b = tid * PER + e;
+            start[b] = bad ? 0 : at[0];
+            back[b] = at[1];
+            more[b] = at[2];
+            at[0] += rows_of[e];
+            at[1] += max(-delta[e], 0);
+            at[2] += max(delta[e], 0);
+        }
+        if (tid == THREADS - 1) {
+            start[N] = bad ? 0 : at[0];
+            back[N] = at[1];
+            more[N] = at[2];
+        }
+        __syncthreads();
+
+        auto keys_of = [&](int b) { return (p.keep ? p.keep[b] : p.held[b]) + p.added[b]; };
+        auto given_back = [&](int i) {
+            const int b = holder(back, n, i);
+            return p.page_table[(long long)b * p.ld_table + pages_of(keys_of(b)) + i - back[b]];
+        };
+        auto page_taken = [&](int i) {
+            const int entry = top - 1 - i;
+            return entry >= count ? given_back(entry - count) : p.free_pages[entry];
+        };
+
+        const int stride = gridDim.x * THREADS, first = blockIdx.x * THREADS;
+        for (int b = first + tid; b <= n; b += stride) p.q_start[b] = start[b];
+        for (int i = first + tid; i < pages; i += stride) {
+            const int b = holder(more, n, i);
+            p.page_table[(long long)b * p.ld_table + pages_of(p.held[b]) + i - more[b]] = page_taken(i);
+        }
+        for (int i = first + tid; i < pushes; i += stride) p.free_pages[count + i] = given_back(i);
+        if (blockIdx.x == 0 && tid < 4)
+            p.status[tid] = tid == 0 ? bad : tid == 1 ? (int)min(missing, 0x7fffffffll) : tid == 2 ? (bad ? 0 : (int)all_rows) : left;
+
+        const int end = start[n];
+        for (int base = first; base < p.tokens; base += stride) {
+            const int t = base + tid;
+            if (p.parent) {
+                __syncthreads();
+                for (int i = tid; i < REACH + THREADS; i += THREADS) {
+                    const int row = base - REACH + i;
+                    parents[i] = row >= 0 && row < end ? p.parent[row] : -1;
+                }
+                __syncthreads();
+            }
+            if (t >= p.tokens) continue;
+            int position = 0;
+            long long slot = -1;
+            if (t < end) {
+                const int b = holder(start, n, t), held = p.held[b], keep = p.keep ? p.keep[b] : held;
+                const int place = keep + t - start[b], at_page = p.page_size.quot(place), old = pages_of(held);
+                const int page = at_page < old ? p.page_table[(long long)b * p.ld_table + at_page] : page_taken(more[b] + at_page - old);
+                if (page >= 0) slot = (long long)page * page_size + place - at_page * page_size;
+                position = place;
+                if (p.parent) {
+                    const int *own = parents + REACH - (base - start[b]);          // own[i]: parent of the sequence's node i
+                    unsigned *row = p.mask + (long long)t * p.ld_mask;
+                    int node = t - start[b], word = p.mask_words - 1, depth = 0;
+                    unsigned bits = 0;
+                    while (true) {
+                        for (; word > node >> 5; --word) {
+                            row[word] = bits;
+                            bits = 0;
+                        }
+                        bits |= 1u << (node & 31);
+                        const int up = own[node];
+                        if (up < 0 || up >= node) break;
+                        node = up;
+                        ++depth;
+                    }
+                    for (; word >= 0; --word) {
+                        row[word] = bits;
+                        bits = 0;
+                    }
+                    position = keep + depth;
+                }
+            } else if (p.parent) {
+                for (int w = 0; w < p.mask_words; ++w) p.mask[(long long)t * p.ld_mask + w] = 0;
+            }
+            if (p.positions) p.positions[t] = position;
+            if (p.slots) p.slots[t] = slot;
+        }
+        __syncthreads();
+    }
+    if constexpr (!LATER) {
+        for (int b = blockIdx.x * THREADS + tid; b < n; b += gridDim.x * THREADS) {
+            const int held = p.held[b];
+            p.kv_len[b] = bad ? held : (p.keep ? p.keep[b] : held) + p.added[b];
+        }
+        if (blockIdx.x == 0 && tid == 0) p.count_out[0] = left;
+    }
+}
+
+template <int THREADS, int PER>
+hipError_t launch_as(const StepParams &p, hipStream_t stream)
+{
+    const bool in_place = p.kv_len == p.held || p.kv_len == p.keep || p.count_out == p.count;
+    const int most = 512, want = (p.tokens + THREADS - 1) / THREADS, groups = want < 1 ? 1 : want < most ? want : most;
+    if (in_place && groups > 1) {
+        paged_step_kernel<THREADS, PER, true, false><<<groups, THREADS, 0, stream>>>(p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        paged_step_kernel<THREADS, PER, false, true><<<1, THREADS, 0, stream>>>(p);
+    } else {
+        paged_step_kernel<THREADS, PER, false, false><<<groups, THREADS, 0, stream>>>(p);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_step(const StepParams &p, hipStream_t stream)
+{
+    if (p.sequences <= 256) return launch_as<256, 1>(p, stream);
+    if (p.sequences <= 1024) return launch_as<256, 4>(p, stream);
+    return launch_as<1024, kStepSequences / 1024>(p, stream);
+}
+
+}  // namespace nnjit

@@ -679,7 +679,7 @@ int nnjit_kv_move(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch, c
 /* Rules for rows of logits; any group of pointers may be NULL (its rule then
  * does not apply).  All on the device. */
 typedef struct nnjit_logit_rules {
-    const int32_t *history;            /* [rows][ld_history]: the tokens so far, */
+    const int32_t *history;            /* [rows][ld_history]: the tokens so far (NULL: history_len 0), */
     int64_t ld_history, history_len;   /* history_len columns at most, */
     const int32_t *length;             /* [rows]: so many of them (clamped to 0 .. history_len; NULL: all); */
     const int32_t *prompt;             /* [rows]: the first so many are the prompt's (NULL: none) */

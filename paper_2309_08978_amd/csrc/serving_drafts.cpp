@@ -81,7 +81,7 @@ int check_norm_rows(const nnjit_rotary_table *rotary, int64_t tokens, int64_t he
     if ((rc = check_weight("weight", weight, w_head, w_dtype, eps, dim)) != NNJIT_OK) return rc;
     if ((rc = check_turned(rotary, positions, tokens, dim)) != NNJIT_OK) return rc;
     if ((rc = check_rows("x", x, tokens, heads, x_token, x_head)) != NNJIT_OK) return rc;
-    if (tokens > 0 && heads > 0 && !weight) return runtime_fail(NNJIT_EINVAL, "weight is NULL");
+    if (heads > 0 && !weight) return runtime_fail(NNJIT_EINVAL, "weight is NULL");
     if (tokens > kMaxGroups) return runtime_fail(NNJIT_EINVAL, "%lld tokens in one call: below 2^24 are served", (long long)tokens);
     return NNJIT_OK;
 }
@@ -310,8 +310,7 @@ int nnjit_adjust_logits(const nnjit_logit_rules *rules, int64_t rows, int64_t vo
     if ((r.bias_token == nullptr) != (r.bias_value == nullptr)) return runtime_fail(NNJIT_EINVAL, "bias_token and bias_value go together");
     if (r.bias_token && (r.bias_len < 0 || r.bias_len > kMaxInt - 1 || r.ld_bias < 0))
         return runtime_fail(NNJIT_EINVAL, "bias_len=%lld out of [0, 2^31) or a negative ld_bias", (long long)r.bias_len);
-    if (!r.history && (r.length || r.prompt || r.repetition || r.presence || r.frequency))
-        return runtime_fail(NNJIT_EINVAL, "lengths and penalties need a history");
+    if (!r.history && r.history_len != 0) return runtime_fail(NNJIT_EINVAL, "history is NULL with history_len=%lld", (long long)r.history_len);
     if (r.mask && (r.ld_mask < 0 || r.mask_rows < 1 || r.mask_rows > kMaxInt))
         return runtime_fail(NNJIT_EINVAL, "mask_rows=%lld out of [1, 2^31) or a negative ld_mask", (long long)r.mask_rows);
     if (!r.mask && r.mask_row) return runtime_fail(NNJIT_EINVAL, "mask_row without mask");

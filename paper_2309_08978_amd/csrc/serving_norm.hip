@@ -358,7 +358,7 @@ int norm_grad_groups(int64_t tokens, int64_t heads, int dim, bool per_head, bool
 {
     const int64_t rows = per_head ? tokens : tokens * heads, at_once = kThreads / lanes_per_head(dim, vec);
     const int64_t want = (rows + at_once - 1) / at_once, most = per_head ? (4 * cus + heads - 1) / heads : 4 * cus;
-    return (int)(want < most ? want : most);
+    return (int)(want < 1 ? 1 : want < most ? want : most);      // (no rows: one adds up nothing)
 }
 
 hipError_t launch_norm_rotary_grad(const NormParams &in, int x_dtype, int dy_dtype, bool vec, int groups, hipStream_t stream)

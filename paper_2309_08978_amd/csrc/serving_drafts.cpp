@@ -71,6 +71,13 @@ void set_rotary(NormParams &p, const nnjit_rotary_table *rotary, const int32_t *
     p.interleaved = rotary && rotary->layout == NNJIT_ROTARY_INTERLEAVED;
 }
 
+// weights and angles can be taken four at a time
+bool norm_in_units(const NormParams &p) {
+    const int dtype = p.weight_half ? NNJIT_F16 : NNJIT_F32;
+    return (!p.q_weight || in_units(p.q_weight, 0, p.qw_head, 4, dtype)) && (!p.k_weight || in_units(p.k_weight, 0, p.kw_head, 4, dtype)) &&
+           (!p.table || in_units(p.table, 0, 0, 4, NNJIT_F32));
+}
+
 // what nnjit_norm_rotary and its gradient have in common: *done: nothing is to be done
 int check_norm_rows(const nnjit_rotary_table *rotary, int64_t tokens, int64_t heads, int64_t dim, const int32_t *positions, const void *weight,
                     int64_t w_head, int w_dtype, float eps, const void *x, int64_t x_token, int64_t x_head) {
@@ -187,7 +194,7 @@ int nnjit_kv_append_slots(const nnjit_paged_kv *cache, int64_t tokens, const int
         c.p.eps = norm->eps;
     }
     c.append = true;
-    c.vec = dim % 8 == 0 && c.p.rot % 8 == 0 && in_units(k, k_token, k_head, 4, src_dtype) && in_units(v, v_token, v_head, 4, src_dtype) &&
+    c.vec = dim % 8 == 0 && c.p.rot % 8 == 0 && norm_in_units(c.p) && in_units(k, k_token, k_head, 4, src_dtype) && in_units(v, v_token, v_head, 4, src_dtype) &&
             (q_heads == 0 || (in_units(q, q_token, q_head, 4, src_dtype) && in_units(q_out, qo_token, qo_head, 4, cache->dtype))) &&
             pool_in_units(cache, 4);
     c.src = src_dtype;
@@ -216,7 +223,7 @@ int nnjit_norm_rotary(const nnjit_rotary_table *rotary, int64_t tokens, int64_t 
     c.p.qw_head = w_head;
     c.p.weight_half = w_dtype == NNJIT_F16;
     c.p.eps = eps;
-    c.vec = head_dim % 8 == 0 && c.p.rot % 8 == 0 && in_units(x, x_token, x_head, 4, x_dtype) && in_units(y, y_token, y_head, 4, y_dtype);
+    c.vec = head_dim % 8 == 0 && c.p.rot % 8 == 0 && norm_in_units(c.p) && in_units(x, x_token, x_head, 4, x_dtype) && in_units(y, y_token, y_head, 4, y_dtype);
     c.src = x_dtype;
     c.dst = y_dtype;
     c.stream = (hipStream_t)stream;
@@ -250,7 +257,7 @@ int nnjit_norm_rotary_grad(const nnjit_rotary_table *rotary, int64_t tokens, int
     c.p.weight_half = w_dtype == NNJIT_F16;
     c.p.eps = eps;
     c.p.dw = dw;
-    c.vec = head_dim % 8 == 0 && c.p.rot % 8 == 0 && in_units(x, x_token, x_head, 4, x_dtype) && in_units(dy, dy_token, dy_head, 4, dy_dtype) &&
+    c.vec = head_dim % 8 == 0 && c.p.rot % 8 == 0 && norm_in_units(c.p) && in_units(x, x_token, x_head, 4, x_dtype) && in_units(dy, dy_token, dy_head, 4, dy_dtype) &&
             (!dx || in_units(dx, dx_token, dx_head, 4, x_dtype));
     c.src = x_dtype;
     c.dst = dy_dtype;

@@ -5,10 +5,11 @@
 //   z -= phi c + (pi if c > 0)            c: how often it is there behind the prompt
 //   z += beta;  -inf where the mask has no bit
 //
-// A workgroup takes kSegment neighbouring tokens of a row: it counts those of the
-// history that fall into them (integer sums in LDS, so their order does not matter),
-// notes for each token the last bias entry, and goes over the logits once.  The
-// history is read once a segment, from the caches.
+// A workgroup takes a segment of neighbouring tokens of a row: it counts those of the
+// history that fall into it (integer sums in LDS, so their order does not matter),
+// notes for each token the last bias entry, and goes over the logits once; they and the
+// first of the history are asked for before all that.  The history is read once a
+// segment, from the caches.
 #include "kcommon.h"
 #include "serving.h"
 #include "nnjit.h"
@@ -18,86 +19,109 @@ namespace nnjit {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr unsigned kInPrompt = 1u << 31;      // of a count: the token is in the prompt
+
+// What LDS holds of a token: bit 31: it is in the prompt; then its count; then the
+// last bias entry, from 1 on.  NARROW: in one word, for histories below 2^15 tokens and
+// biases of less than 2^16 entries, so that twice as many workgroups fit a compute unit; else in two.
+template <bool NARROW>
+struct Noted {
+    static constexpr unsigned kPrompt = 1u << 31, kOne = NARROW ? 1u << 16 : 1u;
+    static constexpr int kWords = NARROW ? 1 : 2;
+    __device__ static __forceinline__ unsigned count(unsigned w) { return (w & ~kPrompt) >> (NARROW ? 16 : 0); }
+    __device__ static __forceinline__ bool seen(unsigned w) { return w >= kOne; }
+};
 
 template <typename T>
 using vec4 = T __attribute__((ext_vector_type(4)));
 
-template <typename S, typename D, bool VEC, int QUADS>   // QUADS: groups of four tokens a thread
+template <typename S, typename D, bool VEC, bool NARROW, int QUADS>   // QUADS: groups of four tokens a thread
 __global__ void __launch_bounds__(kThreads)
 adjust_logits_kernel(LogitParams p, int segments)
 {
-    constexpr int SEGMENT = kThreads * 4 * QUADS;
-    __shared__ __attribute__((aligned(16))) unsigned counts[SEGMENT];
-    __shared__ __attribute__((aligned(16))) int last_bias[SEGMENT];
+    typedef Noted<NARROW> N;
+    constexpr int SEGMENT = kThreads * 4 * QUADS, AHEAD = 8;
+    __shared__ __attribute__((aligned(16))) unsigned noted[N::kWords * SEGMENT];
+    unsigned *entries = noted + (N::kWords - 1) * SEGMENT;             // last bias entries
     const int row = blockIdx.x / segments, v0 = (blockIdx.x - row * segments) * SEGMENT, tid = threadIdx.x;
     const S *x = (const S *)p.x + (long long)row * p.ldx + v0;
     D *y = (D *)p.y + (long long)row * p.ldy + v0;
     const int here = min(p.vocab - v0, SEGMENT);
 
-    float z[QUADS][4];
+    const int *tokens = p.history + (p.history ? (long long)row * p.ld_history : 0);
+    int first[AHEAD];
+    if (p.history) {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) first[k] = k * kThreads + tid < p.history_len ? tokens[k * kThreads + tid] : -1;
+    }
+    vec4<S> raw[QUADS];
 #pragma unroll
     for (int q = 0; q < QUADS; ++q) {
         const int v = (q * kThreads + tid) * 4;
+        raw[q] = vec4<S>{};
         if (VEC && v + 4 <= here) {
-            const f32x4 f = __builtin_convertvector(*(const vec4<S> *)(x + v), f32x4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) z[q][e] = f[e];
+            raw[q] = *(const vec4<S> *)(x + v);
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) z[q][e] = v + e < here ? (float)x[v + e] : 0.f;
+            for (int e = 0; e < 4; ++e)
+                if (v + e < here) raw[q][e] = x[v + e];
         }
     }
-
-    for (int i = tid; i < SEGMENT; i += kThreads) {
-        counts[i] = 0;
-        last_bias[i] = 0;
+    const unsigned *mask = nullptr;
+    if (p.mask) {
+        const int m = p.mask_row ? p.mask_row[row] : row;
+        if (m >= 0) mask = p.mask + (long long)min(m, p.mask_rows - 1) * p.ld_mask;
     }
+    unsigned allowed[QUADS];
+#pragma unroll
+    for (int q = 0; q < QUADS; ++q) {
+        const int v = (q * kThreads + tid) * 4;
+        allowed[q] = mask && v < here ? mask[(v0 + v) >> 5] >> (v & 31) : 15u;
+    }
+
+    for (int i = tid; i < N::kWords * SEGMENT / 4; i += kThreads) ((u32x4 *)noted)[i] = u32x4{0, 0, 0, 0};
     __syncthreads();
+    if (p.bias_token) {
+        const int *bias = p.bias_token + (long long)row * p.ld_bias;
+        for (int i = tid; i < p.bias_len; i += kThreads) {
+            const unsigned v = (unsigned)bias[i] - (unsigned)v0;       // (a negative token lies above every segment)
+            if (v < (unsigned)here) atomicMax(&entries[v], (unsigned)i + 1u);
+        }
+        if (NARROW) __syncthreads();                                   // (counts lie above the entries)
+    }
     if (p.history) {
         const int length = p.length ? min(max(p.length[row], 0), p.history_len) : p.history_len;
         const int prompt = p.prompt ? p.prompt[row] : 0;
-        const int *tokens = p.history + (long long)row * p.ld_history;
-#pragma unroll 4
-        for (int i = tid; i < length; i += kThreads) {
-            const unsigned v = (unsigned)tokens[i] - (unsigned)v0;   // (a negative token lies above every segment)
-            if (v >= (unsigned)here) continue;
-            if (i < prompt) atomicOr(&counts[v], kInPrompt);
-            else atomicAdd(&counts[v], 1u);
-        }
-    }
-    if (p.bias_token) {
-        const int *tokens = p.bias_token + (long long)row * p.ld_bias;
-        for (int i = tid; i < p.bias_len; i += kThreads) {
-            const unsigned v = (unsigned)tokens[i] - (unsigned)v0;
-            if (v < (unsigned)here) atomicMax(&last_bias[v], i + 1);
-        }
+        auto note = [&](int i, int token) {
+            const unsigned v = (unsigned)token - (unsigned)v0;
+            if (i >= length || v >= (unsigned)here) return;
+            if (i < prompt) atomicOr(&noted[v], N::kPrompt);
+            else atomicAdd(&noted[v], N::kOne);
+        };
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) note(k * kThreads + tid, first[k]);
+#pragma unroll 8
+        for (int i = AHEAD * kThreads + tid; i < length; i += kThreads) note(i, tokens[i]);
     }
     __syncthreads();
 
     const float rho = p.repetition ? p.repetition[row] : 1.f, pi = p.presence ? p.presence[row] : 0.f;
     const float phi = p.frequency ? p.frequency[row] : 0.f;
     const float *bias = p.bias_value + (p.bias_token ? (long long)row * p.ld_bias : 0);
-    const unsigned *mask = nullptr;
-    if (p.mask) {
-        const int m = p.mask_row ? p.mask_row[row] : row;
-        if (m >= 0) mask = p.mask + (long long)min(m, p.mask_rows - 1) * p.ld_mask;
-    }
 #pragma unroll
     for (int q = 0; q < QUADS; ++q) {
         const int v = (q * kThreads + tid) * 4;
         if (v >= here) continue;
-        const unsigned allowed = mask ? mask[(v0 + v) >> 5] >> (v & 31) : 15u;
+        const u32x4 four = *(const u32x4 *)&noted[v];
+        u32x4 entry = NARROW ? four & 0xffffu : *(const u32x4 *)&entries[v];
         vec4<D> out;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const unsigned seen = counts[v + e], c = seen & ~kInPrompt;
-            float f = z[q][e];
-            if (p.repetition && seen) f = f > 0.f ? f / rho : f * rho;
+            float f = (float)raw[q][e];
+            const unsigned c = N::count(four[e]), at = entry[e];
+            if (p.repetition && N::seen(four[e])) f = f > 0.f ? f / rho : f * rho;
             if (c > 0) f = f - phi * (float)c - pi;
-            const int entry = last_bias[v + e];
-            if (entry) f += bias[entry - 1];
-            out[e] = (D)(allowed >> e & 1 ? f : -__builtin_inff());
+            if (at) f += bias[at - 1];
+            out[e] = (D)(allowed[q] >> e & 1 ? f : -__builtin_inff());
         }
         if (VEC && v + 4 <= here) {
             *(vec4<D> *)(y + v) = out;
@@ -112,8 +136,11 @@ hipError_t launch_quads(const LogitParams &p, bool vec, hipStream_t stream)
 {
     const int segments = (p.vocab + kThreads * 4 * QUADS - 1) / (kThreads * 4 * QUADS);
     const unsigned grid = (unsigned)p.rows * (unsigned)segments;
-    if (vec) adjust_logits_kernel<S, D, true, QUADS><<<grid, kThreads, 0, stream>>>(p, segments);
-    else adjust_logits_kernel<S, D, false, QUADS><<<grid, kThreads, 0, stream>>>(p, segments);
+    const bool narrow = p.history_len < 1 << 15 && p.bias_len < 1 << 16;
+    if (vec && narrow) adjust_logits_kernel<S, D, true, true, QUADS><<<grid, kThreads, 0, stream>>>(p, segments);
+    else if (vec) adjust_logits_kernel<S, D, true, false, QUADS><<<grid, kThreads, 0, stream>>>(p, segments);
+    else if (narrow) adjust_logits_kernel<S, D, false, true, QUADS><<<grid, kThreads, 0, stream>>>(p, segments);
+    else adjust_logits_kernel<S, D, false, false, QUADS><<<grid, kThreads, 0, stream>>>(p, segments);
     return hipGetLastError();
 }
 

@@ -3,7 +3,7 @@
 //
 // Node path[i] of the new tokens moves to new token i's place, i <= path[i].  A
 // thread takes one piece (16 bytes, where alignment allows) of one head's key or value row
-// and moves it for every i, eight loads before their eight stores: no thread
+// and moves it for every i, sixteen loads before their stores: no thread
 // touches another's piece, and since later i read at or behind themselves,
 // stores of earlier ones never reach what is still to be read.
 #include "serving.h"
@@ -12,20 +12,23 @@ namespace nnjit {
 
 namespace {
 
-constexpr int kThreads = 256, kAhead = 8;
+constexpr int kThreads = 256, kAhead = 16;
 
 template <typename U>
 __global__ void __launch_bounds__(kThreads)
 kv_move_kernel(MoveParams p, int elem_bytes)
 {
     const int b = blockIdx.x;
+    const int *path = p.path + (long long)b * p.ld_path;
+    int ahead[kAhead];                                               // asked for before what says how many of them count
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) ahead[e] = path[min(e, p.path_len - 1)];
     const PageBatch &batch = p.batch;
     const int q0 = min(max(batch.q_start[b], 0), batch.tokens);
     const int added = min(max(batch.q_start[b + 1] - q0, 0), batch.tokens - q0);
     const long long room = min((long long)batch.table_pages * p.pool.page_size.d, kMaxKeys);
     const long long past = (long long)batch.kv_len[b] - added;      // place of the sequence's new token 0
     const int count = min(max(p.accepted[b], 0), p.path_len);
-    const int *path = p.path + (long long)b * p.ld_path;
     const int *table = batch.page_table + (long long)b * batch.ld_table;
 
     const int pieces = p.row_bytes / (int)sizeof(U);                 // of a head's row
@@ -38,26 +41,35 @@ kv_move_kernel(MoveParams p, int elem_bytes)
     const unsigned page_stride = value ? p.pool.v_page : p.pool.k_page, slot_stride = value ? p.pool.v_tok : p.pool.k_tok;
 
     // the piece of new token i; NULL where the cache has no such place
-    auto place_of = [&](int i) -> U * {
+    auto page_at = [&](int i) {
         const long long place = past + i;
-        if (place < 0 || place >= room) return nullptr;
-        const int at = p.pool.page_size.quot((int)place), page = table[at];
+        return place < 0 || place >= room ? -1 : table[p.pool.page_size.quot((int)place)];
+    };
+    auto piece_at = [&](int i, int page) -> U * {
         if (page < 0 || page >= p.pool.pages) return nullptr;
-        return (U *)(base + page_offset(page, page_stride, (int)place - at * (int)p.pool.page_size.d, slot_stride) * elem_bytes);
+        const int place = (int)(past + i), slot = place - p.pool.page_size.quot(place) * (int)p.pool.page_size.d;
+        return (U *)(base + page_offset(page, page_stride, slot, slot_stride) * elem_bytes);
     };
     for (int i0 = 0; i0 < count; i0 += kAhead) {
         U kept[kAhead], *to[kAhead];
+        int from[kAhead], src_page[kAhead], dst_page[kAhead];
 #pragma unroll
         for (int e = 0; e < kAhead; ++e) {
             const int i = i0 + e;
-            to[e] = nullptr;
-            if (i >= count) continue;
-            const int from = path[i];
-            if (from <= i || from >= added) continue;                // (from == i: it is there)
-            const U *src = place_of(from);
-            if (!src) continue;
-            to[e] = place_of(i);
-            kept[e] = *src;
+            if (i0 > 0) ahead[e] = path[min(i, p.path_len - 1)];
+            // (an entry at its own place is there already)
+            from[e] = i < count && ahead[e] > i && ahead[e] < added ? ahead[e] : -1;
+        }
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            src_page[e] = from[e] < 0 ? -1 : page_at(from[e]);
+            dst_page[e] = from[e] < 0 ? -1 : page_at(i0 + e);
+        }
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            const U *src = piece_at(from[e], src_page[e]);
+            to[e] = src ? piece_at(i0 + e, dst_page[e]) : nullptr;
+            if (to[e]) kept[e] = *src;
         }
 #pragma unroll
         for (int e = 0; e < kAhead; ++e)

@@ -60,32 +60,42 @@ struct Place {
         if (VEC) return turn(0) && !interleaved ? 4 * u + rot / 2 : 8 * u + 4;
         return interleaved ? a(e) + 1 : a(e) + rot / 2;
     }
-    // pair of the table
-    __device__ __forceinline__ int pair(int e) const { return VEC ? 4 * u + e : unit(e); }
-
+    // a row's elements as they lie, so that several rows' loads can be on their way
     template <typename S>
-    __device__ __forceinline__ void load(const S *x, float *lo, float *hi) const
+    struct Raw {
+        vec4<S> a, b;
+    };
+    template <typename S>
+    __device__ __forceinline__ Raw<S> fetch(const S *x) const
     {
+        Raw<S> r = {};
         if constexpr (VEC) {
-            f32x4 fa = {}, fb = {};
             if (has(0)) {
-                fa = __builtin_convertvector(*(const vec4<S> *)(x + a(0)), f32x4);
-                fb = __builtin_convertvector(*(const vec4<S> *)(x + b(0)), f32x4);
-            }
-            const bool mixed = interleaved && turn(0);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                lo[e] = mixed ? (e < 2 ? fa[2 * e] : fb[2 * e - 4]) : fa[e];
-                hi[e] = mixed ? (e < 2 ? fa[2 * e + 1] : fb[2 * e - 3]) : fb[e];
+                r.a = *(const vec4<S> *)(x + a(0));
+                r.b = *(const vec4<S> *)(x + b(0));
             }
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                lo[e] = has(e) ? (float)x[a(e)] : 0.f;
-                hi[e] = has_hi(e) ? (float)x[b(e)] : 0.f;
+                if (has(e)) r.a[e] = x[a(e)];
+                if (has_hi(e)) r.b[e] = x[b(e)];
             }
         }
+        return r;
     }
+    template <typename S>
+    __device__ __forceinline__ void unpack(const Raw<S> &r, float *lo, float *hi) const
+    {
+        const f32x4 fa = __builtin_convertvector(r.a, f32x4), fb = __builtin_convertvector(r.b, f32x4);
+        const bool mixed = VEC && interleaved && turn(0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            lo[e] = mixed ? (e < 2 ? fa[2 * e] : fb[2 * e - 4]) : fa[e];
+            hi[e] = mixed ? (e < 2 ? fa[2 * e + 1] : fb[2 * e - 3]) : fb[e];
+        }
+    }
+    template <typename S>
+    __device__ __forceinline__ void load(const S *x, float *lo, float *hi) const { unpack(fetch(x), lo, hi); }
     template <typename D>
     __device__ __forceinline__ void store(D *y, const float *lo, const float *hi) const
     {
@@ -106,45 +116,49 @@ struct Place {
     }
     __device__ __forceinline__ void load_weight(const void *w, int half, float *lo, float *hi) const
     {
-        if (half) {
-            if constexpr (VEC) {       // (weights lie at any address)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) weight_at((const _Float16 *)w, e, lo, hi);
-            } else {
-                load((const _Float16 *)w, lo, hi);
-            }
-        } else {
-            if constexpr (VEC) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) weight_at((const float *)w, e, lo, hi);
-            } else {
-                load((const float *)w, lo, hi);
-            }
-        }
-    }
-    template <typename W>
-    __device__ __forceinline__ void weight_at(const W *w, int e, float *lo, float *hi) const
-    {
-        const bool mixed = interleaved && turn(0);
-        lo[e] = has(0) ? (float)w[mixed ? 8 * u + 2 * e : a(0) + e] : 0.f;
-        hi[e] = has(0) ? (float)w[mixed ? 8 * u + 2 * e + 1 : b(0) + e] : 0.f;
+        if (half) load((const _Float16 *)w, lo, hi);
+        else load((const float *)w, lo, hi);
     }
     __device__ __forceinline__ void load_angles(const NormParams &p, int position, float *c, float *s) const
     {
         const float *row = p.table + (long long)min(max(position, 0), p.table_rows - 1) * rot;
+        if constexpr (VEC) {
+            f32x4 fc = {1.f, 1.f, 1.f, 1.f}, fs = {};
+            if (turn(0)) {
+                fc = *(const f32x4 *)(row + 4 * u);
+                fs = *(const f32x4 *)(row + rot / 2 + 4 * u);
+            }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            c[e] = turn(e) ? row[pair(e)] : 1.f;
-            s[e] = turn(e) ? row[rot / 2 + pair(e)] : 0.f;
+            for (int e = 0; e < 4; ++e) {
+                c[e] = fc[e];
+                s[e] = fs[e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                c[e] = turn(e) ? row[unit(e)] : 1.f;
+                s[e] = turn(e) ? row[rot / 2 + unit(e)] : 0.f;
+            }
         }
     }
 };
 
+// Sum over the LPH lanes of a group, in all of them.  Up to 16 lanes, a row of
+// the wave, by lane permutations of the additions' operands; beyond by exchanges.
+template <int HOW>
+__device__ __forceinline__ float permuted(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), HOW, 0xf, 0xf, true));
+}
 template <int LPH>
 __device__ __forceinline__ float group_sum(float v)
 {
-#pragma unroll
-    for (int i = 1; i < LPH; i <<= 1) v += __shfl_xor(v, i);
+    v += permuted<0xb1>(v);                 // neighbours: lanes 1 0 3 2
+    v += permuted<0x4e>(v);                 // lanes 2 3 0 1
+    v += permuted<0x141>(v);                // eight lanes mirrored: their halves, alike inside by now
+    if constexpr (LPH >= 16) v += permuted<0x140>(v);   // the row mirrored
+    if constexpr (LPH >= 32) v += __shfl_xor(v, 16);
+    if constexpr (LPH >= 64) v += __shfl_xor(v, 32);
     return v;
 }
 
@@ -166,53 +180,76 @@ norm_rotary_kernel(NormParams p)
         kdst = (D *)p.pool.k + page_offset(page, p.pool.k_page, in, p.pool.k_tok);
         vdst = (D *)p.pool.v + page_offset(page, p.pool.v_page, in, p.pool.v_tok);
     }
-    float c[4], s[4];
+    float c[4], s[4], ql[4], qh[4], kl[4], kh[4];
     if (p.table) at.load_angles(p, p.positions[t], c, s);
+    const bool one_weight = (!p.q_weight || p.qw_head == 0) && (!p.k_weight || p.kw_head == 0);
+    if (one_weight && p.q_weight) at.load_weight(p.q_weight, p.weight_half, ql, qh);
+    if (APPEND && one_weight && p.k_weight) at.load_weight(p.k_weight, p.weight_half, kl, kh);
 
     const int heads = p.q_heads + 2 * p.kv_heads;
     const int first = blockIdx.y * p.heads_per_block, last = min(heads, first + p.heads_per_block);
-    for (int h = first + group; h < last; h += GROUPS) {
-        const S *src;
-        D *dst;
-        const void *weight = nullptr;
-        bool turn = p.table != nullptr;
-        if (!APPEND || h < p.q_heads) {
-            src = (const S *)p.q.p + (long long)t * p.q.tok + (long long)h * p.q.head;
-            dst = (D *)p.qo.p + (long long)t * p.qo.tok + (long long)h * p.qo.head;
-            if (p.q_weight) weight = (const char *)p.q_weight + h * p.qw_head * (p.weight_half ? 2 : 4);
-        } else {
-            const bool is_v = h >= p.q_heads + p.kv_heads;
-            const int kh = h - p.q_heads - (is_v ? p.kv_heads : 0);
-            const HeadRows &rows = is_v ? p.v : p.k;
-            src = (const S *)rows.p + (long long)t * rows.tok + (long long)kh * rows.head;
-            dst = is_v ? vdst + (long long)kh * p.pool.v_head : kdst + (long long)kh * p.pool.k_head;
-            if (p.k_weight && !is_v) weight = (const char *)p.k_weight + kh * p.kw_head * (p.weight_half ? 2 : 4);
-            turn &= !is_v;
-        }
-        float lo[4], hi[4];
-        at.load(src, lo, hi);
-        if (weight) {                                  // (the same in all lanes of a group)
-            float wl[4], wh[4], squares = 0.f;
-            at.load_weight(weight, p.weight_half, wl, wh);
+    // rows of a group whose loads are on their way together
+    constexpr int AHEAD = VEC ? 4 : 1;
+    for (int h0 = first + group; h0 < last; h0 += AHEAD * GROUPS) {
+        typename Place<VEC>::template Raw<S> raw[AHEAD];
+        D *dst[AHEAD];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) squares += lo[e] * lo[e] + hi[e] * hi[e];
-            const float r = norm_scale(p, group_sum<LPH>(squares));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                lo[e] = lo[e] * r * wl[e];
-                hi[e] = hi[e] * r * wh[e];
+        for (int j = 0; j < AHEAD; ++j) {
+            const int h = h0 + j * GROUPS;
+            dst[j] = nullptr;
+            if (h >= last) continue;
+            const S *src;
+            if (!APPEND || h < p.q_heads) {
+                src = (const S *)p.q.p + (long long)t * p.q.tok + (long long)h * p.q.head;
+                dst[j] = (D *)p.qo.p + (long long)t * p.qo.tok + (long long)h * p.qo.head;
+            } else {
+                const bool is_v = h >= p.q_heads + p.kv_heads;
+                const int key_head = h - p.q_heads - (is_v ? p.kv_heads : 0);
+                const HeadRows &rows = is_v ? p.v : p.k;
+                src = (const S *)rows.p + (long long)t * rows.tok + (long long)key_head * rows.head;
+                dst[j] = is_v ? vdst + (long long)key_head * p.pool.v_head : kdst + (long long)key_head * p.pool.k_head;
             }
+            raw[j] = at.fetch(src);
         }
-        if (turn) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (!at.turn(e)) continue;
-                const float l = lo[e], k = hi[e];
-                lo[e] = l * c[e] - k * s[e];
-                hi[e] = k * c[e] + l * s[e];
+        for (int j = 0; j < AHEAD; ++j) {
+            const int h = h0 + j * GROUPS;
+            if (h >= last) continue;                       // (the same in all lanes of a group, as all below)
+            const bool is_q = !APPEND || h < p.q_heads, is_v = APPEND && h >= p.q_heads + p.kv_heads;
+            float lo[4], hi[4];
+            at.unpack(raw[j], lo, hi);
+            if (is_q ? p.q_weight != nullptr : !is_v && p.k_weight) {
+                float wl[4], wh[4], squares = 0.f;
+                if (one_weight) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        wl[e] = is_q ? ql[e] : kl[e];
+                        wh[e] = is_q ? qh[e] : kh[e];
+                    }
+                } else {
+                    const long long element = is_q ? h * p.qw_head : (h - p.q_heads) * p.kw_head;
+                    at.load_weight((const char *)(is_q ? p.q_weight : p.k_weight) + element * (p.weight_half ? 2 : 4), p.weight_half, wl, wh);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) squares += lo[e] * lo[e] + hi[e] * hi[e];
+                const float r = norm_scale(p, group_sum<LPH>(squares));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    lo[e] = lo[e] * r * wl[e];
+                    hi[e] = hi[e] * r * wh[e];
+                }
             }
+            if (p.table && !is_v) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (!at.turn(e)) continue;
+                    const float l = lo[e], k = hi[e];
+                    lo[e] = l * c[e] - k * s[e];
+                    hi[e] = k * c[e] + l * s[e];
+                }
+            }
+            at.store(dst[j], lo, hi);
         }
-        at.store(dst, lo, hi);
     }
 }
 
@@ -230,37 +267,58 @@ norm_rotary_grad_kernel(NormParams p, FastDiv heads)
     float wl[4], wh[4], dl[4] = {}, dh[4] = {};
     if constexpr (PER_HEAD) at.load_weight((const char *)p.q_weight + blockIdx.y * p.qw_head * (p.weight_half ? 2 : 4), p.weight_half, wl, wh);
     else at.load_weight(p.q_weight, p.weight_half, wl, wh);
-    for (long long i = first + group; i < last; i += GROUPS) {
-        const int t = PER_HEAD ? (int)i : heads.quot((int)i), h = PER_HEAD ? blockIdx.y : (int)i - t * p.q_heads;
-        float xl[4], xh[4], gl[4], gh[4], squares = 0.f, dots = 0.f;
-        at.load((const X *)p.q.p + (long long)t * p.q.tok + (long long)h * p.q.head, xl, xh);
-        at.load((const Y *)p.dy.p + (long long)t * p.dy.tok + (long long)h * p.dy.head, gl, gh);
-        if (p.table) {
-            float c[4], s[4];
-            at.load_angles(p, p.positions[t], c, s);
+    constexpr int AHEAD = VEC ? 2 : 1;
+    float c[4], s[4];
+    int angles_of = -1;
+    for (long long i0 = first + group; i0 < last; i0 += AHEAD * GROUPS) {
+        typename Place<VEC>::template Raw<X> x[AHEAD];
+        typename Place<VEC>::template Raw<Y> y[AHEAD];
+        int tok[AHEAD], head[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const long long i = i0 + j * GROUPS;
+            if (i >= last) continue;
+            tok[j] = PER_HEAD ? (int)i : heads.quot((int)i);
+            head[j] = PER_HEAD ? blockIdx.y : (int)i - tok[j] * p.q_heads;
+            x[j] = at.fetch((const X *)p.q.p + (long long)tok[j] * p.q.tok + (long long)head[j] * p.q.head);
+            y[j] = at.fetch((const Y *)p.dy.p + (long long)tok[j] * p.dy.tok + (long long)head[j] * p.dy.head);
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            if (i0 + j * GROUPS >= last) continue;
+            const int t = tok[j], h = head[j];
+            float xl[4], xh[4], gl[4], gh[4], squares = 0.f, dots = 0.f;
+            at.unpack(x[j], xl, xh);
+            at.unpack(y[j], gl, gh);
+            if (p.table) {
+                if (t != angles_of) {
+                    at.load_angles(p, p.positions[t], c, s);
+                    angles_of = t;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (!at.turn(e)) continue;
+                    const float l = gl[e], k = gh[e];
+                    gl[e] = l * c[e] + k * s[e];
+                    gh[e] = k * c[e] - l * s[e];
+                }
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (!at.turn(e)) continue;
-                const float l = gl[e], k = gh[e];
-                gl[e] = l * c[e] + k * s[e];
-                gh[e] = k * c[e] - l * s[e];
+                squares += xl[e] * xl[e] + xh[e] * xh[e];
+                dots += gl[e] * wl[e] * xl[e] + gh[e] * wh[e] * xh[e];
             }
-        }
+            const float r = norm_scale(p, group_sum<LPH>(squares)), m = group_sum<LPH>(dots) * r / (float)p.dim;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            squares += xl[e] * xl[e] + xh[e] * xh[e];
-            dots += gl[e] * wl[e] * xl[e] + gh[e] * wh[e] * xh[e];
+            for (int e = 0; e < 4; ++e) {
+                const float ul = xl[e] * r, uh = xh[e] * r;
+                dl[e] += gl[e] * ul;
+                dh[e] += gh[e] * uh;
+                gl[e] = r * (gl[e] * wl[e] - ul * m);
+                gh[e] = r * (gh[e] * wh[e] - uh * m);
+            }
+            if (p.qo.p) at.store((X *)p.qo.p + (long long)t * p.qo.tok + (long long)h * p.qo.head, gl, gh);
         }
-        const float r = norm_scale(p, group_sum<LPH>(squares)), m = group_sum<LPH>(dots) * r / (float)p.dim;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float ul = xl[e] * r, uh = xh[e] * r;
-            dl[e] += gl[e] * ul;
-            dh[e] += gh[e] * uh;
-            gl[e] = r * (gl[e] * wl[e] - ul * m);
-            gh[e] = r * (gh[e] * wh[e] - uh * m);
-        }
-        if (p.qo.p) at.store((X *)p.qo.p + (long long)t * p.qo.tok + (long long)h * p.qo.head, gl, gh);
     }
     if (!p.dw) return;
     at.store(sums[group], dl, dh);

@@ -16,7 +16,7 @@
 // writing them last, or a second launch does.
 //
 // A tree row's ancestors are found by walking up the parents, of which a workgroup holds
-// its rows' and the kStepWords 32 before them in LDS.
+// its rows' and those as far before them as a mask reaches in LDS.
 #include "serving.h"
 
 namespace nnjit {
@@ -25,27 +25,37 @@ namespace {
 
 enum { kMissing = 1, kLengths = 2, kRows = 4, kPool = 8 };
 
-// Sum of `v` over the threads before this one, and of all; `waves`: THREADS / 64 words of LDS.
+// Three sums over the threads before this one, and over all; and what any thread has in `bad`.  One barrier.
 template <int THREADS>
-__device__ __forceinline__ long long sum_before(long long v, long long *waves, long long &total)
+__device__ __forceinline__ void sums_before(long long (&v)[3], long long (&all)[3], int &bad, long long (*waves)[THREADS / 64], int *flags)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    long long run = v;
 #pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-        const long long up = __shfl_up(run, i);
-        if (lane >= i) run += up;
+    for (int k = 0; k < 3; ++k) {
+        long long run = v[k];
+#pragma unroll
+        for (int i = 1; i < 64; i <<= 1) {
+            const long long up = __shfl_up(run, i);
+            if (lane >= i) run += up;
+        }
+        if (lane == 63) waves[k][wave] = run;
+        v[k] = run - v[k];
     }
-    if (lane == 63) waves[wave] = run;
+    const int any = (__ballot(bad & kLengths) ? kLengths : 0) | (__ballot(bad & kRows) ? kRows : 0);
+    if (lane == 0) flags[wave] = any;
     __syncthreads();
-    long long before = run - v;
-    total = 0;
+    bad = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) {
-        if (w < wave) before += waves[w];
-        total += waves[w];
+    for (int w = 0; w < THREADS / 64; ++w) bad |= flags[w];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        all[k] = 0;
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) {
+            if (w < wave) v[k] += waves[k][w];
+            all[k] += waves[k][w];
+        }
     }
-    return before;
 }
 
 // The last b with sums[b] <= i, 0 <= i < sums[n].
@@ -69,6 +79,7 @@ paged_step_kernel(StepParams p)
     constexpr int N = THREADS * PER, REACH = 32 * kStepWords;
     __shared__ int start[N + 1], back[N + 1], more[N + 1];
     __shared__ long long waves[3][THREADS / 64];
+    __shared__ int flags[THREADS / 64];
     __shared__ int parents[REACH + THREADS];
 
     const int tid = threadIdx.x, n = p.sequences;
@@ -77,7 +88,8 @@ paged_step_kernel(StepParams p)
     auto pages_of = [&](int tokens) { return p.page_size.quot(tokens + page_size - 1); };
 
     int rows_of[PER], delta[PER], bad = 0;
-    long long rows = 0, given = 0, taken = 0;
+    long long sums[3] = {0, 0, 0}, all[3];                   // rows, pages given back, pages taken
+    const int count = p.count[0];
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
         const int b = tid * PER + e;
@@ -91,16 +103,12 @@ paged_step_kernel(StepParams p)
         if (p.parent && added > 32 * p.mask_words) bad |= kRows;
         rows_of[e] = added;
         delta[e] = pages_of(keep + added) - pages_of(held);
-        rows += added;
-        given += max(-delta[e], 0);
-        taken += max(delta[e], 0);
+        sums[0] += added;
+        sums[1] += max(-delta[e], 0);
+        sums[2] += max(delta[e], 0);
     }
-    bad = __syncthreads_or(bad & kLengths ? 1 : 0) * kLengths | __syncthreads_or(bad & kRows ? 1 : 0) * kRows;
-    long long all_rows, all_given, all_taken;
-    const long long rows_before = sum_before<THREADS>(rows, waves[0], all_rows);
-    const long long given_before = sum_before<THREADS>(given, waves[1], all_given);
-    const long long taken_before = sum_before<THREADS>(taken, waves[2], all_taken);
-    const int count = p.count[0];
+    sums_before<THREADS>(sums, all, bad, waves, flags);
+    const long long all_rows = all[0], all_given = all[1], all_taken = all[2];
     if (all_rows > p.tokens) bad |= kRows;
     if (count < 0 || count > p.capacity || count + all_given > p.capacity) bad |= kPool;
     const long long missing = bad & (kLengths | kPool) ? 0 : max(all_taken - all_given - count, 0ll);
@@ -109,7 +117,7 @@ paged_step_kernel(StepParams p)
     const int pages = bad ? 0 : (int)all_taken, pushes = max(left - count, 0);
 
     if constexpr (!FINISH) {
-        int at[3] = {(int)rows_before, (int)given_before, (int)taken_before};
+        int at[3] = {(int)sums[0], (int)sums[1], (int)sums[2]};
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
             const int b = tid * PER + e;
@@ -152,7 +160,7 @@ paged_step_kernel(StepParams p)
             const int t = base + tid;
             if (p.parent) {
                 __syncthreads();
-                for (int i = tid; i < REACH + THREADS; i += THREADS) {
+                for (int i = REACH - 32 * p.mask_words + tid; i < REACH + THREADS; i += THREADS) {
                     const int row = base - REACH + i;
                     parents[i] = row >= 0 && row < end ? p.parent[row] : -1;
                 }

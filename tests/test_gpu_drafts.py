@@ -638,6 +638,25 @@ def test_logits_lengths():
     _logits_case(2, 500, 0)
 
 
+def test_logits_of_long_histories_and_many_biases():
+    """Counts above 2^15, entries above 2^16: the last of them counts."""
+    n, vocab = 70000, 50
+    h = np.full((2, n), 7)
+    h[1, ::2] = 9
+    t = np.full((2, n), -1)
+    t[:, [3, 65537, 69999]] = 9
+    v = np.arange(n, dtype=np.float32)[None, :].repeat(2, axis=0) / 1024
+    x = torch.zeros(2, vocab, device="cuda")
+    r = nj.LogitRules(history=_i32(h), prompt=_i32([1, 0]), frequency=torch.tensor([1.0, 0.5], device="cuda"), presence=torch.ones(2, device="cuda"),
+                      bias_token=_i32(t), bias_value=torch.from_numpy(v).cuda())
+    y = nj.adjust_logits(x, r).cpu()
+    assert y[0, 7] == -(n - 1) - 1 and y[1, 7] == -n / 4 - 1
+    assert y[0, 9] == np.float32(69999 / 1024) and y[1, 9] == np.float32(-n / 4 - 1) + np.float32(69999 / 1024)
+    assert int((y != 0).sum()) == 4
+    r = nj.LogitRules(history=_i32(h[:, :32767]), frequency=torch.ones(2, device="cuda"))
+    assert nj.adjust_logits(x, r).cpu()[0, 7] == -32767
+
+
 def test_logits_that_are_not_finite():
     """Infinities and NaN in places that a mask takes away are gone; elsewhere they stay."""
     x = torch.zeros(1, 64, device="cuda")

@@ -146,6 +146,7 @@ struct StepParams {
     int capacity;
     const int *count;
     int *count_out;
+    int page_groups;           // workgroups that see to the pages (0: a lone one does everything)
 };
 hipError_t launch_paged_step(const StepParams &p, hipStream_t stream);
 
@@ -164,12 +165,12 @@ struct NormParams {
     const void *q_weight, *k_weight;   // NULL: not normed
     long long qw_head, kw_head;
     int weight_half;           // weights are fp16
-    float eps;
-    int heads_per_block;
+    float eps, one_by_dim;
+    int heads_per_block, tokens_per_block;
     // gradients: q holds x, qo dx (p NULL: not wanted)
     HeadRows dy;
     float *dw, *part;          // [groups][dim] partial sums (per head: [groups][heads][dim])
-    int chunk;                 // rows (per head: tokens) of a workgroup
+    int chunk;                 // tokens of a workgroup
 };
 hipError_t launch_norm_rotary(const NormParams &p, bool append, int src_dtype, int dst_dtype, bool vec, hipStream_t stream);
 // Workgroups along the rows that add partial sums of dw: sizes the scratch.

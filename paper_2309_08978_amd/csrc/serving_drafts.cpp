@@ -71,11 +71,12 @@ void set_rotary(NormParams &p, const nnjit_rotary_table *rotary, const int32_t *
     p.interleaved = rotary && rotary->layout == NNJIT_ROTARY_INTERLEAVED;
 }
 
-// weights and angles can be taken four at a time
+// weights and angles can be taken four at a time, and steps from head to head fit 32 bits
 bool norm_in_units(const NormParams &p) {
     const int dtype = p.weight_half ? NNJIT_F16 : NNJIT_F32;
     return (!p.q_weight || in_units(p.q_weight, 0, p.qw_head, 4, dtype)) && (!p.k_weight || in_units(p.k_weight, 0, p.kw_head, 4, dtype)) &&
-           (!p.table || in_units(p.table, 0, 0, 4, NNJIT_F32));
+           (!p.table || in_units(p.table, 0, 0, 4, NNJIT_F32)) &&
+           std::max({p.q.head, p.qo.head, p.k.head, p.v.head, p.dy.head, p.pool.k_head, p.pool.v_head}) <= (long long)0xffffffff;
 }
 
 // what nnjit_norm_rotary and its gradient have in common: *done: nothing is to be done

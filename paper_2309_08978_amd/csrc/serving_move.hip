@@ -6,7 +6,7 @@
 // and moves it for every i, sixteen loads before their stores: no thread
 // touches another's piece, and since later i read at or behind themselves,
 // stores of earlier ones never reach what is still to be read.
-#include "serving.h"
+#include "attention_common.h"
 
 namespace nnjit {
 
@@ -19,7 +19,8 @@ __global__ void __launch_bounds__(kThreads)
 kv_move_kernel(MoveParams p, int elem_bytes)
 {
     const int b = blockIdx.x;
-    const int *path = p.path + (long long)b * p.ld_path;
+    // (what says where things go is the same for all threads: scalar loads)
+    const constant_int *path = (const constant_int *)(p.path + (long long)b * p.ld_path);
     int ahead[kAhead];                                               // asked for before what says how many of them count
 #pragma unroll
     for (int e = 0; e < kAhead; ++e) ahead[e] = path[min(e, p.path_len - 1)];
@@ -29,7 +30,7 @@ kv_move_kernel(MoveParams p, int elem_bytes)
     const long long room = min((long long)batch.table_pages * p.pool.page_size.d, kMaxKeys);
     const long long past = (long long)batch.kv_len[b] - added;      // place of the sequence's new token 0
     const int count = min(max(p.accepted[b], 0), p.path_len);
-    const int *table = batch.page_table + (long long)b * batch.ld_table;
+    const constant_int *table = (const constant_int *)(batch.page_table + (long long)b * batch.ld_table);
 
     const int pieces = p.row_bytes / (int)sizeof(U);                 // of a head's row
     const int piece = blockIdx.y * kThreads + threadIdx.x;

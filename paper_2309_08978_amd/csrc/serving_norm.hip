@@ -16,6 +16,8 @@
 // The weight's gradient is summed in registers over the rows of a workgroup, then over
 // its groups through LDS, then by a second launch over workgroups: in an order
 // that the sizes alone decide.
+#include <type_traits>
+
 #include "kcommon.h"
 #include "serving.h"
 #include "nnjit.h"
@@ -30,36 +32,43 @@ using vec4 = T __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256;
 
 // Where a lane's eight elements lie: lo[e] at a(e), hi[e] at b(e), the sides of a
-// pair where turned.  VEC: e neighbours; else unit u + 64 e of a row of pairs and, behind
-// them, single elements (hi[e] is then none).
-template <bool VEC>
+// pair where turned.  HALF, PAIRS (the two layouts): e are neighbours; ANY (either layout, any address): unit
+// u + 64 e of a row of pairs and, behind them, single elements (hi[e] is then none).
+enum { HALF, PAIRS, ANY };
+
+template <int HOW>
 struct Place {
-    int u, units, turned, rot, dim, interleaved;
+    static constexpr bool VEC = HOW != ANY;
+    int u, units, turned, rot, interleaved;
+    bool mine;                 // VEC: the row has elements for this lane (else it loads the last ones', and stores none)
     __device__ __forceinline__ Place(const NormParams &p, int lane)
     {
-        u = lane;
         rot = p.table ? p.rot : 0;
-        dim = p.dim;
         interleaved = p.interleaved;
         turned = VEC ? rot / 8 : rot / 2;
-        units = VEC ? dim / 8 : turned + dim - rot;
+        units = VEC ? p.dim / 8 : turned + p.dim - rot;
+        mine = lane < units;
+        u = VEC ? min(lane, units - 1) : lane;
     }
     __device__ __forceinline__ int unit(int e) const { return VEC ? u : u + 64 * e; }
-    __device__ __forceinline__ bool has(int e) const { return unit(e) < units; }
+    __device__ __forceinline__ bool has(int e) const { return VEC || unit(e) < units; }
     __device__ __forceinline__ bool turn(int e) const { return unit(e) < turned; }
-    __device__ __forceinline__ bool has_hi(int e) const { return VEC ? has(e) : turn(e); }
+    __device__ __forceinline__ bool has_hi(int e) const { return VEC || turn(e); }
     // VEC: first elements of the two runs of four; else the elements themselves
     __device__ __forceinline__ int a(int e) const
     {
-        if (VEC) return turn(0) ? (interleaved ? 8 * u : 4 * u) : 8 * u;       // (rot = 8 turned)
+        if (HOW == HALF) return turn(0) ? 4 * u : 8 * u;                       // (rot = 8 turned)
+        if (HOW == PAIRS) return 8 * u;
         const int i = unit(e);
         return turn(e) ? (interleaved ? 2 * i : i) : rot + i - turned;
     }
     __device__ __forceinline__ int b(int e) const
     {
-        if (VEC) return turn(0) && !interleaved ? 4 * u + rot / 2 : 8 * u + 4;
+        if (HOW == HALF) return turn(0) ? 4 * u + rot / 2 : 8 * u + 4;
+        if (HOW == PAIRS) return 8 * u + 4;
         return interleaved ? a(e) + 1 : a(e) + rot / 2;
     }
+
     // a row's elements as they lie, so that several rows' loads can be on their way
     template <typename S>
     struct Raw {
@@ -68,17 +77,15 @@ struct Place {
     template <typename S>
     __device__ __forceinline__ Raw<S> fetch(const S *x) const
     {
-        Raw<S> r = {};
+        Raw<S> r;
         if constexpr (VEC) {
-            if (has(0)) {
-                r.a = *(const vec4<S> *)(x + a(0));
-                r.b = *(const vec4<S> *)(x + b(0));
-            }
+            r.a = *(const vec4<S> *)(x + a(0));
+            r.b = *(const vec4<S> *)(x + b(0));
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (has(e)) r.a[e] = x[a(e)];
-                if (has_hi(e)) r.b[e] = x[b(e)];
+                r.a[e] = has(e) ? x[a(e)] : (S)0;
+                r.b[e] = has_hi(e) ? x[b(e)] : (S)0;
             }
         }
         return r;
@@ -87,11 +94,10 @@ struct Place {
     __device__ __forceinline__ void unpack(const Raw<S> &r, float *lo, float *hi) const
     {
         const f32x4 fa = __builtin_convertvector(r.a, f32x4), fb = __builtin_convertvector(r.b, f32x4);
-        const bool mixed = VEC && interleaved && turn(0);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            lo[e] = mixed ? (e < 2 ? fa[2 * e] : fb[2 * e - 4]) : fa[e];
-            hi[e] = mixed ? (e < 2 ? fa[2 * e + 1] : fb[2 * e - 3]) : fb[e];
+            lo[e] = HOW == PAIRS ? (e < 2 ? fa[2 * e & 3] : fb[2 * e & 3]) : fa[e];
+            hi[e] = HOW == PAIRS ? (e < 2 ? fa[(2 * e + 1) & 3] : fb[(2 * e + 1) & 3]) : fb[e];
         }
     }
     template <typename S>
@@ -100,10 +106,9 @@ struct Place {
     __device__ __forceinline__ void store(D *y, const float *lo, const float *hi) const
     {
         if constexpr (VEC) {
-            if (!has(0)) return;
-            const bool mixed = interleaved && turn(0);
-            const f32x4 fa = mixed ? f32x4{lo[0], hi[0], lo[1], hi[1]} : f32x4{lo[0], lo[1], lo[2], lo[3]};
-            const f32x4 fb = mixed ? f32x4{lo[2], hi[2], lo[3], hi[3]} : f32x4{hi[0], hi[1], hi[2], hi[3]};
+            const f32x4 fa = HOW == PAIRS ? f32x4{lo[0], hi[0], lo[1], hi[1]} : f32x4{lo[0], lo[1], lo[2], lo[3]};
+            const f32x4 fb = HOW == PAIRS ? f32x4{lo[2], hi[2], lo[3], hi[3]} : f32x4{hi[0], hi[1], hi[2], hi[3]};
+            if (!mine) return;
             *(vec4<D> *)(y + a(0)) = __builtin_convertvector(fa, vec4<D>);
             *(vec4<D> *)(y + b(0)) = __builtin_convertvector(fb, vec4<D>);
         } else {
@@ -114,20 +119,17 @@ struct Place {
             }
         }
     }
-    __device__ __forceinline__ void load_weight(const void *w, int half, float *lo, float *hi) const
+    __device__ __forceinline__ void load_weight(const void *w, long long element, int half, float *lo, float *hi) const
     {
-        if (half) load((const _Float16 *)w, lo, hi);
-        else load((const float *)w, lo, hi);
+        if (half) load((const _Float16 *)w + element, lo, hi);
+        else load((const float *)w + element, lo, hi);
     }
     __device__ __forceinline__ void load_angles(const NormParams &p, int position, float *c, float *s) const
     {
         const float *row = p.table + (long long)min(max(position, 0), p.table_rows - 1) * rot;
         if constexpr (VEC) {
-            f32x4 fc = {1.f, 1.f, 1.f, 1.f}, fs = {};
-            if (turn(0)) {
-                fc = *(const f32x4 *)(row + 4 * u);
-                fs = *(const f32x4 *)(row + rot / 2 + 4 * u);
-            }
+            if (!turn(0)) return;
+            const f32x4 fc = *(const f32x4 *)(row + 4 * u), fs = *(const f32x4 *)(row + rot / 2 + 4 * u);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 c[e] = fc[e];
@@ -141,6 +143,21 @@ struct Place {
             }
         }
     }
+    // lo, hi turned by the angles, or (BACK) by the opposite ones
+    template <bool BACK>
+    __device__ __forceinline__ void rotate(float *lo, float *hi, const float *c, const float *s) const
+    {
+        if (VEC && !turn(0)) return;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (!VEC && !turn(e)) continue;
+            const float l = lo[e], k = hi[e];
+            lo[e] = BACK ? l * c[e] + k * s[e] : l * c[e] - k * s[e];
+            hi[e] = BACK ? k * c[e] - l * s[e] : k * c[e] + l * s[e];
+        }
+    }
+    // a lane's part of a row's sum
+    __device__ __forceinline__ float part(float sum) const { return !VEC || mine ? sum : 0.f; }
 };
 
 // Sum over the LPH lanes of a group, in all of them.  Up to 16 lanes, a row of
@@ -162,64 +179,75 @@ __device__ __forceinline__ float group_sum(float v)
     return v;
 }
 
-__device__ __forceinline__ float norm_scale(const NormParams &p, float squares) { return rsqrtf(squares / (float)p.dim + p.eps); }
+__device__ __forceinline__ float norm_scale(const NormParams &p, float squares) { return rsqrtf(squares * p.one_by_dim + p.eps); }
 
-template <typename S, typename D, bool APPEND, bool VEC, int LPH>
+// row h of strided ones (strides of rows taken eight elements a lane are below 2^32)
+template <bool VEC, typename T>
+__device__ __forceinline__ T *row_of(T *base, int h, long long stride)
+{
+    return base + (VEC ? (unsigned long long)(unsigned)h * (unsigned)stride : (unsigned long long)(h * stride));
+}
+
+// A workgroup takes p.tokens_per_block tokens (a power of two), its groups split evenly among
+// them, so that a group has a few heads of one token: their loads are on their
+// way together, and angles are read once.
+template <typename S, typename D, bool APPEND, int HOW, int LPH>
 __global__ void __launch_bounds__(kThreads)
 norm_rotary_kernel(NormParams p)
 {
     constexpr int GROUPS = kThreads / LPH;
-    const int t = blockIdx.x, group = threadIdx.x / LPH;
-    const Place<VEC> at(p, threadIdx.x % LPH);
+    const int groups = GROUPS / p.tokens_per_block;         // of a token
+    const int in_block = threadIdx.x / LPH / groups, group = threadIdx.x / LPH % groups;
+    const int t = min((int)blockIdx.x * p.tokens_per_block + in_block, p.tokens - 1);
+    bool live = (int)blockIdx.x * p.tokens_per_block + in_block < p.tokens;
+    constexpr bool VEC = HOW != ANY;
+    const Place<HOW> at(p, threadIdx.x % LPH);
     D *kdst = nullptr, *vdst = nullptr;
     if constexpr (APPEND) {
+        // (rows that are left alone are read and normed all the same: no load waits for the slot)
         const long long slot = p.slots[t];
-        if (slot < 0 || slot >= (long long)p.pool.pages * p.pool.page_size.d) return;
+        live &= slot >= 0 && slot < (long long)p.pool.pages * p.pool.page_size.d;
         const unsigned page_size = p.pool.page_size.d;
-        const int page = (int)(slot / page_size), in = (int)(slot - (long long)page * page_size);
+        const int page = live ? (int)(slot / page_size) : 0, in = live ? (int)(slot - (long long)page * page_size) : 0;
         kdst = (D *)p.pool.k + page_offset(page, p.pool.k_page, in, p.pool.k_tok);
         vdst = (D *)p.pool.v + page_offset(page, p.pool.v_page, in, p.pool.v_tok);
     }
     float c[4], s[4], ql[4], qh[4], kl[4], kh[4];
     if (p.table) at.load_angles(p, p.positions[t], c, s);
     const bool one_weight = (!p.q_weight || p.qw_head == 0) && (!p.k_weight || p.kw_head == 0);
-    if (one_weight && p.q_weight) at.load_weight(p.q_weight, p.weight_half, ql, qh);
-    if (APPEND && one_weight && p.k_weight) at.load_weight(p.k_weight, p.weight_half, kl, kh);
+    if (one_weight && p.q_weight) at.load_weight(p.q_weight, 0, p.weight_half, ql, qh);
+    if (APPEND && one_weight && p.k_weight) at.load_weight(p.k_weight, 0, p.weight_half, kl, kh);
 
+    const S *q_src = (const S *)p.q.p + (long long)t * p.q.tok;
+    D *q_dst = (D *)p.qo.p + (long long)t * p.qo.tok;
+    const S *k_src = APPEND ? (const S *)p.k.p + (long long)t * p.k.tok : nullptr, *v_src = APPEND ? (const S *)p.v.p + (long long)t * p.v.tok : nullptr;
     const int heads = p.q_heads + 2 * p.kv_heads;
     const int first = blockIdx.y * p.heads_per_block, last = min(heads, first + p.heads_per_block);
     // rows of a group whose loads are on their way together
     constexpr int AHEAD = VEC ? 4 : 1;
-    for (int h0 = first + group; h0 < last; h0 += AHEAD * GROUPS) {
-        typename Place<VEC>::template Raw<S> raw[AHEAD];
-        D *dst[AHEAD];
+    for (int h0 = first + group; h0 < last; h0 += AHEAD * groups) {
+        typename Place<HOW>::template Raw<S> raw[AHEAD];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
-            const int h = h0 + j * GROUPS;
-            dst[j] = nullptr;
+            const int h = h0 + j * groups;
             if (h >= last) continue;
-            const S *src;
-            if (!APPEND || h < p.q_heads) {
-                src = (const S *)p.q.p + (long long)t * p.q.tok + (long long)h * p.q.head;
-                dst[j] = (D *)p.qo.p + (long long)t * p.qo.tok + (long long)h * p.qo.head;
-            } else {
-                const bool is_v = h >= p.q_heads + p.kv_heads;
-                const int key_head = h - p.q_heads - (is_v ? p.kv_heads : 0);
-                const HeadRows &rows = is_v ? p.v : p.k;
-                src = (const S *)rows.p + (long long)t * rows.tok + (long long)key_head * rows.head;
-                dst[j] = is_v ? vdst + (long long)key_head * p.pool.v_head : kdst + (long long)key_head * p.pool.k_head;
-            }
-            raw[j] = at.fetch(src);
+            const bool is_q = !APPEND || h < p.q_heads, is_v = APPEND && h >= p.q_heads + p.kv_heads;
+            const int of = is_q ? h : h - p.q_heads - (is_v ? p.kv_heads : 0);
+            raw[j] = at.fetch(row_of<VEC>(is_q ? q_src : is_v ? v_src : k_src, of, is_q ? p.q.head : is_v ? p.v.head : p.k.head));
         }
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
-            const int h = h0 + j * GROUPS;
+            const int h = h0 + j * groups;
             if (h >= last) continue;                       // (the same in all lanes of a group, as all below)
             const bool is_q = !APPEND || h < p.q_heads, is_v = APPEND && h >= p.q_heads + p.kv_heads;
+            const int of = is_q ? h : h - p.q_heads - (is_v ? p.kv_heads : 0);
             float lo[4], hi[4];
             at.unpack(raw[j], lo, hi);
             if (is_q ? p.q_weight != nullptr : !is_v && p.k_weight) {
                 float wl[4], wh[4], squares = 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) squares += lo[e] * lo[e] + hi[e] * hi[e];
+                const float r = norm_scale(p, group_sum<LPH>(at.part(squares)));
                 if (one_weight) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -227,108 +255,95 @@ norm_rotary_kernel(NormParams p)
                         wh[e] = is_q ? qh[e] : kh[e];
                     }
                 } else {
-                    const long long element = is_q ? h * p.qw_head : (h - p.q_heads) * p.kw_head;
-                    at.load_weight((const char *)(is_q ? p.q_weight : p.k_weight) + element * (p.weight_half ? 2 : 4), p.weight_half, wl, wh);
+                    at.load_weight(is_q ? p.q_weight : p.k_weight, of * (is_q ? p.qw_head : p.kw_head), p.weight_half, wl, wh);
                 }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) squares += lo[e] * lo[e] + hi[e] * hi[e];
-                const float r = norm_scale(p, group_sum<LPH>(squares));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     lo[e] = lo[e] * r * wl[e];
                     hi[e] = hi[e] * r * wh[e];
                 }
             }
-            if (p.table && !is_v) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (!at.turn(e)) continue;
-                    const float l = lo[e], k = hi[e];
-                    lo[e] = l * c[e] - k * s[e];
-                    hi[e] = k * c[e] + l * s[e];
-                }
-            }
-            at.store(dst[j], lo, hi);
+            if (p.table && !is_v) at.template rotate<false>(lo, hi, c, s);
+            if (live) at.store(row_of<VEC>(is_q ? q_dst : is_v ? vdst : kdst, of, is_q ? p.qo.head : is_v ? p.pool.v_head : p.pool.k_head), lo, hi);
         }
     }
 }
 
-// PER_HEAD: blockIdx.y is a head, rows are its tokens; else rows are all heads of all tokens.
-template <typename X, typename Y, bool PER_HEAD, bool VEC, int LPH>
-__global__ void __launch_bounds__(kThreads)
-norm_rotary_grad_kernel(NormParams p, FastDiv heads)
+constexpr int kGradThreads = 512;
+
+// A workgroup takes a run of p.chunk tokens, p.tokens_per_block at a time, its groups split
+// among them as in the forward pass.  PER_HEAD: p.heads_per_block heads (from blockIdx.y's first on), each
+// group always the same one, so that its sum is that head's.
+template <typename X, typename Y, bool PER_HEAD, int HOW, int LPH>
+__global__ void __launch_bounds__(kGradThreads)
+norm_rotary_grad_kernel(NormParams p)
 {
-    constexpr int GROUPS = kThreads / LPH;
+    constexpr int GROUPS = kGradThreads / LPH;
     __shared__ __attribute__((aligned(16))) float sums[GROUPS][LPH * 8];
-    const int group = threadIdx.x / LPH, lane = threadIdx.x % LPH;
-    const Place<VEC> at(p, lane);
-    const long long all = PER_HEAD ? p.tokens : (long long)p.tokens * p.q_heads;
-    const long long first = (long long)blockIdx.x * p.chunk, last = min(all, first + p.chunk);
+    const int lane = threadIdx.x % LPH, groups = GROUPS / p.tokens_per_block;       // of a token
+    const int in_block = threadIdx.x / LPH / groups, group = threadIdx.x / LPH % groups;
+    constexpr bool VEC = HOW != ANY;
+    const Place<HOW> at(p, lane);
+    const int h_first = PER_HEAD ? blockIdx.y * p.heads_per_block : 0;
+    const int h_last = PER_HEAD ? min(h_first + p.heads_per_block, p.q_heads) : p.q_heads;
     float wl[4], wh[4], dl[4] = {}, dh[4] = {};
-    if constexpr (PER_HEAD) at.load_weight((const char *)p.q_weight + blockIdx.y * p.qw_head * (p.weight_half ? 2 : 4), p.weight_half, wl, wh);
-    else at.load_weight(p.q_weight, p.weight_half, wl, wh);
-    constexpr int AHEAD = VEC ? 2 : 1;
-    float c[4], s[4];
-    int angles_of = -1;
-    for (long long i0 = first + group; i0 < last; i0 += AHEAD * GROUPS) {
-        typename Place<VEC>::template Raw<X> x[AHEAD];
-        typename Place<VEC>::template Raw<Y> y[AHEAD];
-        int tok[AHEAD], head[AHEAD];
+    const int w_head = PER_HEAD ? min(h_first + group, h_last - 1) : 0;
+    at.load_weight(p.q_weight, w_head * p.qw_head, p.weight_half, wl, wh);
+
+    constexpr int AHEAD = VEC && !PER_HEAD ? 4 : 1;
+    const int first = blockIdx.x * p.chunk, last = min(p.tokens, first + p.chunk);
+    for (int t = first + in_block; t < last; t += p.tokens_per_block) {
+        float c[4], s[4];
+        if (p.table) at.load_angles(p, p.positions[t], c, s);
+        const X *x_row = (const X *)p.q.p + (long long)t * p.q.tok;
+        const Y *y_row = (const Y *)p.dy.p + (long long)t * p.dy.tok;
+        X *dx_row = (X *)p.qo.p + (long long)t * p.qo.tok;
+        for (int h0 = h_first + group; h0 < h_last; h0 += AHEAD * groups) {
+            typename Place<HOW>::template Raw<X> x[AHEAD];
+            typename Place<HOW>::template Raw<Y> y[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            const long long i = i0 + j * GROUPS;
-            if (i >= last) continue;
-            tok[j] = PER_HEAD ? (int)i : heads.quot((int)i);
-            head[j] = PER_HEAD ? blockIdx.y : (int)i - tok[j] * p.q_heads;
-            x[j] = at.fetch((const X *)p.q.p + (long long)tok[j] * p.q.tok + (long long)head[j] * p.q.head);
-            y[j] = at.fetch((const Y *)p.dy.p + (long long)tok[j] * p.dy.tok + (long long)head[j] * p.dy.head);
-        }
+            for (int j = 0; j < AHEAD; ++j) {
+                const int h = h0 + j * groups;
+                if (h >= h_last) continue;
+                x[j] = at.fetch(row_of<VEC>(x_row, h, p.q.head));
+                y[j] = at.fetch(row_of<VEC>(y_row, h, p.dy.head));
+            }
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            if (i0 + j * GROUPS >= last) continue;
-            const int t = tok[j], h = head[j];
-            float xl[4], xh[4], gl[4], gh[4], squares = 0.f, dots = 0.f;
-            at.unpack(x[j], xl, xh);
-            at.unpack(y[j], gl, gh);
-            if (p.table) {
-                if (t != angles_of) {
-                    at.load_angles(p, p.positions[t], c, s);
-                    angles_of = t;
-                }
+            for (int j = 0; j < AHEAD; ++j) {
+                const int h = h0 + j * groups;
+                if (h >= h_last) continue;                 // (the same in all lanes of a group)
+                float xl[4], xh[4], gl[4], gh[4], squares = 0.f, dots = 0.f;
+                at.unpack(x[j], xl, xh);
+                at.unpack(y[j], gl, gh);
+                if (p.table) at.template rotate<true>(gl, gh, c, s);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if (!at.turn(e)) continue;
-                    const float l = gl[e], k = gh[e];
-                    gl[e] = l * c[e] + k * s[e];
-                    gh[e] = k * c[e] - l * s[e];
+                    squares += xl[e] * xl[e] + xh[e] * xh[e];
+                    dots += gl[e] * wl[e] * xl[e] + gh[e] * wh[e] * xh[e];
                 }
-            }
+                const float r = norm_scale(p, group_sum<LPH>(at.part(squares))), m = group_sum<LPH>(at.part(dots)) * r * p.one_by_dim;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                squares += xl[e] * xl[e] + xh[e] * xh[e];
-                dots += gl[e] * wl[e] * xl[e] + gh[e] * wh[e] * xh[e];
+                for (int e = 0; e < 4; ++e) {
+                    const float ul = xl[e] * r, uh = xh[e] * r;
+                    dl[e] += gl[e] * ul;
+                    dh[e] += gh[e] * uh;
+                    gl[e] = r * (gl[e] * wl[e] - ul * m);
+                    gh[e] = r * (gh[e] * wh[e] - uh * m);
+                }
+                if (p.qo.p) at.store(row_of<VEC>(dx_row, h, p.qo.head), gl, gh);
             }
-            const float r = norm_scale(p, group_sum<LPH>(squares)), m = group_sum<LPH>(dots) * r / (float)p.dim;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float ul = xl[e] * r, uh = xh[e] * r;
-                dl[e] += gl[e] * ul;
-                dh[e] += gh[e] * uh;
-                gl[e] = r * (gl[e] * wl[e] - ul * m);
-                gh[e] = r * (gh[e] * wh[e] - uh * m);
-            }
-            if (p.qo.p) at.store((X *)p.qo.p + (long long)t * p.qo.tok + (long long)h * p.qo.head, gl, gh);
         }
     }
     if (!p.dw) return;
-    at.store(sums[group], dl, dh);
+    at.store(sums[threadIdx.x / LPH], dl, dh);
     __syncthreads();
-    float *part = p.part + ((long long)blockIdx.x * (PER_HEAD ? p.q_heads : 1) + (PER_HEAD ? blockIdx.y : 0)) * p.dim;
-    for (int i = threadIdx.x; i < p.dim; i += kThreads) {
+    // per head: group g of every token is head h_first + g
+    const int out = PER_HEAD ? h_last - h_first : 1;
+    for (int i = threadIdx.x; i < out * p.dim; i += kGradThreads) {
+        const int g0 = PER_HEAD ? i / p.dim : 0, d = i - g0 * p.dim;
         float sum = 0.f;
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) sum += sums[g][i];
-        part[i] = sum;
+        for (int g = g0; g < GROUPS; g += PER_HEAD ? groups : 1) sum += sums[g][d];
+        p.part[((long long)blockIdx.x * (PER_HEAD ? p.q_heads : 1) + h_first + g0) * p.dim + d] = sum;
     }
 }
 
@@ -341,7 +356,7 @@ sum_parts_kernel(const float *part, float *dw, int groups, long long n)
     const long long i = (long long)blockIdx.x * 32 + col;
     float sum = 0.f;
     if (i < n) {
-#pragma unroll 4
+#pragma unroll 8
         for (int g = slice; g < groups; g += 32) sum += part[g * n + i];
     }
     sums[slice][col] = sum;
@@ -356,15 +371,26 @@ sum_parts_kernel(const float *part, float *dw, int groups, long long n)
 
 int lanes_per_head(int dim, bool vec) { return !vec ? 64 : dim <= 64 ? 8 : dim <= 128 ? 16 : 32; }
 
+// launch(how, lanes) with both as constants
+template <typename F>
+void pick(const NormParams &p, bool vec, F launch)
+{
+    using std::integral_constant;
+    const int lanes = lanes_per_head(p.dim, vec);
+    auto of = [&](auto how) {
+        if (lanes == 8) launch(how, integral_constant<int, 8>{});
+        else if (lanes == 16) launch(how, integral_constant<int, 16>{});
+        else launch(how, integral_constant<int, 32>{});
+    };
+    if (!vec) launch(integral_constant<int, ANY>{}, integral_constant<int, 64>{});
+    else if (p.interleaved) of(integral_constant<int, PAIRS>{});
+    else of(integral_constant<int, HALF>{});
+}
+
 template <typename S, typename D, bool APPEND>
 hipError_t launch_as(const NormParams &p, bool vec, dim3 grid, hipStream_t stream)
 {
-    switch (lanes_per_head(p.dim, vec)) {
-    case 8: norm_rotary_kernel<S, D, APPEND, true, 8><<<grid, kThreads, 0, stream>>>(p); break;
-    case 16: norm_rotary_kernel<S, D, APPEND, true, 16><<<grid, kThreads, 0, stream>>>(p); break;
-    case 32: norm_rotary_kernel<S, D, APPEND, true, 32><<<grid, kThreads, 0, stream>>>(p); break;
-    default: norm_rotary_kernel<S, D, APPEND, false, 64><<<grid, kThreads, 0, stream>>>(p);
-    }
+    pick(p, vec, [&](auto how, auto lanes) { norm_rotary_kernel<S, D, APPEND, how(), lanes()><<<grid, kThreads, 0, stream>>>(p); });
     return hipGetLastError();
 }
 
@@ -377,21 +403,32 @@ hipError_t launch_typed(const NormParams &p, bool append, bool vec, dim3 grid, h
 template <typename X, typename Y, bool PER_HEAD>
 hipError_t launch_grad_as(const NormParams &p, bool vec, dim3 grid, hipStream_t stream)
 {
-    const FastDiv heads((unsigned)p.q_heads);
-    switch (lanes_per_head(p.dim, vec)) {
-    case 8: norm_rotary_grad_kernel<X, Y, PER_HEAD, true, 8><<<grid, kThreads, 0, stream>>>(p, heads); break;
-    case 16: norm_rotary_grad_kernel<X, Y, PER_HEAD, true, 16><<<grid, kThreads, 0, stream>>>(p, heads); break;
-    case 32: norm_rotary_grad_kernel<X, Y, PER_HEAD, true, 32><<<grid, kThreads, 0, stream>>>(p, heads); break;
-    default: norm_rotary_grad_kernel<X, Y, PER_HEAD, false, 64><<<grid, kThreads, 0, stream>>>(p, heads);
-    }
+    pick(p, vec, [&](auto how, auto lanes) { norm_rotary_grad_kernel<X, Y, PER_HEAD, how(), lanes()><<<grid, kGradThreads, 0, stream>>>(p); });
     return hipGetLastError();
 }
 
 template <typename X, typename Y>
 hipError_t launch_grad_typed(const NormParams &p, bool vec, int groups, hipStream_t stream)
 {
-    return p.qw_head > 0 ? launch_grad_as<X, Y, true>(p, vec, dim3((unsigned)groups, (unsigned)p.q_heads), stream)
+    const unsigned blocks = (unsigned)((p.q_heads + p.heads_per_block - 1) / p.heads_per_block);
+    return p.qw_head > 0 ? launch_grad_as<X, Y, true>(p, vec, dim3((unsigned)groups, blocks), stream)
                          : launch_grad_as<X, Y, false>(p, vec, dim3((unsigned)groups), stream);
+}
+
+// Tokens that the groups of a workgroup are split among: about four heads a group.
+int tokens_per_block(int groups, int heads)
+{
+    int t = 1;
+    while (2 * t <= groups && groups / (2 * t) * 4 >= heads) t *= 2;
+    return t;
+}
+
+// ... per head: a group a head, if there are so many groups
+int tokens_per_block_of_heads(int groups, int heads)
+{
+    int t = 1;
+    while (2 * t <= groups && groups / (2 * t) >= heads) t *= 2;
+    return t;
 }
 
 }  // namespace
@@ -399,12 +436,14 @@ hipError_t launch_grad_typed(const NormParams &p, bool vec, int groups, hipStrea
 hipError_t launch_norm_rotary(const NormParams &in, bool append, int src_dtype, int dst_dtype, bool vec, hipStream_t stream)
 {
     NormParams p = in;
-    const int heads = p.q_heads + 2 * p.kv_heads, rows = kThreads / lanes_per_head(p.dim, vec);
+    p.one_by_dim = 1.f / (float)p.dim;
+    const int heads = p.q_heads + 2 * p.kv_heads, groups = kThreads / lanes_per_head(p.dim, vec);
     // few tokens: their heads are spread over workgroups until about four a compute unit are there
-    const int most = (heads + rows - 1) / rows, want = (1024 + p.tokens - 1) / p.tokens, blocks = want < most ? want : most;
+    const int most = (heads + groups - 1) / groups, want = (1024 + p.tokens - 1) / p.tokens, blocks = want < most ? want : most;
     p.heads_per_block = (heads + blocks - 1) / blocks;
-    p.heads_per_block = (p.heads_per_block + rows - 1) / rows * rows;
-    const dim3 grid((unsigned)p.tokens, (unsigned)((heads + p.heads_per_block - 1) / p.heads_per_block));
+    p.heads_per_block = (p.heads_per_block + groups - 1) / groups * groups;
+    p.tokens_per_block = blocks == 1 && p.tokens >= 1024 ? tokens_per_block(groups, heads) : 1;
+    const dim3 grid((unsigned)((p.tokens + p.tokens_per_block - 1) / p.tokens_per_block), (unsigned)((heads + p.heads_per_block - 1) / p.heads_per_block));
     if (src_dtype == NNJIT_F32)
         return dst_dtype == NNJIT_F32 ? launch_typed<float, float>(p, append, vec, grid, stream)
                                       : launch_typed<float, _Float16>(p, append, vec, grid, stream);
@@ -414,16 +453,21 @@ hipError_t launch_norm_rotary(const NormParams &in, bool append, int src_dtype, 
 
 int norm_grad_groups(int64_t tokens, int64_t heads, int dim, bool per_head, bool vec, int cus)
 {
-    const int64_t rows = per_head ? tokens : tokens * heads, at_once = kThreads / lanes_per_head(dim, vec);
-    const int64_t want = (rows + at_once - 1) / at_once, most = per_head ? (4 * cus + heads - 1) / heads : 4 * cus;
-    return (int)(want < 1 ? 1 : want < most ? want : most);      // (no rows: one adds up nothing)
+    const int groups = kGradThreads / lanes_per_head(dim, vec);
+    const int64_t at_once = per_head ? tokens_per_block_of_heads(groups, (int)heads) : tokens_per_block(groups, (int)heads);
+    const int64_t blocks = per_head ? (heads * at_once + groups - 1) / groups : 1;           // of heads
+    const int64_t want = (tokens + at_once - 1) / at_once, most = (2 * cus + blocks - 1) / blocks;
+    return (int)(want < 1 ? 1 : want < most ? want : most);      // (no tokens: one adds up nothing)
 }
 
 hipError_t launch_norm_rotary_grad(const NormParams &in, int x_dtype, int dy_dtype, bool vec, int groups, hipStream_t stream)
 {
     NormParams p = in;
-    const long long rows = p.qw_head > 0 ? p.tokens : (long long)p.tokens * p.q_heads;
-    p.chunk = (int)((rows + groups - 1) / groups);
+    p.one_by_dim = 1.f / (float)p.dim;
+    const int at_once = kGradThreads / lanes_per_head(p.dim, vec);
+    p.tokens_per_block = p.qw_head > 0 ? tokens_per_block_of_heads(at_once, p.q_heads) : tokens_per_block(at_once, p.q_heads);
+    p.heads_per_block = at_once / p.tokens_per_block;
+    p.chunk = (p.tokens + groups - 1) / groups;
     hipError_t e;
     if (x_dtype == NNJIT_F32)
         e = dy_dtype == NNJIT_F32 ? launch_grad_typed<float, float>(p, vec, groups, stream) : launch_grad_typed<float, _Float16>(p, vec, groups, stream);

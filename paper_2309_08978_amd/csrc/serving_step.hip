@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(THREADS)
 paged_step_kernel(StepParams p)
 {
     constexpr int N = THREADS * PER, REACH = 32 * kStepWords;
-    __shared__ int start[N + 1], back[N + 1], more[N + 1];
+    __shared__ int start[N + 1], back[N + 1], more[N + 1], old_pages[N];
     __shared__ long long waves[3][THREADS / 64];
     __shared__ int flags[THREADS / 64];
     __shared__ int parents[REACH + THREADS];
@@ -87,13 +87,13 @@ paged_step_kernel(StepParams p)
     const long long room = min((long long)p.table_pages * page_size, kMaxKeys);
     auto pages_of = [&](int tokens) { return p.page_size.quot(tokens + page_size - 1); };
 
-    int rows_of[PER], delta[PER], bad = 0;
+    int rows_of[PER], delta[PER], old_of[PER], bad = 0;
     long long sums[3] = {0, 0, 0}, all[3];                   // rows, pages given back, pages taken
     const int count = p.count[0];
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
         const int b = tid * PER + e;
-        rows_of[e] = delta[e] = 0;
+        rows_of[e] = delta[e] = old_of[e] = 0;
         if (b >= n) continue;
         const int held = p.held[b], keep = p.keep ? p.keep[b] : held, added = p.added[b];
         if (held < 0 || keep < 0 || keep > held || added < 0 || held > room || (long long)keep + added > room) {
@@ -102,7 +102,8 @@ paged_step_kernel(StepParams p)
         }
         if (p.parent && added > 32 * p.mask_words) bad |= kRows;
         rows_of[e] = added;
-        delta[e] = pages_of(keep + added) - pages_of(held);
+        old_of[e] = pages_of(held);
+        delta[e] = pages_of(keep + added) - old_of[e];
         sums[0] += added;
         sums[1] += max(-delta[e], 0);
         sums[2] += max(delta[e], 0);
@@ -124,6 +125,7 @@ paged_step_kernel(StepParams p)
             start[b] = bad ? 0 : at[0];
             back[b] = at[1];
             more[b] = at[2];
+            old_pages[b] = old_of[e];
             at[0] += rows_of[e];
             at[1] += max(-delta[e], 0);
             at[2] += max(delta[e], 0);
@@ -135,28 +137,31 @@ paged_step_kernel(StepParams p)
         }
         __syncthreads();
 
-        auto keys_of = [&](int b) { return (p.keep ? p.keep[b] : p.held[b]) + p.added[b]; };
         auto given_back = [&](int i) {
-            const int b = holder(back, n, i);
-            return p.page_table[(long long)b * p.ld_table + pages_of(keys_of(b)) + i - back[b]];
+            const int b = holder(back, n, i);                            // its last pages, up to old_pages[b]
+            return p.page_table[(long long)b * p.ld_table + old_pages[b] - (back[b + 1] - i)];
         };
         auto page_taken = [&](int i) {
             const int entry = top - 1 - i;
             return entry >= count ? given_back(entry - count) : p.free_pages[entry];
         };
 
-        const int stride = gridDim.x * THREADS, first = blockIdx.x * THREADS;
-        for (int b = first + tid; b <= n; b += stride) p.q_start[b] = start[b];
-        for (int i = first + tid; i < pages; i += stride) {
+        // rows are the first workgroups' share, pages the others' (a lone workgroup does both)
+        const int row_groups = gridDim.x > 1 ? gridDim.x - p.page_groups : 1, page_groups = gridDim.x > 1 ? p.page_groups : 1;
+        const bool has_rows = (int)blockIdx.x < row_groups, has_pages = gridDim.x == 1 || !has_rows;
+        const int page_stride = page_groups * THREADS;
+        const int page_first = has_pages ? (gridDim.x > 1 ? (int)blockIdx.x - row_groups : 0) * THREADS + tid : 0x7fffffff;
+        for (int b = page_first; b <= n; b += page_stride) p.q_start[b] = start[b];
+        for (int i = page_first; i < pages; i += page_stride) {
             const int b = holder(more, n, i);
-            p.page_table[(long long)b * p.ld_table + pages_of(p.held[b]) + i - more[b]] = page_taken(i);
+            p.page_table[(long long)b * p.ld_table + old_pages[b] + i - more[b]] = page_taken(i);
         }
-        for (int i = first + tid; i < pushes; i += stride) p.free_pages[count + i] = given_back(i);
+        for (int i = page_first; i < pushes; i += page_stride) p.free_pages[count + i] = given_back(i);
         if (blockIdx.x == 0 && tid < 4)
             p.status[tid] = tid == 0 ? bad : tid == 1 ? (int)min(missing, 0x7fffffffll) : tid == 2 ? (bad ? 0 : (int)all_rows) : left;
 
         const int end = start[n];
-        for (int base = first; base < p.tokens; base += stride) {
+        for (int base = has_rows ? blockIdx.x * THREADS : p.tokens; base < p.tokens; base += row_groups * THREADS) {
             const int t = base + tid;
             if (p.parent) {
                 __syncthreads();
@@ -170,8 +175,8 @@ paged_step_kernel(StepParams p)
             int position = 0;
             long long slot = -1;
             if (t < end) {
-                const int b = holder(start, n, t), held = p.held[b], keep = p.keep ? p.keep[b] : held;
-                const int place = keep + t - start[b], at_page = p.page_size.quot(place), old = pages_of(held);
+                const int b = holder(start, n, t), keep = p.keep ? p.keep[b] : p.held[b];
+                const int place = keep + t - start[b], at_page = p.page_size.quot(place), old = old_pages[b];
                 const int page = at_page < old ? p.page_table[(long long)b * p.ld_table + at_page] : page_taken(more[b] + at_page - old);
                 if (page >= 0) slot = (long long)page * page_size + place - at_page * page_size;
                 position = place;
@@ -218,14 +223,17 @@ template <int THREADS, int PER>
 hipError_t launch_as(const StepParams &p, hipStream_t stream)
 {
     const bool in_place = p.kv_len == p.held || p.kv_len == p.keep || p.count_out == p.count;
-    const int most = 512, want = (p.tokens + THREADS - 1) / THREADS, groups = want < 1 ? 1 : want < most ? want : most;
+    StepParams q = p;
+    const int most = 512, want = (p.tokens + THREADS - 1) / THREADS, rows = want < 1 ? 1 : want < most ? want : most;
+    q.page_groups = rows > 1 ? (rows + 3) / 4 : 0;
+    const int groups = rows + q.page_groups;
     if (in_place && groups > 1) {
-        paged_step_kernel<THREADS, PER, true, false><<<groups, THREADS, 0, stream>>>(p);
+        paged_step_kernel<THREADS, PER, true, false><<<groups, THREADS, 0, stream>>>(q);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        paged_step_kernel<THREADS, PER, false, true><<<1, THREADS, 0, stream>>>(p);
+        paged_step_kernel<THREADS, PER, false, true><<<1, THREADS, 0, stream>>>(q);
     } else {
-        paged_step_kernel<THREADS, PER, false, false><<<groups, THREADS, 0, stream>>>(p);
+        paged_step_kernel<THREADS, PER, false, false><<<groups, THREADS, 0, stream>>>(q);
     }
     return hipGetLastError();
 }

@@ -1020,9 +1020,10 @@ def kv_append_slots(cache: PagedCache, slots, k, v, positions=None, rotary: Opti
     q).  ``rotary`` turns by the angles of ``positions`` int32 [tokens]."""
     torch = _torch()
     dim, dev, dt = cache.head_dim, cache.device_index, k.dtype
-    if dt not in _CODES:
+    code = _CODES.get(dt)
+    if code is None:
         raise TypeError(f"unsupported dtype {dt}")
-    if slots.dim() != 1 or slots.dtype is not torch.int64 or slots.get_device() != dev or (slots.shape[0] > 1 and slots.stride(0) != 1):
+    if slots.dtype is not torch.int64 or slots.dim() != 1 or slots.get_device() != dev or (slots.shape[0] > 1 and slots.stride(0) != 1):
         raise ValueError(f"slots must be a contiguous int64 vector on the cache's GPU, got {slots.dtype} {tuple(slots.shape)}")
     n = slots.shape[0]
     pp = None
@@ -1032,8 +1033,12 @@ def kv_append_slots(cache: PagedCache, slots, k, v, positions=None, rotary: Opti
         if positions is None:
             raise ValueError("rotary needs positions")
         pp = _step_ints("positions", positions, n, dev)
-    sk = _head_rows("k", k, n, cache.kv_heads, dim, dt, dev)
-    sv = _head_rows("v", v, n, cache.kv_heads, dim, dt, dev)
+    shape = k.shape
+    sk, sv = k.stride(), v.stride()
+    if not (shape == (n, cache.kv_heads, dim) and shape == v.shape and v.dtype is dt and sk[2] == 1 and sv[2] == 1
+            and k.get_device() == dev and v.get_device() == dev):
+        sk = _head_rows("k", k, n, cache.kv_heads, dim, dt, dev)
+        sv = _head_rows("v", v, n, cache.kv_heads, dim, dt, dev)
     heads, sq, so, qp, op = 0, (0, 0), (0, 0), None, None
     if q is not None:
         heads = q.shape[1] if q.dim() == 3 else -1
@@ -1051,7 +1056,7 @@ def kv_append_slots(cache: PagedCache, slots, k, v, positions=None, rotary: Opti
             raise ValueError(f"weights of {norm.q_heads} query and {norm.k_heads} key heads for {heads} and {cache.kv_heads}")
     _launch((_lib or load()).nnjit_kv_append_slots, dev, stream, cache.address, n, slots.data_ptr(), pp,
             None if rotary is None else rotary.address, None if norm is None else norm.address, k.data_ptr(), sk[0], sk[1],
-            v.data_ptr(), sv[0], sv[1], heads, qp, sq[0], sq[1], op, so[0], so[1], _CODES[dt])
+            v.data_ptr(), sv[0], sv[1], heads, qp, sq[0], sq[1], op, so[0], so[1], code)
     return q_out
 
 

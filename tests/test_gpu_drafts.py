@@ -359,7 +359,8 @@ def test_kv_append_slots(dim, rot, layout, gap, shift, src, dtype, how):
 
 
 def test_append_slots_is_append():
-    """Without norms, with the positions of the batch's rows, it is kv_append to the last bit."""
+    """Without norms, with the positions of the batch's rows, it is kv_append: values to the last bit; turned rows within both
+    bounds (which product of a turn is fused with the sum is the compiler's choice, so their last bits may differ)."""
     B = Batch([5, 1, 40], [25, 1, 133], 4, 2, 64, 16, "f16", seed=5).device()
     C = Batch([5, 1, 40], [25, 1, 133], 4, 2, 64, 16, "f16", seed=5).device()
     rng = np.random.default_rng(1)
@@ -370,8 +371,16 @@ def test_append_slots_is_append():
     slots = [int(B.table[b, (p + i) // 16]) * 16 + (p + i) % 16 for b, (n, p) in enumerate(zip(B.news, past)) for i in range(n)]
     a = nj.kv_append(B.cache, B.batch, rows[:, 4:6], rows[:, 6:], table, rows[:, :4])
     b = nj.kv_append_slots(C.cache, torch.tensor(slots).cuda(), rows[:, 4:6], rows[:, 6:], _i32(pos), table, rows[:, :4])
-    for x, y in ((a, b), (B.dk, C.dk), (B.dv, C.dv)):
-        assert np.array_equal(_np(x), _np(y), equal_nan=True)
+    cos, sin = _np(table.table)[pos, :32], _np(table.table)[pos, 32:]
+    x = _np(rows)
+    want, bound = turned_with_bound(x[:, :4], np.zeros((46, 4, 64)), cos, sin, "half")
+    _inside(_np(a), _np(b), 2 * rounded(want, bound, "f16"))
+    want, bound = turned_with_bound(x[:, 4:6], np.zeros((46, 2, 64)), cos, sin, "half")
+    first, second = (_np(k).reshape(-1, 2, 64) for k in (B.dk, C.dk))
+    _inside(first[slots], second[slots], 2 * rounded(want, bound, "f16"))
+    rest = np.setdiff1d(np.arange(len(first)), slots)
+    assert np.array_equal(first[rest], second[rest], equal_nan=True)
+    assert np.array_equal(_np(B.dv), _np(C.dv), equal_nan=True)
 
 
 # ---------------------------------------------------------------- trees

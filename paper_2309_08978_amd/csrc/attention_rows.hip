@@ -171,6 +171,19 @@ struct StepCost {
 };
 constexpr StepCost kStepF16[] = {{16, 128, 1.5, 0, 1.0, 2.0}, {64, 64, 0.35, 0.8, 0.325, 0.35}, {128, 64, 0.5, 1.1, 0.4, 0.65}};
 constexpr StepCost kStepF32[] = {{16, 64, 0.9, 1.2, 0.5, 1.0}, {64, 64, 0.4, 4.2, -0.7, 5.8}, {128, 64, -0.3, 7.6, 0.7, 4.65}};
+// Trees: few rows over many keys.  Workgroups count in whole rounds for both types, and
+// splits that fill the chip's workgroups once to four times are tried as well (64 nodes behind 65536 keys: 26 splits
+// of 128 rows 109 us, 32 splits, two workgroups a CU, 97).  Fitted to 300 shapes of 17 .. 1024 rows, 150
+// .. 65536 keys, 1 .. 32 sequences; on 150 others within 3.4% of the best choice on the geometric mean, where the
+// constants above are within 5.7%.
+constexpr StepCost kTreeF16[] = {{16, 128, 1.06, -0.12, 0.82, 2.07}, {64, 64, 0.38, 1.23, 0.38, 0.58}, {128, 64, 0.5, 2.05, 0.47, 0.84}};
+constexpr StepCost kTreeF32[] = {{16, 64, 0.78, 1.2, 0.55, 1.31}, {64, 64, 0.4, 4.2, -0.78, 5.9}, {128, 64, -0.3, 7.6, 0.7, 4.46}};
+// The second launch of a split, the share of its partial sums' traffic, a later start of tall tiles, and what
+// sequences of different lengths cost.
+struct SplitCost {
+    double join, part, tall, spread;
+};
+constexpr SplitCost kPromptSplit = {3.8, 1, 1.5, 1.15}, kTreeSplit = {4.9, 1.32, 2.5, 1.02};
 
 // The kernel and the splits of the keys that these estimates call cheapest.
 // Tall tiles read keys and values least often but leave CUs idle where rows are
@@ -180,19 +193,28 @@ constexpr StepCost kStepF32[] = {{16, 64, 0.9, 1.2, 0.5, 1.0}, {64, 64, 0.4, 4.2
 // a split costs a second launch and writes and reads the partial sums (512 new
 // tokens alone: 16 unsplit, 28 in two).
 AttentionPlan many_rows_plan(int dtype, int64_t tokens, int64_t sequences, int q_heads, int kv_heads, int dim, int64_t rows,
-                             int64_t max_kv, int64_t window, int cus)
+                             int64_t max_kv, int64_t window, bool tree, int cus)
 {
+    const SplitCost &of = tree ? kTreeSplit : kPromptSplit;
+    const StepCost (&steps)[3] = dtype == NNJIT_F16 ? (tree ? kTreeF16 : kStepF16) : (tree ? kTreeF32 : kStepF32);
     const int64_t group = q_heads / kv_heads, lanes = (int64_t)kv_heads * sequences;
     const int elt = dtype == NNJIT_F16 ? 2 : 4;
     const double d = dim / 128.0, part_us = (double)tokens * q_heads * dim * 8 / 3.3e6;   // partial sums of a split, written and read
     AttentionPlan best{};
     double least = 0;
-    for (const StepCost &c : dtype == NNJIT_F16 ? kStepF16 : kStepF32) {
+    for (const StepCost &c : steps) {
         if (c.tile_rows == 64 && dim > 128) continue;      // not built: registers
         const int64_t row_tiles = (rows + c.tile_rows - 1) / c.tile_rows;
         const int64_t span = seen_span(max_kv, window, c.tile_rows, group);
-        for (int64_t want = 1; want <= 256; want = want < 4 ? want + 1 : want * 3 / 2 - want * 3 / 2 % 2) {
-            const int64_t per = (span + want - 1) / want;
+        const int64_t filled = tree ? cus / (row_tiles * lanes) : 0;      // splits that give every CU a workgroup
+        int64_t want = 1, fill = filled;
+        while (want <= 256) {
+            // the next number of splits: of the row 1, 2, 3, 4, 6, 8, 12, ..., and one to four times `filled` between them
+            const bool between = fill > 0 && fill <= 4 * filled && fill < want;
+            const int64_t tried = between ? fill : want;
+            if (between || fill == want) fill += filled;
+            if (!between) want = want < 4 ? want + 1 : want * 3 / 2 - want * 3 / 2 % 2;
+            const int64_t per = (span + tried - 1) / tried;
             const int64_t split_keys = std::max<int64_t>((per + 31) / 32 * 32, 32);
             const int64_t splits = std::max<int64_t>((span + split_keys - 1) / split_keys, 1);
             const double o = (double)row_tiles * lanes * splits / cus;
@@ -201,12 +223,12 @@ AttentionPlan many_rows_plan(int dtype, int64_t tokens, int64_t sequences, int q
             // sequences of different lengths unless there are many workgroups
             const double even = o < 4 ? std::ceil(o) : o;
             double bytes_us = 2.0 * c.keys * dim * elt * (even / row_tiles) * 256 / (5.5e6 * std::min(1.0, 0.9 + 0.05 * o));
-            if (sequences > 1 && o < 8) bytes_us *= 1.15;
+            if (sequences > 1 && o < 8) bytes_us *= of.spread;
             // fp32 products fill the matrix cores of a CU: its second workgroup takes as long again
-            const double share = elt == 4 && c.tile_rows > 16 ? std::ceil(o) : o;
+            const double share = elt == 4 && c.tile_rows > 16 ? std::ceil(o) : tree ? even : o;
             const double step = std::max({c.a0 + c.a1 * d, (c.b0 + c.b1 * d) * share, bytes_us});
-            const double cost = ((split_keys < span ? split_keys : span) + c.keys - 1) / c.keys * step + (splits > 1 ? 3.8 + splits * part_us : 0) +
-                                (c.tile_rows == 16 ? 0 : 1.5);   // a later start: copies, then products
+            const double cost = ((split_keys < span ? split_keys : span) + c.keys - 1) / c.keys * step + (splits > 1 ? of.join + splits * part_us * of.part : 0) +
+                                (c.tile_rows == 16 ? 0 : of.tall);   // a later start: copies, then products
             if (best.tile_rows == 0 || cost < least) {
                 least = cost;
                 best.tile_rows = c.tile_rows;
@@ -215,10 +237,20 @@ AttentionPlan many_rows_plan(int dtype, int64_t tokens, int64_t sequences, int q
                 best.split_keys = (int)split_keys;
                 best.waves = 4;
             }
-            if (splits < want || o > 16) break;            // more splits than keys, or than the chip holds
+            if (splits < tried || o > 16) break;           // more splits than keys, or than the chip holds
         }
     }
     return best;
+}
+
+AttentionPlan plan_of(int dtype, int64_t tokens, int64_t sequences, int q_heads, int kv_heads, int dim, int64_t max_q, int64_t max_kv,
+                      int64_t window, bool tree, int cus)
+{
+    const int64_t group = q_heads / kv_heads, rows = max_q * group;
+    AttentionPlan plan = rows <= 16 ? few_rows_plan(dtype, tokens, sequences, q_heads, kv_heads, dim, seen_span(max_kv, window, 16, group), cus)
+                                    : many_rows_plan(dtype, tokens, sequences, q_heads, kv_heads, dim, rows, max_kv, window, tree, cus);
+    plan.ws_floats = plan.splits > 1 ? plan.splits * tokens * q_heads * ((dim + 3) / 4 * 4 + 2) : 0;
+    return plan;
 }
 
 }  // namespace
@@ -226,12 +258,13 @@ AttentionPlan many_rows_plan(int dtype, int64_t tokens, int64_t sequences, int q
 AttentionPlan attention_plan(int dtype, int64_t tokens, int64_t sequences, int q_heads, int kv_heads, int dim, int64_t max_q,
                              int64_t max_kv, int causal, int64_t window, int cus)
 {
-    const int64_t group = q_heads / kv_heads, rows = max_q * group;
-    if (!causal) window = 0;
-    AttentionPlan plan = rows <= 16 ? few_rows_plan(dtype, tokens, sequences, q_heads, kv_heads, dim, seen_span(max_kv, window, 16, group), cus)
-                                    : many_rows_plan(dtype, tokens, sequences, q_heads, kv_heads, dim, rows, max_kv, window, cus);
-    plan.ws_floats = plan.splits > 1 ? plan.splits * tokens * q_heads * ((dim + 3) / 4 * 4 + 2) : 0;
-    return plan;
+    return plan_of(dtype, tokens, sequences, q_heads, kv_heads, dim, max_q, max_kv, causal ? window : 0, false, cus);
+}
+
+AttentionPlan tree_plan(int dtype, int64_t tokens, int64_t sequences, int q_heads, int kv_heads, int dim, int64_t max_q, int64_t max_kv,
+                        int64_t window, int cus)
+{
+    return plan_of(dtype, tokens, sequences, q_heads, kv_heads, dim, max_q, max_kv, window, true, cus);
 }
 
 hipError_t launch_attention(AttentionParams p, const AttentionPlan &plan, int dtype, bool vec, hipStream_t stream)

@@ -25,15 +25,19 @@ struct AttentionCall {
     int64_t max_q = 0, max_kv = 0;
     hipStream_t stream = nullptr;
 
-    // keys that a row's window and, of a tree, the new tokens behind it reach over
-    int64_t window() const { return p.window > 0 && p.mask ? p.window + max_q : p.window; }
+    AttentionPlan plan_for(int cus) const
+    {
+        const int kv_heads = p.q_heads / p.group;
+        // (a tree's rows see over their window and the new tokens behind it)
+        return p.mask ? tree_plan(dtype, p.batch.tokens, p.batch.sequences, p.q_heads, kv_heads, p.dim, max_q, max_kv,
+                                  p.window > 0 ? p.window + max_q : 0, cus)
+                      : attention_plan(dtype, p.batch.tokens, p.batch.sequences, p.q_heads, kv_heads, p.dim, max_q, max_kv, p.causal, p.window, cus);
+    }
 };
 
 int64_t attention_floats(void *ctx, int cus) {
     AttentionCall &c = *(AttentionCall *)ctx;
-    const AttentionParams &p = c.p;
-    c.plan = attention_plan(c.dtype, p.batch.tokens, p.batch.sequences, p.q_heads, p.q_heads / p.group, p.dim, c.max_q, c.max_kv,
-                            p.causal, c.window(), cus);
+    c.plan = c.plan_for(cus);
     return c.plan.ws_floats;
 }
 
@@ -90,8 +94,7 @@ int attend(AttentionCall &c, const nnjit_paged_kv *cache, const nnjit_paged_batc
     c.stream = (hipStream_t)stream;
     if (rows * q_heads > kMaxInt || c.max_q * c.p.group > kMaxInt - 64)
         return runtime_fail(NNJIT_EINVAL, "%lld rows of %lld heads in one call: below 2^31 are served", (long long)rows, (long long)q_heads);
-    const AttentionPlan least = attention_plan(c.dtype, rows, batch->sequences, c.p.q_heads, (int)cache->kv_heads, c.p.dim, c.max_q, c.max_kv,
-                                               c.p.causal, c.window(), 1024);
+    const AttentionPlan least = c.plan_for(1024);
     if ((double)least.row_tiles * least.splits * (double)cache->kv_heads * (double)batch->sequences > (double)kMaxGroups)
         return runtime_fail(NNJIT_EINVAL, "more than 2^24 - 1 workgroups (sequences times key heads times tiles)");
     return runtime_launch(c.stream, attention_floats, do_attention, &c, what);

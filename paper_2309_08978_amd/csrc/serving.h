@@ -119,6 +119,9 @@ struct AttentionPlan {
 };
 AttentionPlan attention_plan(int dtype, int64_t tokens, int64_t sequences, int q_heads, int kv_heads, int dim, int64_t max_q,
                              int64_t max_kv, int causal, int64_t window, int cus);
+// ... of drafted trees (window: with the new tokens behind it)
+AttentionPlan tree_plan(int dtype, int64_t tokens, int64_t sequences, int q_heads, int kv_heads, int dim, int64_t max_q, int64_t max_kv,
+                        int64_t window, int cus);
 hipError_t launch_attention_tiles_f16(const AttentionParams &p, int tile_rows, bool vec, int grid, hipStream_t stream);
 hipError_t launch_attention_tiles_f32(const AttentionParams &p, int tile_rows, bool vec, int grid, hipStream_t stream);
 // The same kernels for drafted trees (p.mask).

@@ -94,8 +94,10 @@ int attend(AttentionCall &c, const nnjit_paged_kv *cache, const nnjit_paged_batc
     c.stream = (hipStream_t)stream;
     if (rows * q_heads > kMaxInt || c.max_q * c.p.group > kMaxInt - 64)
         return runtime_fail(NNJIT_EINVAL, "%lld rows of %lld heads in one call: below 2^31 are served", (long long)rows, (long long)q_heads);
-    const AttentionPlan least = c.plan_for(1024);
-    if ((double)least.row_tiles * least.splits * (double)cache->kv_heads * (double)batch->sequences > (double)kMaxGroups)
+    // (a plan has tiles of 16 rows or more and up to 256 splits: most calls need no closer look)
+    const double lanes = (double)cache->kv_heads * (double)batch->sequences;
+    const AttentionPlan least = ((c.max_q * c.p.group + 15) / 16) * 256 * lanes <= (double)kMaxGroups ? AttentionPlan{} : c.plan_for(1024);
+    if (least.row_tiles * (double)least.splits * lanes > (double)kMaxGroups)
         return runtime_fail(NNJIT_EINVAL, "more than 2^24 - 1 workgroups (sequences times key heads times tiles)");
     return runtime_launch(c.stream, attention_floats, do_attention, &c, what);
 }

@@ -239,7 +239,7 @@ norm_rotary_kernel(NormParams p)
     };
 
     // rows of a group whose loads are on their way together: of queries, of keys and values
-    constexpr int AHEAD = VEC ? 4 : 1, AHEAD_KV = VEC ? 2 : 1;
+    constexpr int AHEAD = !VEC ? 1 : sizeof(S) == 4 ? 2 : 4, AHEAD_KV = VEC && sizeof(S) == 2 ? 2 : 1;
     typename Place<HOW>::template Raw<S> raw[AHEAD], raw_kv[AHEAD_KV];
     const int kv_last = APPEND ? last - p.q_heads : 0;
     auto fetch_kv = [&](int r0) {

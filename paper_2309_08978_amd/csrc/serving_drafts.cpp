@@ -288,8 +288,8 @@ int nnjit_kv_move(const nnjit_paged_kv *cache, const nnjit_paged_batch *batch, c
         break;
     }
     const double threads = 2.0 * (double)cache->kv_heads * (double)(row / c.unit);
-    if (batch->sequences > kMaxGroups || threads > 65535.0 * 256)
-        return runtime_fail(NNJIT_EINVAL, "sequences=%lld (below 2^24) of rows of %lld heads (65535 workgroups of 256 pieces) are too many",
+    if (batch->sequences > kMaxGroups || threads > 65535.0 * 16)
+        return runtime_fail(NNJIT_EINVAL, "sequences=%lld (below 2^24) of rows of %lld heads (65535 workgroups of 16 pieces) are too many",
                             (long long)batch->sequences, (long long)cache->kv_heads);
     c.p.pool = pool_of(cache);
     c.p.batch = batch_of(batch);

@@ -541,17 +541,17 @@ def _plain_lds(A, B, C, sa, sb, sc):
 
 
 _CODES: dict = {}     # torch dtype -> code; filled on first use (torch is imported lazily)
-_F32 = None
+_F32 = _I32 = None
 _torch_module = None
 _torch_stream = _torch_device = None     # handle of torch's current stream on a GPU; the current GPU (0.1 us each)
 
 
 def _torch():
-    global _F32, _torch_module, _torch_stream, _torch_device
+    global _F32, _I32, _torch_module, _torch_stream, _torch_device
     if _torch_module is None:
         import torch
         _CODES.update({torch.float32: NNJIT_F32, torch.float16: NNJIT_F16})
-        _F32 = torch.float32
+        _F32, _I32 = torch.float32, torch.int32
         _torch_stream, _torch_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         _torch_module = torch
     return _torch_module
@@ -945,7 +945,7 @@ class PagedStep:
 
 
 def _step_ints(name: str, t, count: int, device_index: int) -> int:
-    if t.shape == (count,) and t.dtype is _torch_module.int32 and t.get_device() == device_index and (count < 2 or t.stride(0) == 1):
+    if t.dtype is _I32 and t.shape == (count,) and t.get_device() == device_index and (count < 2 or t.stride(0) == 1):
         return t.data_ptr()
     _int32(name, t, count)
     raise ValueError(f"{name} must be on one GPU with the step, got {t.device}")
@@ -961,7 +961,7 @@ def paged_step(step: PagedStep, pool: PagePool, held, added, keep=None, parent=N
     n, dev = step.sequences, step.device_index
     if pool.device_index != dev:
         raise ValueError("pool and step must be on one GPU")
-    d = StepDesc.from_buffer_copy(step.desc)
+    d = StepDesc.from_buffer_copy(step.desc)           # (a copy: another thread may fill the step's with its own)
     d.held, d.added = _step_ints("held", held, n, dev), _step_ints("added", added, n, dev)
     if keep is not None:
         d.keep = _step_ints("keep", keep, n, dev)
@@ -1165,11 +1165,13 @@ def kv_move(cache: PagedCache, batch: PagedBatch, path, accepted, stream=None) -
     dev, sequences = cache.device_index, batch.kv_len.shape[0]
     if batch.device_index != dev:
         raise ValueError("cache and batch must be on one GPU")
-    _int32("path", path, sequences, None)
-    if path.get_device() != dev or (path.shape[1] > 1 and path.stride(1) != 1) or path.stride(0) < 0:
-        raise ValueError(f"path must be on the cache's GPU with unit stride along the last dimension, got {path.device} {tuple(path.stride())}")
-    _launch((_lib or load()).nnjit_kv_move, dev, stream, cache.address, batch.address, path.data_ptr(),
-            max(path.stride(0), path.shape[1]), path.shape[1], _step_ints("accepted", accepted, sequences, dev))
+    if path.dtype is not _I32 or path.dim() != 2 or path.shape[0] != sequences:
+        raise ValueError(f"path must be int32 [{sequences}, nodes], got {path.dtype} {tuple(path.shape)}")
+    nodes, ld = path.shape[1], path.stride(0)
+    if path.get_device() != dev or (nodes > 1 and path.stride(1) != 1) or (sequences > 1 and ld < nodes):
+        raise ValueError(f"path must be rows of their own on the cache's GPU with unit stride along the last dimension, got {path.device} {tuple(path.stride())}")
+    _launch((_lib or load()).nnjit_kv_move, dev, stream, cache.address, batch.address, path.data_ptr(), ld if ld > nodes else nodes, nodes,
+            _step_ints("accepted", accepted, sequences, dev))
 
 
 class LogitRules:
@@ -1228,25 +1230,29 @@ def adjust_logits(logits, rules: LogitRules, out=None, stream=None):
     that are there already, biases, -infinity where a mask has no bit.  ``out`` (fp32 or
     fp16, allocated like logits if None) may be logits."""
     _torch()
-    if logits.dim() != 2:
-        raise ValueError(f"logits must be [rows, vocab], got {tuple(logits.shape)}")
-    rows, vocab = logits.shape
+    shape = logits.shape
+    if len(shape) != 2:
+        raise ValueError(f"logits must be [rows, vocab], got {tuple(shape)}")
+    rows, vocab = shape
     dev = rules.device_index
     if out is None:
         out = _empty((rows, vocab), logits.dtype, logits.device, stream)
     if rules.rows != rows:
         raise ValueError(f"{rows} rows of logits, rules for {rules.rows}")
-    if rules.words is not None and rules.words < -(-vocab // 32):
+    if rules.words is not None and 32 * rules.words < vocab:
         raise ValueError(f"mask rows of {rules.words} words for {vocab} tokens")
-    for name, t in (("logits", logits), ("out", out)):
-        if t.dtype not in _CODES:
-            raise TypeError(f"unsupported dtype {t.dtype}")
-        if t.shape != logits.shape or (vocab > 1 and t.stride(1) != 1) or t.get_device() != dev:
-            raise ValueError(f"{name} must be [{rows}, {vocab}] with unit stride along the last dimension on the rules' GPU, got {tuple(t.shape)} on {t.device}")
-    if rows > 1 and out.stride(0) < vocab:
-        raise ValueError("rows of out overlap")
-    _launch((_lib or load()).nnjit_adjust_logits, dev, stream, rules.address, rows, vocab, logits.data_ptr(), logits.stride(0),
-            _CODES[logits.dtype], out.data_ptr(), out.stride(0), _CODES[out.dtype])
+    sx, sy, xc, yc = logits.stride(), out.stride(), _CODES.get(logits.dtype), _CODES.get(out.dtype)
+    if not (out.shape == shape and sx[1] == 1 and sy[1] == 1 and sy[0] >= vocab and xc is not None and yc is not None
+            and logits.get_device() == dev and out.get_device() == dev):       # plain rows need no closer look
+        for name, t in (("logits", logits), ("out", out)):
+            if t.dtype not in _CODES:
+                raise TypeError(f"unsupported dtype {t.dtype}")
+            if t.shape != shape or (vocab > 1 and t.stride(1) != 1) or t.get_device() != dev:
+                raise ValueError(f"{name} must be [{rows}, {vocab}] with unit stride along the last dimension on the rules' GPU, got {tuple(t.shape)} on {t.device}")
+        if rows > 1 and sy[0] < vocab:
+            raise ValueError("rows of out overlap")
+    _launch((_lib or load()).nnjit_adjust_logits, dev, stream, rules.address, rows, vocab, logits.data_ptr(), sx[0], xc,
+            out.data_ptr(), sy[0], yc)
     return out
 
 

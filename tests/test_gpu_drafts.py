@@ -715,3 +715,19 @@ def test_every_call_on_another_stream_and_in_a_graph():
         torch.cuda.synchronize()
         for k in eager:
             assert torch.equal(outs[k], eager[k]) and torch.equal(again[k], eager[k]), k
+
+
+@pytest.mark.parametrize("prompts,new,nodes,page", [([40, 7, 1], 24, 12, 16), ([3, 70], 20, 40, 5), ([5], 9, 1, 16)])
+def test_decoding_with_drafted_trees(prompts, new, nodes, page):
+    """The operators together: every generated token is the best allowed one of the formulas in 64 bits without a cache.
+
+    Logits are sums of 256 products of values rounded to fp16 (the attention's output, x + o and the cache: relative U16 each, against
+    logits of size 1 to 4), so a choice may lie a few 2^-11 times 4 below the best."""
+    from examples import speculate
+    said, steps, worst = speculate.generate(prompts, new, nodes, page_size=page, check=True)
+    assert [len(s) for s in said] == [new] * len(prompts)
+    assert worst < 4 * 4 * U16
+    if nodes > 1:
+        plain, more, _ = speculate.generate(prompts, new, 1, page_size=page)
+        assert steps < more, "drafts save steps"
+        assert plain == said or worst > 0

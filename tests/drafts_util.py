@@ -1,11 +1,13 @@
 """Plain forms of the operators of a step of drafted tokens: lists and 64 bits."""
 from __future__ import annotations
 
+import ctypes
 import math
 
 import numpy as np
 import torch
 
+import paper_2309_08978_amd as nj
 from tests.serving_util import U16, U32, turn
 
 MISSING, LENGTHS, ROWS, POOL = 1, 2, 4, 8
@@ -131,26 +133,100 @@ def attention_of(B, seen, scale=None):
         k = np.stack([B.k[s].double().numpy() for s in slots]) if slots else np.zeros((0, B.hk, B.dim))
         v = np.stack([B.v[s].double().numpy() for s in slots]) if slots else np.zeros((0, B.hk, B.dim))
         rows, sees = slice(B.start[b], B.start[b] + n), seen[b]
+        some = sees.any(1)[:, None]
         for h in range(B.hq if n else 0):
             qq, kk, vv = q[rows, h], k[:, h // group], v[:, h // group]
-            for i in range(n):
-                at = B.start[b] + i
-                j = np.flatnonzero(sees[i])
-                if j.size == 0:
-                    out[at, h] = 0.0
-                    continue
-                with np.errstate(all="ignore"):
-                    x = scale * (kk[j] @ qq[i])
-                    w = np.exp(x - x.max())
-                    o = (w[:, None] * vv[j]).sum(0) / w.sum()
-                    size = abs(scale) * np.linalg.norm(qq[i]) * np.linalg.norm(kk[j], axis=1).max()
-                    e = (B.dim + 4) * U32 * size + 2 * U32 * np.abs(x - x.max()).max() + 4 * U32
-                    most = np.abs(vv[j]).max()
-                    bd = most * (2 * e + 2 * j.size * U32) * np.ones(B.dim)
-                    if B.dtype == "f16":
-                        bd = bd + most * U16 + np.abs(o) * U16 + 2.0 ** -24
-                out[at, h], bound[at, h] = o, bd
+            out[rows, h] = 0.0
+            if not some.any():
+                continue
+            with np.errstate(all="ignore"):
+                x = np.where(sees, scale * (qq @ kk.T), -np.inf)
+                top = x.max(1, keepdims=True)
+                w = np.where(sees, np.exp(x - top), 0.0)
+                fine = np.isfinite(vv).all()
+                # (a sum of values that are not finite is left to the formula, row by row, over what the row sees)
+                o = w @ vv if fine else np.stack([(w[i, sees[i]][:, None] * vv[sees[i]]).sum(0) for i in range(n)])
+                o = o / w.sum(1, keepdims=True)
+                size = abs(scale) * np.linalg.norm(qq, axis=1) * np.where(sees, np.linalg.norm(kk, axis=1), 0.0).max(1)
+                e = (B.dim + 4) * U32 * size + 2 * U32 * np.where(sees, np.abs(x - top), 0.0).max(1) + 4 * U32
+                most = np.where(sees, np.abs(vv).max(1), 0.0).max(1)
+                bd = (most * (2 * e + 2 * sees.sum(1) * U32))[:, None] * np.ones((1, B.dim))
+                if B.dtype == "f16":
+                    bd = bd + most[:, None] * U16 + np.abs(o) * U16 + 2.0 ** -24
+            out[rows, h], bound[rows, h] = np.where(some, o, 0.0), np.where(some, bd, 0.0)
     return out, np.where(np.isfinite(bound), bound, np.inf)
+
+
+class Plan(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("tile_rows", "row_tiles", "splits", "split_keys", "waves")] + [("ws_floats", ctypes.c_int64)]
+
+
+def tree_plan(dtype, news, keys, hq, hk, dim, window=0, cus=256) -> Plan:
+    """nnjit::tree_plan (csrc/serving.h) for a batch whose max_q and max_kv are its longest."""
+    f = nj.load(build_if_missing=True)._ZN5nnjit9tree_planEilliiillli
+    i, n = ctypes.c_int, ctypes.c_int64
+    f.restype, f.argtypes = Plan, [i, n, n, i, i, i, n, n, n, i]
+    return f(nj.NNJIT_F16 if dtype == "f16" else nj.NNJIT_F32, sum(news), len(news), hq, hk, dim, max(news), max(keys),
+             window + max(news) if window else 0, cus)
+
+
+# (dtype, new tokens, keys, query heads, key heads, dim, tile rows, split over the keys, waves): every tile height, split and
+# unsplit, for each class of head dims of either type
+TREE_COVER = [
+    ("f16", [4, 1], [24, 14], 1, 1, 64, 16, False, 4),
+    ("f16", [4, 1], [204, 134], 1, 1, 64, 16, False, 8),
+    ("f16", [4, 1], [1004, 667], 1, 1, 64, 16, True, 4),
+    ("f16", [40, 7, 1], [60, 20, 21], 64, 16, 64, 64, False, 4),
+    ("f16", [40, 7, 1], [3040, 2007, 3001], 4, 4, 64, 64, True, 4),
+    ("f16", [128, 1, 100, 90, 77, 128], [148, 14, 120, 96, 90, 148], 64, 16, 64, 128, False, 4),
+    ("f16", [40, 7, 1], [2040, 1340, 2001], 32, 8, 64, 128, True, 4),
+    ("f16", [4, 1], [24, 14], 1, 1, 96, 16, False, 4),
+    ("f16", [4, 1], [204, 134], 1, 1, 96, 16, False, 8),
+    ("f16", [4, 1], [504, 334], 1, 1, 96, 16, True, 4),
+    ("f16", [40, 7, 1], [60, 20, 21], 64, 16, 96, 64, False, 4),
+    ("f16", [40, 7, 1], [2040, 1340, 2001], 4, 4, 96, 64, True, 4),
+    ("f16", [128, 1, 100, 90, 77, 128], [148, 14, 120, 96, 90, 148], 64, 16, 96, 128, False, 4),
+    ("f16", [40, 7, 1], [2040, 1340, 2001], 32, 8, 96, 128, True, 4),
+    ("f16", [4, 1], [24, 14], 1, 1, 128, 16, False, 4),
+    ("f16", [4, 1], [304, 201], 1, 1, 128, 16, True, 4),
+    ("f16", [40, 7, 1], [60, 20, 21], 64, 16, 128, 64, False, 4),
+    ("f16", [40, 7, 1], [2040, 1340, 2001], 4, 4, 128, 64, True, 4),
+    ("f16", [128, 1, 100, 90, 77, 128], [148, 14, 120, 96, 90, 148], 64, 16, 128, 128, False, 4),
+    ("f16", [40, 7, 1], [3040, 2007, 3001], 64, 16, 128, 128, True, 4),
+    ("f16", [4, 1], [24, 14], 1, 1, 200, 16, False, 4),
+    ("f16", [4, 1], [304, 201], 1, 1, 200, 16, True, 4),
+    ("f16", [40, 7, 1], [60, 20, 21], 64, 16, 200, 128, False, 4),
+    ("f16", [40, 7, 1], [540, 340, 501], 16, 4, 200, 128, True, 4),
+    ("f32", [4, 1], [24, 14], 1, 1, 64, 16, False, 4),
+    ("f32", [4, 1], [204, 134], 1, 1, 64, 16, False, 8),
+    ("f32", [4, 1], [504, 334], 1, 1, 64, 16, True, 4),
+    ("f32", [100, 3], [120, 16], 64, 16, 64, 64, False, 4),
+    ("f32", [40, 7, 1], [1040, 673, 1001], 16, 4, 64, 64, True, 4),
+    ("f32", [100, 31, 77, 90], [120, 44, 97, 96], 64, 16, 64, 128, False, 4),
+    ("f32", [40, 33, 40, 1], [540, 366, 540, 167], 32, 8, 64, 128, True, 4),
+    ("f32", [4, 1], [24, 14], 1, 1, 96, 16, False, 4),
+    ("f32", [4, 1], [204, 134], 1, 1, 96, 16, False, 8),
+    ("f32", [4, 1], [304, 201], 1, 1, 96, 16, True, 4),
+    ("f32", [100, 3], [120, 16], 64, 16, 96, 64, False, 4),
+    ("f32", [40, 7, 1], [1040, 673, 1001], 16, 4, 96, 64, True, 4),
+    ("f32", [100, 31, 77, 90], [120, 44, 97, 96], 64, 16, 96, 128, False, 4),
+    ("f32", [100, 3], [1100, 669], 16, 4, 96, 128, True, 4),
+    ("f32", [4, 1], [24, 14], 1, 1, 128, 16, False, 4),
+    ("f32", [4, 1], [204, 134], 1, 1, 128, 16, True, 4),
+    ("f32", [100, 3], [120, 16], 64, 16, 128, 64, False, 4),
+    ("f32", [128, 1, 100, 90, 77, 128], [1128, 667, 1100, 423, 743, 1128], 2, 1, 128, 64, True, 4),
+    ("f32", [100, 31, 77, 90], [120, 44, 97, 96], 64, 16, 128, 128, False, 4),
+    ("f32", [100, 3], [1100, 669], 16, 4, 128, 128, True, 4),
+    ("f32", [4, 1], [24, 14], 1, 1, 200, 16, False, 4),
+    ("f32", [4, 1], [204, 134], 1, 1, 200, 16, True, 4),
+    ("f32", [100, 31, 77, 90], [120, 44, 97, 96], 64, 16, 200, 128, False, 4),
+    ("f32", [128, 1, 100, 90, 77, 128], [2128, 1334, 2100, 756, 1410, 2128], 2, 1, 200, 128, True, 4),
+]
+
+
+def cover_name(case) -> str:
+    dtype, news, keys, hq, hk, dim, rows, split, waves = case
+    return f"{dtype}-{dim}-{rows}rows-{'split' if split else 'whole'}-{waves}waves"
 
 
 def random_mask(B, words, rng, density=0.4):

@@ -10,7 +10,8 @@ import pytest
 import torch
 
 import paper_2309_08978_amd as nj
-from tests.drafts_util import (LENGTHS, MISSING, POOL, ROWS, attention_of, norm_grad, normed, plain_logits, plain_step, tree_seen, words_of)
+from tests.drafts_util import (LENGTHS, MISSING, POOL, ROWS, TREE_COVER, attention_of, cover_name, norm_grad, normed, plain_logits, plain_step,
+                               tree_plan, tree_seen, words_of)
 from tests.serving_util import Batch
 from tests.test_serving_cpu import BAD_BATCHES, BAD_CACHES, _batch, _kv, _rot
 
@@ -206,6 +207,41 @@ def test_structs_are_as_in_c():
     """Sizes of the descriptions: eight bytes a field, ints and floats four."""
     assert ctypes.sizeof(nj.PagePoolDesc) == 32 and ctypes.sizeof(nj.HeadNormDesc) == 40
     assert ctypes.sizeof(nj.StepDesc) == 18 * 8 and ctypes.sizeof(nj.LogitRulesDesc) == 16 * 8
+
+
+# ------------------------------------------------------------- which kernel a tree gets
+
+@pytest.mark.parametrize("case", TREE_COVER, ids=cover_name)
+def test_kernel_of_a_tree(case):
+    dtype, news, keys, hq, hk, dim, rows, split, waves = case
+    p = tree_plan(dtype, news, keys, hq, hk, dim)
+    assert (p.tile_rows, p.splits > 1, p.waves) == (rows, split, waves)
+
+
+def test_tree_cover_is_whole():
+    have = {(c[0], c[5], c[6], c[7], c[8]) for c in TREE_COVER}
+    for dtype in ("f16", "f32"):
+        for dim in (64, 96, 128, 200):
+            for rows in (16, 64, 128) if dim <= 128 else (16, 128):
+                assert {(dtype, dim, rows, split, 4) for split in (False, True)} <= have
+        assert (dtype, 64, 16, False, 8) in have and (dtype, 96, 16, False, 8) in have
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("window", [0, 1, 100, 5000])
+def test_tree_plans_reach_every_key(dtype, window):
+    """Tiles for all rows, splits over all keys that a row's window and the new tokens behind it span."""
+    rng = np.random.default_rng(0)
+    for _ in range(300):
+        n = int(rng.integers(1, 40))
+        new = [int(2 ** rng.uniform(0, 7)) for _ in range(n)]
+        keys = [a + int(2 ** rng.uniform(0, 16)) for a in new]
+        hk, group, dim = int(rng.choice([1, 4, 8, 32])), int(rng.choice([1, 2, 3, 8])), int(rng.choice([64, 96, 128, 256]))
+        p = tree_plan(dtype, new, keys, hk * group, hk, dim, window)
+        assert p.row_tiles * p.tile_rows >= max(new) * group and p.split_keys % 32 == 0
+        span = min(max(keys), window + max(new) + 31) if window else max(keys)
+        assert p.splits * p.split_keys >= span and p.splits <= 256
+        assert p.ws_floats == (p.splits * sum(new) * hk * group * ((dim + 3) // 4 * 4 + 2) if p.splits > 1 else 0)
 
 
 # ------------------------------------------------------------- the plain forms

@@ -6,8 +6,8 @@ import pytest
 import torch
 
 import paper_2309_08978_amd as nj
-from tests.drafts_util import (LENGTHS, MISSING, POOL, ROWS, attention_of, norm_grad, normed, plain_logits, plain_step, random_mask, signed,
-                               tree_mask, tree_seen, turned_with_bound, words_of)
+from tests.drafts_util import (LENGTHS, MISSING, POOL, ROWS, TREE_COVER, attention_of, cover_name, norm_grad, normed, plain_logits, plain_step,
+                               random_mask, signed, tree_mask, tree_seen, turned_with_bound, words_of)
 from tests.serving_util import DT, U16, Batch, rounded
 
 pytestmark = pytest.mark.gpu
@@ -425,6 +425,14 @@ SHAPES = [(4, 4, 64), (8, 2, 128), (6, 2, 96), (16, 1, 64), (5, 1, 256), (3, 3, 
 def test_trees(dtype, hq, hk, dim, page, kind):
     """Trees of one node to sixty at the ends of tiles and pages; masks of any pattern, with bits of tokens that are not there."""
     _tree_case([1, 7, 16, 33, 60, 2], [1, 20, 48, 160, 61, 130], hq, hk, dim, page, dtype, 2, kind)
+
+
+@pytest.mark.parametrize("case", TREE_COVER, ids=cover_name)
+def test_every_kernel_of_trees(case):
+    """Every tile height, split and whole, by whole pages and by look-ups a lane, element by element."""
+    dtype, news, keys, hq, hk, dim, _, _, _ = case
+    _tree_case(news, keys, hq, hk, dim, 16, dtype, 4, "tree", seed=31)
+    _tree_case(news, keys, hq, hk, dim, 12, dtype, 4, "any", 150, seed=32)
 
 
 @pytest.mark.parametrize("dtype", ["f16", "f32"])

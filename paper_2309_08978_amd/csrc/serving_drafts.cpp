@@ -241,7 +241,9 @@ int nnjit_norm_rotary_grad(const nnjit_rotary_table *rotary, int64_t tokens, int
     if (rc != NNJIT_OK) return rc;
     if ((rc = check_rows("dy", dy, tokens, heads, dy_token, dy_head)) != NNJIT_OK) return rc;
     if (dx && (rc = check_written("dx", dx, tokens, heads, head_dim, dx_token, dx_head)) != NNJIT_OK) return rc;
-    if (heads == 0 || (tokens == 0 && !dw) || (!dx && !dw)) return NNJIT_OK;
+    if (dw && !weight) return runtime_fail(NNJIT_EINVAL, "weight is NULL");
+    // (no rows: dx has none, the sum of dw is 0)
+    if ((!dx && !dw) || ((tokens == 0 || heads == 0) && !dw) || (heads == 0 && w_head > 0)) return NNJIT_OK;
     if (tokens * heads > kMaxInt || (w_head > 0 && heads > 0xffff))
         return runtime_fail(NNJIT_EINVAL, "%lld rows of %lld heads in one call: below 2^31 rows (a weight a head: 2^16 heads) are served",
                             (long long)tokens, (long long)heads);

@@ -107,7 +107,7 @@ def test_bad_batches(bad):
     lambda: _forward(dim=0), lambda: _forward(dim=257), lambda: _forward(rot=_rot(), pos=None), lambda: _forward(w=None), lambda: _forward(wh=31),
     lambda: _forward(eps=math.inf), lambda: _forward(x=None), lambda: _forward(xst=(-64, 32)), lambda: _forward(y=None),
     lambda: _forward(tokens=2, yst=(32, 32)), lambda: _forward(rot=_rot(table=None)),
-    lambda: _grad(w=None), lambda: _grad(w=None, tokens=0), lambda: _grad(x=None), lambda: _grad(dy=None), lambda: _grad(dyst=(64, -1)),
+    lambda: _grad(w=None), lambda: _grad(w=None, tokens=0), lambda: _grad(w=None, heads=0), lambda: _grad(x=None), lambda: _grad(dy=None), lambda: _grad(dyst=(64, -1)),
     lambda: _grad(tokens=2, dxst=(63, 32)), lambda: _grad(tokens=1 << 23, heads=256, dxst=(8192, 32)), lambda: _grad(heads=1 << 16, wh=32, dxst=(1 << 21, 32)),
     lambda: nj.nnjit_tree_attention(None, _batch(), 16, 1, 1, None, 4, 16, 128, 32, 16, 128, 32, 0.1),
     lambda: nj.nnjit_tree_attention(_kv(), None, 16, 1, 1, None, 4, 16, 128, 32, 16, 128, 32, 0.1),
@@ -140,7 +140,8 @@ def test_nothing_to_do():
     assert _append(tokens=0, slots=None, k=None, v=None, q=None, out=None) == nj.NNJIT_OK
     assert _forward(tokens=0, x=None, y=None, pos=None) == nj.NNJIT_OK
     assert _forward(heads=0, x=None, y=None, w=None) == nj.NNJIT_OK
-    assert _grad(heads=0, x=None, dy=None, dx=None, w=None) == nj.NNJIT_OK
+    assert _grad(heads=0, x=None, dy=None, dx=None, dw=None, w=None) == nj.NNJIT_OK
+    assert _grad(heads=0, x=None, dy=None, dx=None, wh=32) == nj.NNJIT_OK
     assert _grad(tokens=0, x=None, dy=None, dx=None, dw=None) == nj.NNJIT_OK
     assert _tree(batch=_batch(tokens=0), mask=None, q=None, out=None) == nj.NNJIT_OK
     assert _tree(batch=_batch(max_q=0)) == nj.NNJIT_OK

@@ -1,6 +1,8 @@
 """A step of drafted tokens on the GPU against plain forms: the step's arrays,
 norms of heads with turn and append and their gradients, attention of trees,
 moves of accepted tokens, logit rules."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -314,6 +316,12 @@ def test_norm_grad_of_one_side_only():
     call(0, None, b)
     torch.cuda.synchronize()
     assert bool((b == 0).all())
+    for shape in ((0, 2, 32), (5, 0, 32)):                 # no rows: the sum is 0
+        none = torch.zeros(shape, device="cuda")
+        b.fill_(5.0)
+        dx, dw = nj.norm_rotary_grad(none, none, w, dweight=b)
+        assert dx.shape == shape and bool((b == 0).all())
+        assert nj.norm_rotary(none, w).shape == shape
 
 
 @pytest.mark.parametrize("dim,rot,layout,gap,shift", HEADS)
@@ -687,42 +695,135 @@ def test_logits_that_are_not_finite():
 
 # --------------------------------------------------- streams, graphs, all together
 
-def test_every_call_on_another_stream_and_in_a_graph():
-    """Captured on one stream, replayed between eager calls of the same leaves on another; every replay is the eager result."""
-    rng = np.random.default_rng(11)
-    B = Batch([9, 30], [120, 300], 8, 2, 64, 16, "f16", seed=2).device()
-    mask, depth = tree_mask(B, 1, rng)
-    dmask = torch.from_numpy(mask.view(np.int32)).cuda()
-    x, dy, w = _rows(rng, 39, 8, 64, "f16"), _rows(rng, 39, 8, 64, "f16"), torch.ones(64, device="cuda")
-    logits, rules = _rows(rng, 6, 1, 500, "f32").view(6, 500), nj.LogitRules(history=_i32([[1, 2, 1]] * 6), frequency=torch.ones(6, device="cuda"))
-    outs = {}
+def _calls():
+    """name -> (inputs, call of them that returns one tensor)"""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    r = lambda *shape, dtype=torch.float16: torch.randn(shape, device="cuda", generator=g).to(dtype)
+    table, w = nj.rotary_table(600, 64), r(64, dtype=torch.float32) + 2
+    cache = nj.PagedCache(r(40, 16, 2, 64), r(40, 16, 2, 64))
+    pages = torch.randperm(40, generator=g, device="cuda").to(torch.int32)[None]
+    batch = nj.PagedBatch(_i32([0, 9]), _i32([600]), pages, tokens=9, max_q=9, max_kv=600)
+    pos, slots = _i32(list(range(591, 600))), torch.arange(9, device="cuda") * 3
+    mask, path, accepted = _i32([[(2 << i) - 1] for i in range(9)]), _i32([[0, 2, 5, 8]]), _i32([4])
+    norm = nj.HeadNorm(w, w)
+    rules = nj.LogitRules(history=_i32([[1, 2, 1]] * 6), frequency=torch.ones(6, device="cuda"))
+    backup = cache.k.clone(), cache.v.clone()
 
-    def calls(to):
-        to["a"] = nj.tree_attention(B.dq, B.cache, B.batch, dmask, to.get("a"))
-        to["n"] = nj.norm_rotary(x, w, out=to.get("n"))
-        to["g"], to["w"] = nj.norm_rotary_grad(dy, x, w, dx=to.get("g"), dweight=to.get("w"))
-        to["l"] = nj.adjust_logits(logits, rules, to.get("l"))
-        return to
+    def append(k, v, q, **kw):
+        out = nj.kv_append_slots(cache, slots, k, v, pos, table, q, norm=norm, **kw)
+        return torch.cat([out.flatten(), cache.k.flatten(), cache.v.flatten()])
 
-    eager = calls({})
+    def move(k, **kw):
+        cache.k.copy_(k)                       # (the same places are moved in every call)
+        cache.v.copy_(k)
+        nj.kv_move(cache, batch, path, accepted, **kw)
+        return torch.cat([cache.k.flatten(), cache.v.flatten()])
+
+    pool = nj.PagePool(torch.arange(100, 160, dtype=torch.int32, device="cuda"), _i32([50]), _i32([0]))
+    step = nj.PagedStep(_i32([list(range(20)), list(range(20, 40))]), 4, 30, 1)
+    parent = _i32([-1, 0, 0, 1] + [-1, 0, 1, 2] + [0] * 22)
+
+    def arrays(lengths, **kw):
+        nj.paged_step(step, pool, lengths[0], lengths[1], lengths[2], parent, **kw)
+        return torch.cat([t.flatten().long() for t in (step.q_start, step.kv_len, step.positions, step.slots, step.mask, step.page_table,
+                                                       step.status, pool.count_out, pool.free_pages)])
+
+    return {
+        "paged_step": ([_i32([[9, 30], [4, 4], [9, 12]])], arrays),
+        "kv_append_slots": ([r(9, 2, 64), r(9, 2, 64), r(9, 8, 64)], append),
+        "norm_rotary": ([r(9, 8, 64)], lambda x, **kw: nj.norm_rotary(x, w, pos, table, **kw)),
+        "norm_rotary_grad": ([r(9, 8, 64), r(9, 8, 64)],
+                             lambda dy, x, **kw: torch.cat([t.flatten().float() for t in nj.norm_rotary_grad(dy, x, w, pos, table, **kw)])),
+        "tree_attention": ([r(9, 8, 64)], lambda q, **kw: nj.tree_attention(q, cache, batch, mask, **kw)),
+        "kv_move": ([backup[0]], move),
+        "adjust_logits": ([r(6, 500, dtype=torch.float32)], lambda x, **kw: nj.adjust_logits(x, rules, **kw)),
+    }
+
+
+NAMES = ["paged_step", "kv_append_slots", "norm_rotary", "norm_rotary_grad", "tree_attention", "kv_move", "adjust_logits"]
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_current_stream(name):
+    """The inputs are written behind other work of the current stream, the result is read there."""
+    inputs, call = _calls()[name]
+    want = call(*inputs).clone()
     torch.cuda.synchronize()
+    late = [torch.zeros_like(x) for x in inputs]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)                        # about 10 ms
+        for x, y in zip(late, inputs):
+            x.copy_(y)
+        got = call(*late).clone()
+    side.synchronize()
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_captured_without_a_stream(name):
+    """Inside a capture the current stream is the captured one; replays between eager calls of the same inputs give the same."""
+    inputs, call = _calls()[name]
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
-        calls(outs)                               # the stream's scratch
-        side.synchronize()
-        graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(graph, stream=side):
-            calls(outs)
-    for _ in range(3):
-        for t in outs.values():
-            t.fill_(1.0)
+        want = call(*inputs).clone()                         # the stream's scratch
+    torch.cuda.synchronize()
+    held = [x.clone() for x in inputs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = call(*held)
+    for rep in range(3):
+        got.zero_()
+        eager = call(*inputs).clone()
         torch.cuda.synchronize()
-        again = calls({})
         graph.replay()
         torch.cuda.synchronize()
-        for k in eager:
-            assert torch.equal(outs[k], eager[k]) and torch.equal(again[k], eager[k]), k
+        assert torch.equal(got, want) and torch.equal(eager, want), rep
+
+
+@pytest.mark.parametrize("name", ["norm_rotary", "norm_rotary_grad", "tree_attention", "adjust_logits"])
+def test_outputs_belong_to_the_given_stream(name):
+    """Memory that the current stream still writes is not handed to a call on another stream."""
+    inputs, call = _calls()[name]
+    want = call(*inputs).clone()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for given in (side, side.cuda_stream):
+        busy = torch.empty_like(inputs[0])
+        torch.cuda._sleep(4_000_000)
+        busy.fill_(3.0)                                      # queued behind the sleep, on the current stream
+        del busy                                             # its block may be reused there at once
+        with torch.cuda.stream(side):
+            got = call(*inputs, stream=given)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+
+
+def test_capture_that_needs_scratch():
+    """A captured call whose stream lacks the scratch is refused; it works once a call of the sizes has run."""
+    rng = np.random.default_rng(5)
+    x, dy, w = _rows(rng, 3000, 4, 64, "f32"), _rows(rng, 3000, 4, 64, "f32"), torch.ones(64, device="cuda")
+    # a stream of its own: torch hands its streams out again and again, with the scratch of earlier calls
+    handle = ctypes.c_void_p()
+    assert nj.load().hipStreamCreateWithFlags(ctypes.byref(handle), 1) == 0
+    s = torch.cuda.ExternalStream(handle.value)
+    dx, dw = torch.empty_like(x), torch.empty(64, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        with pytest.raises(nj.NnjitError, match="run a call of the same sizes once"):
+            nj.norm_rotary_grad(dy, x, w, dx=dx, dweight=dw)
+    nj.norm_rotary_grad(dy, x, w, dx=dx, dweight=dw, stream=s)
+    torch.cuda.synchronize()
+    want = dw.clone()
+    with torch.cuda.graph(graph := torch.cuda.CUDAGraph(), stream=s):
+        nj.norm_rotary_grad(dy, x, w, dx=dx, dweight=dw)
+    for _ in range(3):
+        dw.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(dw, want)
 
 
 @pytest.mark.parametrize("prompts,new,nodes,page", [([40, 7, 1], 24, 12, 16), ([3, 70], 20, 40, 5), ([5], 9, 1, 16)])

@@ -313,47 +313,74 @@ norm_rotary_grad_kernel(NormParams p)
     const int w_head = PER_HEAD ? min(h_first + group, h_last - 1) : 0;
     at.load_weight(p.q_weight, w_head * p.qw_head, p.weight_half, wl, wh);
 
-    constexpr int AHEAD = VEC && !PER_HEAD ? 4 : 1;
+    // a row: its part of dw, and dx
+    auto row = [&](const typename Place<HOW>::template Raw<X> &x, const typename Place<HOW>::template Raw<Y> &y, const float *c, const float *s, X *dx) {
+        float xl[4], xh[4], gl[4], gh[4], squares = 0.f, dots = 0.f;
+        at.unpack(x, xl, xh);
+        at.unpack(y, gl, gh);
+        if (p.table) at.template rotate<true>(gl, gh, c, s);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            squares += xl[e] * xl[e] + xh[e] * xh[e];
+            dots += gl[e] * wl[e] * xl[e] + gh[e] * wh[e] * xh[e];
+        }
+        const float r = norm_scale(p, group_sum<LPH>(at.part(squares))), m = group_sum<LPH>(at.part(dots)) * r * p.one_by_dim;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float ul = xl[e] * r, uh = xh[e] * r;
+            dl[e] += gl[e] * ul;
+            dh[e] += gh[e] * uh;
+            gl[e] = r * (gl[e] * wl[e] - ul * m);
+            gh[e] = r * (gh[e] * wh[e] - uh * m);
+        }
+        if (p.qo.p) at.store(dx, gl, gh);
+    };
+    auto x_row = [&](int t) { return (const X *)p.q.p + (long long)t * p.q.tok; };
+    auto y_row = [&](int t) { return (const Y *)p.dy.p + (long long)t * p.dy.tok; };
+    auto dx_row = [&](int t) { return (X *)p.qo.p + (long long)t * p.qo.tok; };
+
     const int first = blockIdx.x * p.chunk, last = min(p.tokens, first + p.chunk);
-    for (int t = first + in_block; t < last; t += p.tokens_per_block) {
-        float c[4], s[4];
-        if (p.table) at.load_angles(p, p.positions[t], c, s);
-        const X *x_row = (const X *)p.q.p + (long long)t * p.q.tok;
-        const Y *y_row = (const Y *)p.dy.p + (long long)t * p.dy.tok;
-        X *dx_row = (X *)p.qo.p + (long long)t * p.qo.tok;
-        for (int h0 = h_first + group; h0 < h_last; h0 += AHEAD * groups) {
+    if constexpr (PER_HEAD) {
+        // a group's head is always the same: tokens are what it has loads ahead of
+        constexpr int AHEAD = VEC ? 3 : 1;
+        const int h = h_first + group;
+        for (int t0 = first + in_block; t0 < last && h < h_last; t0 += AHEAD * p.tokens_per_block) {      // (the same in all lanes of a group)
             typename Place<HOW>::template Raw<X> x[AHEAD];
             typename Place<HOW>::template Raw<Y> y[AHEAD];
+            float c[AHEAD][4], s[AHEAD][4];
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
-                const int h = h0 + j * groups;
-                if (h >= h_last) continue;
-                x[j] = at.fetch(row_of<VEC>(x_row, h, p.q.head));
-                y[j] = at.fetch(row_of<VEC>(y_row, h, p.dy.head));
+                const int t = min(t0 + j * p.tokens_per_block, last - 1);
+                x[j] = at.fetch(row_of<VEC>(x_row(t), h, p.q.head));
+                y[j] = at.fetch(row_of<VEC>(y_row(t), h, p.dy.head));
+                if (p.table) at.load_angles(p, p.positions[t], c[j], s[j]);
             }
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
-                const int h = h0 + j * groups;
-                if (h >= h_last) continue;                 // (the same in all lanes of a group)
-                float xl[4], xh[4], gl[4], gh[4], squares = 0.f, dots = 0.f;
-                at.unpack(x[j], xl, xh);
-                at.unpack(y[j], gl, gh);
-                if (p.table) at.template rotate<true>(gl, gh, c, s);
+                const int t = t0 + j * p.tokens_per_block;
+                if (t < last) row(x[j], y[j], c[j], s[j], row_of<VEC>(dx_row(t), h, p.qo.head));
+            }
+        }
+    } else {
+        constexpr int AHEAD = VEC ? 4 : 1;
+        for (int t = first + in_block; t < last; t += p.tokens_per_block) {
+            float c[4], s[4];
+            if (p.table) at.load_angles(p, p.positions[t], c, s);
+            for (int h0 = group; h0 < p.q_heads; h0 += AHEAD * groups) {
+                typename Place<HOW>::template Raw<X> x[AHEAD];
+                typename Place<HOW>::template Raw<Y> y[AHEAD];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    squares += xl[e] * xl[e] + xh[e] * xh[e];
-                    dots += gl[e] * wl[e] * xl[e] + gh[e] * wh[e] * xh[e];
+                for (int j = 0; j < AHEAD; ++j) {
+                    const int h = h0 + j * groups;
+                    if (h >= p.q_heads) continue;
+                    x[j] = at.fetch(row_of<VEC>(x_row(t), h, p.q.head));
+                    y[j] = at.fetch(row_of<VEC>(y_row(t), h, p.dy.head));
                 }
-                const float r = norm_scale(p, group_sum<LPH>(at.part(squares))), m = group_sum<LPH>(at.part(dots)) * r * p.one_by_dim;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float ul = xl[e] * r, uh = xh[e] * r;
-                    dl[e] += gl[e] * ul;
-                    dh[e] += gh[e] * uh;
-                    gl[e] = r * (gl[e] * wl[e] - ul * m);
-                    gh[e] = r * (gh[e] * wh[e] - uh * m);
+                for (int j = 0; j < AHEAD; ++j) {
+                    const int h = h0 + j * groups;
+                    if (h < p.q_heads) row(x[j], y[j], c, s, row_of<VEC>(dx_row(t), h, p.qo.head));
                 }
-                if (p.qo.p) at.store(row_of<VEC>(dx_row, h, p.qo.head), gl, gh);
             }
         }
     }

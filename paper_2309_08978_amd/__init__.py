@@ -1067,13 +1067,16 @@ def _norm_operands(x, weight, positions, table):
         raise ValueError(f"x must be [tokens, heads, head_dim], got {tuple(shape)}")
     tokens, heads, dim = shape
     dev = x.get_device()
-    if not x.is_cuda or weight.get_device() != dev or (table is not None and table.device_index != dev):
+    if dev < 0 or weight.get_device() != dev or (table is not None and table.device_index != dev):
         raise ValueError("x, weight and table must be on one GPU")
     if x.dtype not in _CODES:
         raise TypeError(f"unsupported dtype {x.dtype}")
-    w_heads, w_head = _norm_weight("weight", weight, None)
-    if weight.shape[-1] != dim or w_heads not in (None, heads):
-        raise ValueError(f"weight must be [{dim}] or [{heads}, {dim}], got {tuple(weight.shape)}")
+    if not (weight.shape == (dim,) and weight.stride(0) == 1 and weight.dtype in _CODES):       # one plain weight needs no closer look
+        w_heads, w_head = _norm_weight("weight", weight, None)
+        if weight.shape[-1] != dim or w_heads not in (None, heads):
+            raise ValueError(f"weight must be [{dim}] or [{heads}, {dim}], got {tuple(weight.shape)}")
+    else:
+        w_head = 0
     if table is None:
         return tokens, heads, dim, dev, None, None, w_head
     if positions is None:
@@ -1093,7 +1096,9 @@ def norm_rotary(x, weight, positions=None, table: Optional[RotaryTable] = None, 
     xd, yd = x.dtype, out.dtype
     if yd not in _CODES:
         raise TypeError(f"unsupported dtype {yd}")
-    sx = _head_rows("x", x, tokens, heads, dim, xd, dev)
+    sx = x.stride()
+    if sx[2] != 1:
+        sx = _head_rows("x", x, tokens, heads, dim, xd, dev)
     sy = _written_rows("out", out, tokens, heads, dim, yd, dev)
     _launch((_lib or load()).nnjit_norm_rotary, dev, stream, tp, tokens, heads, dim, pp, weight.data_ptr(), w_head, _CODES[weight.dtype],
             eps, x.data_ptr(), sx[0], sx[1], _CODES[xd], out.data_ptr(), sy[0], sy[1], _CODES[yd])
@@ -1110,15 +1115,18 @@ def norm_rotary_grad(dy, x, weight, positions=None, table: Optional[RotaryTable]
         dx = _empty((tokens, heads, dim), x.dtype, x.device, stream)
     if dweight is None:
         dweight = _empty(tuple(weight.shape), torch.float32, x.device, stream)
-    if dy.dtype not in _CODES:
-        raise TypeError(f"unsupported dtype {dy.dtype}")
-    sx = _head_rows("x", x, tokens, heads, dim, x.dtype, dev)
-    sd = _head_rows("dy", dy, tokens, heads, dim, dy.dtype, dev)
-    so = _written_rows("dx", dx, tokens, heads, dim, x.dtype, dev)
+    xd, dd = x.dtype, dy.dtype
+    if dd not in _CODES:
+        raise TypeError(f"unsupported dtype {dd}")
+    sx = x.stride()
+    if sx[2] != 1:
+        sx = _head_rows("x", x, tokens, heads, dim, xd, dev)
+    sd = _head_rows("dy", dy, tokens, heads, dim, dd, dev)
+    so = _written_rows("dx", dx, tokens, heads, dim, xd, dev)
     if dweight.shape != weight.shape or dweight.dtype is not _F32 or not dweight.is_contiguous() or dweight.get_device() != dev:
         raise ValueError(f"dweight must be contiguous float32 {tuple(weight.shape)} on x's GPU, got {dweight.dtype} {tuple(dweight.shape)}")
     _launch((_lib or load()).nnjit_norm_rotary_grad, dev, stream, tp, tokens, heads, dim, pp, weight.data_ptr(), w_head,
-            _CODES[weight.dtype], eps, x.data_ptr(), sx[0], sx[1], _CODES[x.dtype], dy.data_ptr(), sd[0], sd[1], _CODES[dy.dtype],
+            _CODES[weight.dtype], eps, x.data_ptr(), sx[0], sx[1], _CODES[xd], dy.data_ptr(), sd[0], sd[1], _CODES[dd],
             dx.data_ptr(), so[0], so[1], dweight.data_ptr())
     return dx, dweight
 

@@ -27,7 +27,7 @@ int64_t norm_grad_floats(void *ctx, int cus) {
     auto &c = *(Call<NormParams> *)ctx;
     const bool per_head = c.p.qw_head > 0;
     c.groups = norm_grad_groups(c.p.tokens, c.p.q_heads, c.p.dim, per_head, c.vec, cus);
-    return c.p.dw ? (int64_t)c.groups * c.p.dim * (per_head ? c.p.q_heads : 1) : 0;
+    return c.p.dw && c.groups > 1 ? (int64_t)c.groups * c.p.dim * (per_head ? c.p.q_heads : 1) : 0;
 }
 
 hipError_t do_norm_grad(void *ctx, const RuntimeDevice &d) {

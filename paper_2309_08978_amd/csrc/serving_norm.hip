@@ -393,7 +393,7 @@ norm_rotary_grad_kernel(NormParams p)
         const int g0 = PER_HEAD ? i / p.dim : 0, d = i - g0 * p.dim;
         float sum = 0.f;
         for (int g = g0; g < GROUPS; g += PER_HEAD ? groups : 1) sum += sums[g][d];
-        p.part[((long long)blockIdx.x * (PER_HEAD ? p.q_heads : 1) + h_first + g0) * p.dim + d] = sum;
+        (gridDim.x == 1 ? p.dw : p.part)[((long long)blockIdx.x * (PER_HEAD ? p.q_heads : 1) + h_first + g0) * p.dim + d] = sum;
     }
 }
 
@@ -507,7 +507,9 @@ int norm_grad_groups(int64_t tokens, int64_t heads, int dim, bool per_head, bool
     const int groups = kGradThreads / lanes_per_head(dim, vec);
     const int64_t at_once = per_head ? tokens_per_block_of_heads(groups, (int)heads) : tokens_per_block(groups, (int)heads, 4);
     const int64_t blocks = per_head ? (heads * at_once + groups - 1) / groups : 1;           // of heads
-    const int64_t want = (tokens + at_once - 1) / at_once, most = (2 * cus + blocks - 1) / blocks;
+    // (up to two runs by a lone workgroup, which needs no second launch: 8 tokens of 32 heads 7.2 us, with one 10; but
+    // 20 tokens, five runs, 14.7 alone and 10.2 by five)
+    const int64_t runs = (tokens + at_once - 1) / at_once, want = runs <= 2 ? 1 : runs, most = (2 * cus + blocks - 1) / blocks;
     return (int)(want < 1 ? 1 : want < most ? want : most);      // (no tokens: one adds up nothing)
 }
 
@@ -525,7 +527,7 @@ hipError_t launch_norm_rotary_grad(const NormParams &in, int x_dtype, int dy_dty
     else
         e = dy_dtype == NNJIT_F32 ? launch_grad_typed<_Float16, float>(p, vec, groups, stream)
                                   : launch_grad_typed<_Float16, _Float16>(p, vec, groups, stream);
-    if (e != hipSuccess || !p.dw) return e;
+    if (e != hipSuccess || !p.dw || groups == 1) return e;
     const long long n = (long long)p.dim * (p.qw_head > 0 ? p.q_heads : 1);
     sum_parts_kernel<<<dim3((unsigned)((n + 31) / 32)), 1024, 0, stream>>>(p.part, p.dw, groups, n);
     return hipGetLastError();

@@ -541,17 +541,17 @@ def _plain_lds(A, B, C, sa, sb, sc):
 
 
 _CODES: dict = {}     # torch dtype -> code; filled on first use (torch is imported lazily)
-_F32 = _I32 = None
+_F32 = _I32 = _I64 = None
 _torch_module = None
 _torch_stream = _torch_device = None     # handle of torch's current stream on a GPU; the current GPU (0.1 us each)
 
 
 def _torch():
-    global _F32, _I32, _torch_module, _torch_stream, _torch_device
+    global _F32, _I32, _I64, _torch_module, _torch_stream, _torch_device
     if _torch_module is None:
         import torch
         _CODES.update({torch.float32: NNJIT_F32, torch.float16: NNJIT_F16})
-        _F32, _I32 = torch.float32, torch.int32
+        _F32, _I32, _I64 = torch.float32, torch.int32, torch.int64
         _torch_stream, _torch_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         _torch_module = torch
     return _torch_module
@@ -564,7 +564,8 @@ def _launch(entry, device_index: int, stream, *args) -> int:
     memory."""
     s = _torch_stream(device_index) if stream is None else _stream(stream)
     if _torch_device() == device_index:
-        return check(entry(*args, s))
+        rc = entry(*args, s)
+        return rc if rc >= 0 else check(rc)
     with _torch_module.cuda.device(device_index):
         return check(entry(*args, s))
 
@@ -808,6 +809,16 @@ def _written_rows(name: str, t, tokens, heads, dim, dtype, device_index):
     return st
 
 
+def _rows_in_and_out(name: str, x, out_name: str, out, shape, dtype, out_dtype, device_index):
+    """Strides of head rows x and out of this shape, checked; plain ones by as few tensor accesses as that takes."""
+    sx, so = x.stride(), out.stride()
+    if not (x.shape == shape and out.shape == shape and x.dtype is dtype and out.dtype is out_dtype and sx[2] == 1 and so[2] == 1
+            and so[1] >= shape[2] and so[0] >= so[1] * shape[1] and x.get_device() == device_index and out.get_device() == device_index):
+        sx = _head_rows(name, x, *shape, dtype, device_index)
+        so = _written_rows(out_name, out, *shape, out_dtype, device_index)
+    return sx, so
+
+
 def rotary(x, positions, table: RotaryTable, out=None, transpose: bool = False, stream=None):
     """x [tokens, heads, head_dim] turned by the angles of positions (int32
     [tokens]); ``transpose``: by the opposite ones (the gradient).  ``out``
@@ -1018,12 +1029,12 @@ def kv_append_slots(cache: PagedCache, slots, k, v, positions=None, rotary: Opti
     alone); norms and turns q [tokens, heads, head_dim] of the same type into
     q_out (of the cache's type, allocated if None), which is returned (None without
     q).  ``rotary`` turns by the angles of ``positions`` int32 [tokens]."""
-    torch = _torch()
+    _torch()
     dim, dev, dt = cache.head_dim, cache.device_index, k.dtype
     code = _CODES.get(dt)
     if code is None:
         raise TypeError(f"unsupported dtype {dt}")
-    if slots.dtype is not torch.int64 or slots.dim() != 1 or slots.get_device() != dev or (slots.shape[0] > 1 and slots.stride(0) != 1):
+    if slots.dtype is not _I64 or slots.dim() != 1 or slots.get_device() != dev or (slots.shape[0] > 1 and slots.stride(0) != 1):
         raise ValueError(f"slots must be a contiguous int64 vector on the cache's GPU, got {slots.dtype} {tuple(slots.shape)}")
     n = slots.shape[0]
     pp = None
@@ -1041,11 +1052,13 @@ def kv_append_slots(cache: PagedCache, slots, k, v, positions=None, rotary: Opti
         sv = _head_rows("v", v, n, cache.kv_heads, dim, dt, dev)
     heads, sq, so, qp, op = 0, (0, 0), (0, 0), None, None
     if q is not None:
-        heads = q.shape[1] if q.dim() == 3 else -1
-        sq = _head_rows("q", q, n, heads, dim, dt, dev)
+        shape = q.shape
+        if len(shape) != 3:
+            raise ValueError(f"q must be [tokens, heads, head_dim], got {tuple(shape)}")
+        heads = shape[1]
         if q_out is None:
             q_out = _empty((n, heads, dim), cache.dtype, q.device, stream)
-        so = _written_rows("q_out", q_out, n, heads, dim, cache.dtype, dev)
+        sq, so = _rows_in_and_out("q", q, "q_out", q_out, (n, heads, dim), dt, cache.dtype, dev)
         qp, op = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out without q")
@@ -1096,10 +1109,7 @@ def norm_rotary(x, weight, positions=None, table: Optional[RotaryTable] = None, 
     xd, yd = x.dtype, out.dtype
     if yd not in _CODES:
         raise TypeError(f"unsupported dtype {yd}")
-    sx = x.stride()
-    if sx[2] != 1:
-        sx = _head_rows("x", x, tokens, heads, dim, xd, dev)
-    sy = _written_rows("out", out, tokens, heads, dim, yd, dev)
+    sx, sy = _rows_in_and_out("x", x, "out", out, (tokens, heads, dim), xd, yd, dev)
     _launch((_lib or load()).nnjit_norm_rotary, dev, stream, tp, tokens, heads, dim, pp, weight.data_ptr(), w_head, _CODES[weight.dtype],
             eps, x.data_ptr(), sx[0], sx[1], _CODES[xd], out.data_ptr(), sy[0], sy[1], _CODES[yd])
     return out
@@ -1138,27 +1148,28 @@ def tree_attention(q, cache: PagedCache, batch: PagedBatch, mask, out=None, scal
     [tokens, words], bit i % 32 of word i / 32: new token i) names.  ``window`` > 0: of
     the keys before the new ones the last only, those above positions (int32
     [tokens]) - window.  Otherwise as ``paged_attention``."""
-    torch = _torch()
+    _torch()
     shape = q.shape
     if len(shape) != 3:
         raise ValueError(f"q must be [tokens, heads, head_dim], got {tuple(shape)}")
     heads, dim, dev, n = shape[1], cache.head_dim, cache.device_index, batch.tokens
     if batch.device_index != dev:
         raise ValueError("cache and batch must be on one GPU")
-    if mask.dim() != 2 or mask.shape[0] != n or mask.shape[1] < 1 or mask.dtype is not torch.int32 or mask.get_device() != dev:
-        raise ValueError(f"mask must be int32 [{n}, words] on the cache's GPU, got {mask.dtype} {tuple(mask.shape)}")
-    words, ld = mask.shape[1], mask.stride(0)
-    if words > 1 and mask.stride(1) != 1:
+    ms = mask.shape
+    if len(ms) != 2 or ms[0] != n or ms[1] < 1 or mask.dtype is not _I32 or mask.get_device() != dev:
+        raise ValueError(f"mask must be int32 [{n}, words] on the cache's GPU, got {mask.dtype} {tuple(ms)}")
+    words = ms[1]
+    ld, step = mask.stride()
+    if words > 1 and step != 1:
         raise ValueError("mask must have unit stride along the last dimension")
     pp = None
     if window > 0:
         if positions is None:
             raise ValueError("a window needs positions")
         pp = _step_ints("positions", positions, n, dev)
-    sq = _head_rows("q", q, n, heads, dim, cache.dtype, dev)
     if out is None:
         out = _empty((n, heads, dim), cache.dtype, q.device, stream)
-    so = _written_rows("out", out, n, heads, dim, cache.dtype, dev)
+    sq, so = _rows_in_and_out("q", q, "out", out, (n, heads, dim), cache.dtype, cache.dtype, dev)
     _launch((_lib or load()).nnjit_tree_attention, dev, stream, cache.address, batch.address, mask.data_ptr(), ld, words, pp, heads,
             q.data_ptr(), sq[0], sq[1], out.data_ptr(), so[0], so[1], dim ** -0.5 if scale is None else scale, window)
     return out

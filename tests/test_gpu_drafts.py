@@ -695,6 +695,51 @@ def test_logits_that_are_not_finite():
 
 # --------------------------------------------------- streams, graphs, all together
 
+def test_binding_refuses_operands():
+    """Tensors on the GPU that the entry points would read or write out of bounds; nothing is launched."""
+    r = lambda *shape, dtype=torch.float16: torch.zeros(shape, dtype=dtype, device="cuda")  # noqa: E731
+    cache = nj.PagedCache(r(4, 16, 2, 64), r(4, 16, 2, 64))
+    batch = nj.PagedBatch(_i32([0, 3]), _i32([20]), _i32([[0, 1]]), tokens=3)
+    table, slots, pos = nj.rotary_table(32, 64), torch.zeros(3, dtype=torch.int64, device="cuda"), _i32([0, 1, 2])
+    k, q, w, mask = r(3, 2, 64), r(3, 4, 64), r(64, dtype=torch.float32), _i32([[1]] * 3)
+    step, pool = nj.PagedStep(_i32([[0, 1], [2, 3]]), 16, 8, 1), nj.PagePool(_i32([5, 6]), _i32([2]))
+    rules = nj.LogitRules(history=_i32([[1], [2]]), mask=_i32([[-1], [-1]]))
+    bad = [
+        lambda: nj.kv_append_slots(cache, slots.int(), k, k), lambda: nj.kv_append_slots(cache, slots.cpu(), k, k),
+        lambda: nj.kv_append_slots(cache, slots[:2], k, k), lambda: nj.kv_append_slots(cache, slots, k[:, :1], k),
+        lambda: nj.kv_append_slots(cache, slots, k, k.float()), lambda: nj.kv_append_slots(cache, slots, k, k, rotary=table),
+        lambda: nj.kv_append_slots(cache, slots, k, k, pos[:2], table), lambda: nj.kv_append_slots(cache, slots, k, k, q_out=q),
+        lambda: nj.kv_append_slots(cache, slots, k, k, q=q[0]), lambda: nj.kv_append_slots(cache, slots, k, k, q=q, q_out=q[:, :3]),
+        lambda: nj.kv_append_slots(cache, slots, k, k, q=q, q_out=q[:, :1].expand(3, 4, 64)),
+        lambda: nj.kv_append_slots(cache, slots, k, k, norm=nj.HeadNorm(w[:32])),
+        lambda: nj.kv_append_slots(cache, slots, k, k, norm=nj.HeadNorm(None, r(3, 64))),
+        lambda: nj.kv_append_slots(cache, slots, k, k, q=q, norm=nj.HeadNorm(r(3, 64))),
+        lambda: nj.norm_rotary(q, w[:32]), lambda: nj.norm_rotary(q, r(3, 64)), lambda: nj.norm_rotary(q, w, table=table),
+        lambda: nj.norm_rotary(q, w, pos.long(), table), lambda: nj.norm_rotary(q, w, out=r(3, 4, 32)), lambda: nj.norm_rotary(q, w.cpu()),
+        lambda: nj.norm_rotary(q.transpose(1, 2), r(4)), lambda: nj.norm_rotary(q.double(), w), lambda: nj.norm_rotary(q, w.double()),
+        lambda: nj.norm_rotary_grad(q[:2], q, w), lambda: nj.norm_rotary_grad(q, q, w, dweight=w[:32]),
+        lambda: nj.norm_rotary_grad(q, q, w, dweight=w.half()), lambda: nj.norm_rotary_grad(q, q, w, dx=q.float()),
+        lambda: nj.tree_attention(q, cache, batch, mask[:2]), lambda: nj.tree_attention(q, cache, batch, mask.long()),
+        lambda: nj.tree_attention(q, cache, batch, mask[:, :0]), lambda: nj.tree_attention(q, cache, batch, mask.cpu()),
+        lambda: nj.tree_attention(q, cache, batch, mask, window=3), lambda: nj.tree_attention(q[:2], cache, batch, mask),
+        lambda: nj.tree_attention(q, cache, batch, mask, out=q.float()), lambda: nj.tree_attention(q[:, :3], cache, batch, mask),
+        lambda: nj.tree_attention(q, cache, batch, mask, positions=pos[:2], window=3),
+        lambda: nj.kv_move(cache, batch, _i32([[0], [0]]), _i32([1])), lambda: nj.kv_move(cache, batch, _i32([[0]]), _i32([1, 1])),
+        lambda: nj.kv_move(cache, batch, _i32([[0]]).long(), _i32([1])), lambda: nj.kv_move(cache, batch, _i32([0]), _i32([1])),
+        lambda: nj.paged_step(step, pool, pos, pos[:2]), lambda: nj.paged_step(step, pool, pos[:2].cpu(), pos[:2]),
+        lambda: nj.paged_step(step, pool, pos[:2].long(), pos[:2]), lambda: nj.paged_step(step, pool, pos[:2], pos[:2], keep=pos),
+        lambda: nj.paged_step(step, pool, pos[:2], pos[:2], parent=pos),
+        lambda: nj.paged_step(nj.PagedStep(_i32([[0]]), 16, 8), pool, pos[:1], pos[:1], parent=pos),
+        lambda: nj.adjust_logits(r(3, 32), rules), lambda: nj.adjust_logits(r(2, 33), rules), lambda: nj.adjust_logits(r(2, 32).cpu(), rules),
+        lambda: nj.adjust_logits(r(2, 32), rules, r(2, 31)), lambda: nj.adjust_logits(r(2, 32), rules, r(1, 32).expand(2, 32)),
+        lambda: nj.adjust_logits(r(32, 2).t(), rules), lambda: nj.adjust_logits(r(2, 32, dtype=torch.float64), rules),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises((ValueError, TypeError, nj.NnjitError)):
+            call()
+            raise AssertionError(f"call {i} was not refused")
+
+
 def _calls():
     """name -> (inputs, call of them that returns one tensor)"""
     g = torch.Generator(device="cuda").manual_seed(3)

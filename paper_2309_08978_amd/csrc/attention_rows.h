@@ -86,7 +86,9 @@ __device__ __forceinline__ V load_some(const T *src, int valid, int n)
 // of 128: 110 -> 102 us; two row tiles would lose, 39 -> 46, as would heads of 96
 // dims, 22 -> 27, and of 64, whose loads take half a line, 24 -> 27).
 // TREE: drafted trees: a row sees its sequence's cached keys (with a window from
-// first_cached() on) and the new tokens that its mask names.
+// first_cached() on) and the new tokens that its mask names.  Only tiles of keys that hold new
+// tokens look at masks.  24 nodes behind 1000 keys, 12 heads of 64 in fp32: 7.8 us and 4.4 for
+// the join.
 template <typename T, int DP, bool VEC, bool PAGE16, bool STREAM, int NW, bool TREE>
 __global__ void __launch_bounds__(NW * 64)
 attention_rows_kernel(AttentionParams p)

@@ -184,7 +184,11 @@ template <typename T, int DP, int HOW, int BLOCKS>
 constexpr int waves_per_simd() { return DP <= 128 && lds_bytes<T, DP, HOW, BLOCKS>() <= 80 * 1024 ? 2 : 1; }
 
 // TREE: drafted trees: a row sees its sequence's cached keys (with a window from
-// first_cached() on) and the new tokens that its mask names.
+// first_cached() on) and the new tokens that its mask names.  Only steps that hold new tokens
+// look at masks.  64 nodes behind 65536 keys, 32 heads of 128 on 8, fp16: 97 to 101 us with the join of 32 splits, 690
+// TFLOP/s and 2.7 TB/s of keys and values; 16 sequences of up to 4096 keys with 32 nodes each: 56 us, 3.1 TB/s.
+// (Tiles of 256 rows by eight waves with four stages: 103; eight waves on 128 rows, half of the keys
+// of a step each, with half of the splits: 113 and 61.)
 template <typename T, int DP, int HOW, int WR, int WK, int KB, bool TREE>
 __global__ void __launch_bounds__(WR * WK * 64, (waves_per_simd<T, DP, HOW, KB * WK>()))
 attention_tiles_kernel(AttentionParams p)

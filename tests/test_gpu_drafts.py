@@ -682,6 +682,16 @@ def test_logits_of_long_histories_and_many_biases():
     assert nj.adjust_logits(x, r).cpu()[0, 7] == -32767
 
 
+@pytest.mark.parametrize("src,dst", [("f32", "f32"), ("f16", "f16"), ("f16", "f32")])
+@pytest.mark.parametrize("gap", [0, 3])
+def test_logits_of_many_rows(src, dst, gap):
+    """Segments of each length, their last ones partly beyond the row; histories that could overflow a narrow count."""
+    _logits_case(200, 8193, 90, src, dst, gap=gap)
+    _logits_case(400, 16390, 90, src, dst, gap=gap, mask_rows=5)
+    _logits_case(130, 9000, 33000, src, dst, gap=gap, length=[33000 if i == 0 else i for i in range(130)], mask_rows=5)
+    _logits_case(130, 9000, 33000, src, dst, gap=gap, length=[5000 if i == 0 else i for i in range(130)], mask_rows=5, prompt=False)
+
+
 def test_logits_that_are_not_finite():
     """Infinities and NaN in places that a mask takes away are gone; elsewhere they stay."""
     x = torch.zeros(1, 64, device="cuda")

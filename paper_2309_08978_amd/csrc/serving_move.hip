@@ -27,7 +27,9 @@ kv_move_kernel(MoveParams p, int elem_bytes)
     const int q0 = min(max(batch.q_start[b], 0), batch.tokens);
     const int added = min(max(batch.q_start[b + 1] - q0, 0), batch.tokens - q0);
     const long long room = min((long long)batch.table_pages * p.pool.page_size.d, kMaxKeys);
-    const long long past = (long long)batch.kv_len[b] - added;      // place of the sequence's new token 0
+    // place of the sequence's new token 0: from the starts as they stand, as appends and attention take it, though the
+    // batch may hold fewer rows
+    const long long past = (long long)batch.kv_len[b] - ((long long)batch.q_start[b + 1] - q0);
     const int count = min(max(p.accepted[b], 0), p.path_len);
     const int *table = batch.page_table + (long long)b * batch.ld_table;
 

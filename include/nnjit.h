@@ -578,7 +578,7 @@ typedef struct nnjit_step_arrays {
     int32_t *kv_len;                   /* [sequences]; may be held or keep */
     int32_t *positions;                /* [tokens], or NULL */
     int64_t *slots;                    /* [tokens], or NULL */
-    uint32_t *mask;                    /* [tokens][ld_mask], mask_words used; only with parent */
+    uint32_t *mask;                    /* [tokens][ld_mask], mask_words used; NULL (or 0 words): none, only without parent */
     int64_t ld_mask, mask_words;
     int32_t *status;                   /* [4] */
 } nnjit_step_arrays;
@@ -598,7 +598,9 @@ typedef struct nnjit_step_arrays {
  *   positions[t] keep[b] + the number of t's ancestors among the new tokens
  *   mask[t]      bit i (of word i / 32) set if t sees new token i: its ancestors and itself;
  *                words of rows behind the last sequence are 0
- * and a sequence has up to 32 mask_words new tokens, mask_words <= 32.
+ * and a sequence has up to 32 mask_words new tokens, mask_words <= 32.  Without parent a
+ * mask is filled as well, each sequence's with a chain: new token i sees 0 .. i, as far as the
+ * words go -- longer sequences are for nnjit_paged_attention, which needs no mask.
  * All or nothing: status[0] is 0, or the sum of 1 (pages are missing: status[1] of
  * them), 2 (a length is negative, keep above held, or more keys than the table has
  * columns for or 2^30), 4 (more new rows than tokens, or than mask_words hold), 8 (count

@@ -966,7 +966,8 @@ def paged_step(step: PagedStep, pool: PagePool, held, added, keep=None, parent=N
     """Fills the step's arrays from lengths on the GPU (nnjit_paged_step):
     sequence b holds the pages of held[b] tokens, of which keep[b] (default: all)
     stay, and gets added[b] new ones (int32 [sequences] each).  ``parent`` int32
-    [tokens] makes the new tokens of a sequence a drafted tree.  Unless
+    [tokens] makes the new tokens of a sequence a drafted tree; without it a step with masks
+    gets those of chains (up to the 32 mask_words new tokens that they hold).  Unless
     ``step.status[0]`` is 0 afterwards nothing was changed and the step is empty."""
     _torch()
     n, dev = step.sequences, step.device_index

@@ -118,7 +118,8 @@ int nnjit_paged_step(const nnjit_page_pool *pool, const nnjit_step_arrays *step,
     if (s.sequences > 0 && (!s.held || !s.added || !s.kv_len || (s.table_pages > 0 && !s.page_table)))
         return runtime_fail(NNJIT_EINVAL, "held, added, kv_len or page_table is NULL");
     if (s.kv_len && (s.kv_len == s.added || s.kv_len == s.q_start)) return runtime_fail(NNJIT_EINVAL, "kv_len may be held or keep, not added or q_start");
-    if (s.parent) {
+    const bool masks = s.parent || (s.mask && s.mask_words != 0);
+    if (masks) {
         if (s.mask_words < 1 || s.mask_words > kStepWords)
             return runtime_fail(NNJIT_EINVAL, "mask_words=%lld out of [1, %d]", (long long)s.mask_words, kStepWords);
         if (s.ld_mask < s.mask_words) return runtime_fail(NNJIT_EINVAL, "ld_mask=%lld < %lld words", (long long)s.ld_mask, (long long)s.mask_words);
@@ -139,9 +140,9 @@ int nnjit_paged_step(const nnjit_page_pool *pool, const nnjit_step_arrays *step,
     c.p.kv_len = s.kv_len;
     c.p.positions = s.positions;
     c.p.slots = (long long *)s.slots;
-    c.p.mask = s.mask;
+    c.p.mask = masks ? s.mask : nullptr;
     c.p.ld_mask = s.ld_mask;
-    c.p.mask_words = s.parent ? (int)s.mask_words : 0;
+    c.p.mask_words = masks ? (int)s.mask_words : 0;
     c.p.status = s.status;
     c.p.free_pages = pool->free_pages;
     c.p.capacity = (int)pool->capacity;

@@ -179,6 +179,7 @@ paged_step_kernel(StepParams p)
             if (t >= p.tokens) continue;
             int position = 0;
             long long slot = -1;
+            unsigned *mask_row = p.mask ? p.mask + (long long)t * p.ld_mask : nullptr;
             if (t < end) {
                 const int b = holder(start, n, t), keep = p.keep ? p.keep[b] : p.held[b];
                 const int place = keep + t - start[b], at_page = p.page_size.quot(place), old = old_pages[b];
@@ -187,12 +188,11 @@ paged_step_kernel(StepParams p)
                 position = place;
                 if (p.parent) {
                     const int *own = parents + REACH - (base - start[b]);          // own[i]: parent of the sequence's node i
-                    unsigned *row = p.mask + (long long)t * p.ld_mask;
                     int node = t - start[b], word = p.mask_words - 1, depth = 0;
                     unsigned bits = 0;
                     while (true) {
                         for (; word > node >> 5; --word) {
-                            row[word] = bits;
+                            mask_row[word] = bits;
                             bits = 0;
                         }
                         bits |= 1u << (node & 31);
@@ -202,13 +202,20 @@ paged_step_kernel(StepParams p)
                         ++depth;
                     }
                     for (; word >= 0; --word) {
-                        row[word] = bits;
+                        mask_row[word] = bits;
                         bits = 0;
                     }
                     position = keep + depth;
+                } else if (mask_row) {
+                    // no trees: the chain, as far as the words go
+                    const int node = t - start[b];
+                    for (int w = 0; w < p.mask_words; ++w) {
+                        const int last_bit = node - 32 * w;               // of this word
+                        mask_row[w] = last_bit < 0 ? 0u : last_bit >= 31 ? ~0u : (2u << last_bit) - 1u;
+                    }
                 }
-            } else if (p.parent) {
-                for (int w = 0; w < p.mask_words; ++w) p.mask[(long long)t * p.ld_mask + w] = 0;
+            } else if (mask_row) {
+                for (int w = 0; w < p.mask_words; ++w) mask_row[w] = 0;
             }
             if (p.positions) p.positions[t] = position;
             if (p.slots) p.slots[t] = slot;

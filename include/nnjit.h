@@ -575,7 +575,7 @@ typedef struct nnjit_step_arrays {
     int32_t *page_table;               /* [sequences][ld_table], table_pages used: read and written */
     int64_t ld_table, table_pages, page_size;
     int32_t *q_start;                  /* [sequences + 1], written, as all below */
-    int32_t *kv_len;                   /* [sequences]; may be held or keep */
+    int32_t *kv_len;                   /* [sequences]; may be held or keep, else no part of them, added or q_start */
     int32_t *positions;                /* [tokens], or NULL */
     int64_t *slots;                    /* [tokens], or NULL */
     uint32_t *mask;                    /* [tokens][ld_mask], mask_words used; NULL (or 0 words): none, only without parent */

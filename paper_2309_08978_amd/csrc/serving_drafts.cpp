@@ -117,7 +117,13 @@ int nnjit_paged_step(const nnjit_page_pool *pool, const nnjit_step_arrays *step,
     if (!s.q_start || !s.status) return runtime_fail(NNJIT_EINVAL, "q_start or status is NULL");
     if (s.sequences > 0 && (!s.held || !s.added || !s.kv_len || (s.table_pages > 0 && !s.page_table)))
         return runtime_fail(NNJIT_EINVAL, "held, added, kv_len or page_table is NULL");
-    if (s.kv_len && (s.kv_len == s.added || s.kv_len == s.q_start)) return runtime_fail(NNJIT_EINVAL, "kv_len may be held or keep, not added or q_start");
+    // lengths are replaced in place where kv_len is held or keep as a whole; any other overlap would be read and written at once
+    const auto kv_len_meets = [&](const int32_t *p, int64_t n) {
+        return p && (uintptr_t)p < (uintptr_t)(s.kv_len + s.sequences) && (uintptr_t)s.kv_len < (uintptr_t)(p + n);
+    };
+    if (s.sequences > 0 && (kv_len_meets(s.added, s.sequences) || kv_len_meets(s.q_start, s.sequences + 1) ||
+                            (s.kv_len != s.held && kv_len_meets(s.held, s.sequences)) || (s.kv_len != s.keep && kv_len_meets(s.keep, s.sequences))))
+        return runtime_fail(NNJIT_EINVAL, "kv_len may be held or keep; it must not overlap a part of them, or added or q_start");
     const bool masks = s.parent || (s.mask && s.mask_words != 0);
     if (masks) {
         if (s.mask_words < 1 || s.mask_words > kStepWords)

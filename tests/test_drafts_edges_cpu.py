@@ -25,3 +25,27 @@ def test_masks_without_trees_are_checked():
 def test_no_masks_without_words():
     assert _step(arrays=_arrays(mask=16)) == nj.NNJIT_EHIP
     assert _step(arrays=_arrays(mask_words=99)) == nj.NNJIT_EHIP
+
+
+# ------------------------------------------------------------- memory that is read and written
+
+@pytest.mark.parametrize("arrays", [
+    dict(held=1000, kv_len=1004), dict(held=1004, kv_len=1000), dict(keep=1000, kv_len=1012), dict(keep=1012, kv_len=1000), dict(added=1000, kv_len=1000),
+    dict(added=1000, kv_len=1012), dict(q_start=1000, kv_len=1016), dict(q_start=1016, kv_len=1004), dict(held=1000, keep=1004, kv_len=1000),
+    dict(held=1000, keep=1004, kv_len=1004),
+])
+def test_lengths_that_overlap_in_part(arrays):
+    """kv_len may be held or keep as a whole (a second launch replaces them); it would race with a part of any length."""
+    a = dict(held=4000, keep=5000, added=6000, q_start=7000, kv_len=8000, sequences=4)
+    a.update(arrays)
+    assert _step(arrays=_arrays(**a)) == nj.NNJIT_EINVAL and "kv_len" in nj.nnjit_last_error()
+
+
+@no_gpu
+@pytest.mark.parametrize("arrays", [dict(held=1000, kv_len=1000), dict(keep=1000, kv_len=1000), dict(held=1000, keep=1000, kv_len=1000),
+                                    dict(held=1000, kv_len=1016), dict(held=1016, kv_len=1000), dict(q_start=1000, kv_len=1020),
+                                    dict(added=1016, kv_len=1000)])
+def test_lengths_in_place_or_apart(arrays):
+    a = dict(held=4000, keep=5000, added=6000, q_start=7000, kv_len=8000, sequences=4)
+    a.update(arrays)
+    assert _step(arrays=_arrays(**a)) == nj.NNJIT_EHIP

@@ -702,8 +702,8 @@ typedef struct nnjit_logit_rules {
  *   y = z where the mask allows v, -infinity elsewhere
  * in fp32, rounded once to y's type; a mask that allows nothing leaves only
  * -infinity.  Tokens of the history outside the vocabulary are ignored;
- * a mask row at or behind mask_rows counts as the last.  y may be x (same stride and type); rows of y must not
- * overlap.  rows < 2^20, vocab < 2^30. */
+ * a mask row at or behind mask_rows counts as the last.  y may be x (same stride and type), but not overlap it
+ * otherwise; rows of y must not overlap.  rows < 2^20, vocab < 2^30. */
 int nnjit_adjust_logits(const nnjit_logit_rules *rules, int64_t rows, int64_t vocab, const void *x, int64_t ldx, int x_dtype,
                         void *y, int64_t ldy, int y_dtype, void *stream);
 

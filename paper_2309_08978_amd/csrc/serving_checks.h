@@ -43,6 +43,46 @@ int check_written(const char *name, const void *p, int64_t rows, int64_t heads, 
     return NNJIT_OK;
 }
 
+// Where rows lie: n0 by n1 runs of `width` bytes, s0 and s1 bytes apart.
+struct Laid {
+    const void *p;
+    int64_t n0, s0, n1, s1, width;
+    int dtype;
+};
+
+Laid laid(const void *p, int64_t rows, int64_t row, int64_t heads, int64_t head, int64_t dim, int dtype) {
+    const int64_t e = bytes_of(dtype);
+    return Laid{p, rows, row * e, heads, head * e, dim * e, dtype};
+}
+
+// the very same elements, each at its own place
+bool same_place(const Laid &a, const Laid &b) {
+    return a.p == b.p && a.dtype == b.dtype && a.n0 == b.n0 && a.n1 == b.n1 && a.width == b.width && (a.n0 < 2 || a.s0 == b.s0) && (a.n1 < 2 || a.s1 == b.s1);
+}
+
+// No byte of a is one of b: by their ends, or because both repeat with a period within which they lie
+// apart, as column ranges of one tensor do.  (May say no of rows that mesh otherwise.)
+bool apart(const Laid &a, const Laid &b) {
+    typedef __int128 wide;
+    if (a.n0 < 1 || a.n1 < 1 || b.n0 < 1 || b.n1 < 1 || a.width < 1 || b.width < 1) return true;
+    const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
+    // bytes from the first run's begin to the last one's end, whole periods taken off
+    const auto extent = [](const Laid &l, int64_t period) {
+        wide e = l.width;
+        if (l.n0 > 1 && !(period && l.s0 % period == 0)) e += (wide)(l.n0 - 1) * l.s0;
+        if (l.n1 > 1 && !(period && l.s1 % period == 0)) e += (wide)(l.n1 - 1) * l.s1;
+        return e;
+    };
+    if ((wide)pa + extent(a, 0) <= (wide)pb || (wide)pb + extent(b, 0) <= (wide)pa) return true;
+    const int64_t periods[4] = {a.n0 > 1 ? a.s0 : 0, a.n1 > 1 ? a.s1 : 0, b.n0 > 1 ? b.s0 : 0, b.n1 > 1 ? b.s1 : 0};
+    for (const int64_t period : periods) {
+        if (period <= 0) continue;
+        const wide from = pb >= pa ? (wide)((pb - pa) % (uintptr_t)period) : (wide)((period - (int64_t)((pa - pb) % (uintptr_t)period)) % period);
+        if (extent(a, period) <= from && from + extent(b, period) <= (wide)period) return true;
+    }
+    return false;
+}
+
 int check_dim(int64_t dim) {
     if (dim < 1 || dim > kMaxHeadDim) return runtime_fail(NNJIT_EINVAL, "head_dim=%lld out of [1, %d]", (long long)dim, kMaxHeadDim);
     return NNJIT_OK;

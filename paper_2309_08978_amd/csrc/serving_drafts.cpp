@@ -333,6 +333,8 @@ int nnjit_adjust_logits(const nnjit_logit_rules *rules, int64_t rows, int64_t vo
     if (!r.mask && r.mask_row) return runtime_fail(NNJIT_EINVAL, "mask_row without mask");
     if (rows == 0 || vocab == 0) return NNJIT_OK;
     if (!x || !y) return runtime_fail(NNJIT_EINVAL, "x or y is NULL");
+    const Laid from = laid(x, rows, ldx, 1, 0, vocab, x_dtype), to = laid(y, rows, ldy, 1, 0, vocab, y_dtype);
+    if (!same_place(from, to) && !apart(from, to)) return runtime_fail(NNJIT_EINVAL, "y may be x with its stride and type, but not overlap it otherwise");
     if ((double)rows * (double)((vocab + 1023) / 1024) > (double)kMaxGroups)
         return runtime_fail(NNJIT_EINVAL, "%lld rows of %lld logits in one call: below 2^24 pieces of 1024 are served", (long long)rows, (long long)vocab);
     Call<LogitParams> c;

@@ -627,7 +627,8 @@ typedef struct nnjit_head_norm {
  * angles of positions[t].  norm NULL: no norms; rotary NULL: nothing is
  * turned (positions may then be NULL).  A row whose slot is negative or not in the cache is left
  * alone: nothing is stored, and its row of q_out is not written.  No
- * slot twice.  (Queries alone: nnjit_norm_rotary.) */
+ * slot twice.  q_out may be q (same strides and type), but overlap neither it otherwise
+ * nor k or v.  (Queries alone: nnjit_norm_rotary.) */
 int nnjit_kv_append_slots(const nnjit_paged_kv *cache, int64_t tokens, const int64_t *slots, const int32_t *positions,
                           const nnjit_rotary_table *rotary, const nnjit_head_norm *norm,
                           const void *k, int64_t k_token, int64_t k_head, const void *v, int64_t v_token, int64_t v_head,
@@ -636,7 +637,8 @@ int nnjit_kv_append_slots(const nnjit_paged_kv *cache, int64_t tokens, const int
 
 /* y = the normed rows of x, turned, without a cache: what a training step
  * runs forward.  weight, w_head, w_dtype, eps as nnjit_head_norm's, but
- * weight must be given; rotary NULL: norm only.  y may be x (same strides and type). */
+ * weight must be given; rotary NULL: norm only.  y may be x (same strides and
+ * type), but not overlap it otherwise. */
 int nnjit_norm_rotary(const nnjit_rotary_table *rotary, int64_t tokens, int64_t heads, int64_t head_dim, const int32_t *positions,
                       const void *weight, int64_t w_head, int w_dtype, float eps,
                       const void *x, int64_t x_token, int64_t x_head, int x_dtype,
@@ -646,7 +648,7 @@ int nnjit_norm_rotary(const nnjit_rotary_table *rotary, int64_t tokens, int64_t 
  *   dx = r (g w - x r mean(g w x r)),   dw = sum over rows of g x r
  * (of each head on its own if w_head > 0, dw [heads][head_dim], else of all heads, dw
  * [head_dim]; fp32, overwritten).  dx has x's type and may be dy or x (same
- * strides and type); dx or dw may be NULL.  Sums are added in an order
+ * strides and type), but not overlap them otherwise; dx or dw may be NULL.  Sums are added in an order
  * that depends on the sizes only.  The stream's scratch holds the partial
  * sums of dw. */
 int nnjit_norm_rotary_grad(const nnjit_rotary_table *rotary, int64_t tokens, int64_t heads, int64_t head_dim, const int32_t *positions,

@@ -1108,6 +1108,7 @@ int runtime_launch(hipStream_t stream, int64_t (*floats)(void *ctx, int cus),
         if (rc != NNJIT_OK) return rc;
         RuntimeDevice rd{nullptr, d->zero, d->limits.num_cus};
         const int64_t need = floats ? floats(ctx, rd.cus) : 0;
+        if (need < 0) return (int)need;
         if (need > 0) {
             rc = workspace_for(*d, stream, need, &rd.ws);
             if (rc != NNJIT_OK) return rc;

@@ -220,7 +220,8 @@ struct RuntimeDevice {
 };
 // Readies the current device, takes its stream's scratch and calls
 // launch(ctx, device) under the library's lock; `floats` (may be NULL)
-// returns how much scratch the launch needs on a device of so many CUs.
+// returns how much scratch the launch needs on a device of so many CUs, or
+// the (negative) code of a refusal.
 // Reports errors as the entry points do; lets no exception out.
 int runtime_launch(hipStream_t stream, int64_t (*floats)(void *ctx, int cus), hipError_t (*launch)(void *ctx, const RuntimeDevice &),
                    void *ctx, const char *what);

@@ -60,25 +60,45 @@ bool same_place(const Laid &a, const Laid &b) {
     return a.p == b.p && a.dtype == b.dtype && a.n0 == b.n0 && a.n1 == b.n1 && a.width == b.width && (a.n0 < 2 || a.s0 == b.s0) && (a.n1 < 2 || a.s1 == b.s1);
 }
 
-// No byte of a is one of b: by their ends, or because both repeat with a period within which they lie
-// apart, as column ranges of one tensor do.  (May say no of rows that mesh otherwise.)
+// No byte of a is one of b: by their ends, or because both repeat with a period within which their
+// runs lie apart, as column ranges of one tensor do.  (Says no of runs that mesh over several periods.)
 bool apart(const Laid &a, const Laid &b) {
     typedef __int128 wide;
     if (a.n0 < 1 || a.n1 < 1 || b.n0 < 1 || b.n1 < 1 || a.width < 1 || b.width < 1) return true;
-    const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
-    // bytes from the first run's begin to the last one's end, whole periods taken off
-    const auto extent = [](const Laid &l, int64_t period) {
-        wide e = l.width;
-        if (l.n0 > 1 && !(period && l.s0 % period == 0)) e += (wide)(l.n0 - 1) * l.s0;
-        if (l.n1 > 1 && !(period && l.s1 % period == 0)) e += (wide)(l.n1 - 1) * l.s1;
-        return e;
+    const wide pa = (wide)(uintptr_t)a.p, pb = (wide)(uintptr_t)b.p;
+    // what is left of the runs once whole periods (0: none) are taken off: n runs, s apart; false: still two axes of them
+    struct Runs {
+        wide n, s, width, end;
     };
-    if ((wide)pa + extent(a, 0) <= (wide)pb || (wide)pb + extent(b, 0) <= (wide)pa) return true;
+    const auto runs_of = [](const Laid &l, int64_t period, Runs &r) {
+        const bool more0 = l.n0 > 1 && !(period && l.s0 % period == 0), more1 = l.n1 > 1 && !(period && l.s1 % period == 0);
+        r = Runs{more0 ? l.n0 : more1 ? l.n1 : 1, more0 ? l.s0 : l.s1, l.width, 0};
+        r.end = (more0 ? (wide)(l.n0 - 1) * l.s0 : 0) + (more1 ? (wide)(l.n1 - 1) * l.s1 : 0) + l.width;
+        return !(more0 && more1);
+    };
+    Runs ra, rb;
+    runs_of(a, 0, ra);
+    runs_of(b, 0, rb);
+    if (pa + ra.end <= pb || pb + rb.end <= pa) return true;
     const int64_t periods[4] = {a.n0 > 1 ? a.s0 : 0, a.n1 > 1 ? a.s1 : 0, b.n0 > 1 ? b.s0 : 0, b.n1 > 1 ? b.s1 : 0};
+    // both within one period, b's runs beginning `from` behind a's
+    const auto lie_apart = [](const Runs &a, const Runs &b, wide from, wide period, bool lines) {
+        if (a.end > period || from + b.end > period) return false;
+        if (a.end <= from) return true;
+        if (!lines || a.n > 4096) return false;
+        for (wide i = 0; i < a.n; ++i) {
+            const wide x = i * a.s - from;                               // a's run i, as seen from b's first
+            // the first of b's runs that ends behind x: does it begin before x + width?
+            const wide j = x < b.width ? 0 : b.s > 0 ? (x - b.width) / b.s + 1 : b.n;
+            if (j < b.n && j * b.s < x + a.width) return false;
+        }
+        return true;
+    };
     for (const int64_t period : periods) {
         if (period <= 0) continue;
-        const wide from = pb >= pa ? (wide)((pb - pa) % (uintptr_t)period) : (wide)((period - (int64_t)((pa - pb) % (uintptr_t)period)) % period);
-        if (extent(a, period) <= from && from + extent(b, period) <= (wide)period) return true;
+        const bool lines = runs_of(a, period, ra) & runs_of(b, period, rb);
+        const wide from = ((pb - pa) % period + period) % period;
+        if (lie_apart(ra, rb, from, period, lines) || lie_apart(rb, ra, (period - from) % period, period, lines)) return true;
     }
     return false;
 }

@@ -10,12 +10,18 @@ struct Call {
     P p{};
     bool append = false, vec = false;
     int src = 0, dst = 0, unit = 0, groups = 0;
+    const char *refused = nullptr;        // why, for calls that are looked at once there is a GPU
     hipStream_t stream = nullptr;
 };
 
 hipError_t do_step(void *ctx, const RuntimeDevice &) {
     const auto &c = *(const Call<StepParams> *)ctx;
     return launch_paged_step(c.p, c.stream);
+}
+
+int64_t norm_refused(void *ctx, int) {
+    const auto &c = *(const Call<NormParams> *)ctx;
+    return c.refused ? runtime_fail(NNJIT_EINVAL, "%s", c.refused) : 0;
 }
 
 hipError_t do_norm(void *ctx, const RuntimeDevice &) {
@@ -208,7 +214,11 @@ int nnjit_kv_append_slots(const nnjit_paged_kv *cache, int64_t tokens, const int
     c.src = src_dtype;
     c.dst = cache->dtype;
     c.stream = (hipStream_t)stream;
-    return runtime_launch(c.stream, nullptr, do_norm, &c, "kv_append_slots");
+    const Laid turned = laid(q_out, tokens, qo_token, q_heads, qo_head, dim, cache->dtype), rows = laid(q, tokens, q_token, q_heads, q_head, dim, src_dtype);
+    if (!(same_place(rows, turned) || apart(rows, turned)) || !apart(laid(k, tokens, k_token, cache->kv_heads, k_head, dim, src_dtype), turned) ||
+        !apart(laid(v, tokens, v_token, cache->kv_heads, v_head, dim, src_dtype), turned))
+        c.refused = "q_out may be q with its strides and type, but not overlap it otherwise, nor k or v";
+    return runtime_launch(c.stream, norm_refused, do_norm, &c, "kv_append_slots");
 }
 
 int nnjit_norm_rotary(const nnjit_rotary_table *rotary, int64_t tokens, int64_t heads, int64_t head_dim, const int32_t *positions,
@@ -235,7 +245,9 @@ int nnjit_norm_rotary(const nnjit_rotary_table *rotary, int64_t tokens, int64_t 
     c.src = x_dtype;
     c.dst = y_dtype;
     c.stream = (hipStream_t)stream;
-    return runtime_launch(c.stream, nullptr, do_norm, &c, "norm_rotary");
+    const Laid from = laid(x, tokens, x_token, heads, x_head, head_dim, x_dtype), to = laid(y, tokens, y_token, heads, y_head, head_dim, y_dtype);
+    if (!same_place(from, to) && !apart(from, to)) c.refused = "y may be x with its strides and type, but not overlap it otherwise";
+    return runtime_launch(c.stream, norm_refused, do_norm, &c, "norm_rotary");
 }
 
 int nnjit_norm_rotary_grad(const nnjit_rotary_table *rotary, int64_t tokens, int64_t heads, int64_t head_dim, const int32_t *positions,
@@ -254,6 +266,12 @@ int nnjit_norm_rotary_grad(const nnjit_rotary_table *rotary, int64_t tokens, int
     if (tokens * heads > kMaxInt || (w_head > 0 && heads > 0xffff))
         return runtime_fail(NNJIT_EINVAL, "%lld rows of %lld heads in one call: below 2^31 rows (a weight a head: 2^16 heads) are served",
                             (long long)tokens, (long long)heads);
+    if (dx) {
+        const Laid to = laid(dx, tokens, dx_token, heads, dx_head, head_dim, x_dtype);
+        for (const Laid &from : {laid(x, tokens, x_token, heads, x_head, head_dim, x_dtype), laid(dy, tokens, dy_token, heads, dy_head, head_dim, dy_dtype)})
+            if (!same_place(from, to) && !apart(from, to))
+                return runtime_fail(NNJIT_EINVAL, "dx may be x or dy with its strides and type, but not overlap them otherwise");
+    }
     Call<NormParams> c;
     c.p.q = HeadRows{x, x_token, x_head};
     c.p.qo = HeadRows{dx, dx_token, dx_head};

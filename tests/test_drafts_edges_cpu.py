@@ -1,10 +1,11 @@
 """Host-side tests of what the entry points of a step of drafted tokens take and
 refuse beyond the plain cases (no GPU)."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2309_08978_amd as nj
-from tests.test_drafts_cpu import _arrays, _logits, _step
+from tests.test_drafts_cpu import _arrays, _grad, _logits, _step
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -75,3 +76,64 @@ def test_logits_that_overlap(call):
 @pytest.mark.parametrize("call", FINE)
 def test_logits_in_place_or_apart(call):
     assert _logits(**{**dict(rows=4, x=100000), **call}) == nj.NNJIT_EHIP
+
+
+# 3 tokens of 2 heads of 32 dims; x (64, 32) floats apart from address 100000 on, dy and dx by default far away
+@pytest.mark.parametrize("call", [
+    dict(dx=100000, dxst=(96, 32)), dict(dx=100000, dxst=(32, 96)), dict(dx=100004), dict(dx=100128), dict(dx=99900),
+    dict(dy=200000, dx=200000, dyd=1), dict(dy=200000, dx=200128), dict(dy=200000, dyst=(0, 0), dx=200000),
+    dict(dy=200000, dyst=(64, 0), dx=200000), dict(dy=200124, dyst=(128, 32), dx=200000, dxst=(128, 96)),
+    dict(dy=200132, dyst=(128, 32), dx=200000, dxst=(128, 96)), dict(dy=200512, dyst=(256, 32), dyd=1, dx=200000, dxst=(128, 32), x=400000),
+])
+def test_gradients_that_overlap(call):
+    assert _grad(**{**dict(tokens=3, x=100000, dy=200000, dx=300000), **call}) == nj.NNJIT_EINVAL and "overlap" in nj.nnjit_last_error()
+
+
+@no_gpu
+@pytest.mark.parametrize("call", [
+    dict(), dict(dx=100000), dict(dx=200000), dict(dy=100000), dict(dx=100768), dict(dx=99232), dict(dy=200000, dyd=1, dx=200384),
+    dict(dy=200128, dyst=(128, 64), dx=200000, dxst=(128, 64)),                 # sides of each head
+    dict(dy=200256, dyst=(128, 32), dx=200000, dxst=(128, 32)),                 # heads of each token
+    dict(dy=200000, dyst=(32, 200), dx=200384, dxst=(32, 200)),                 # tokens of each head
+    dict(dy=200128, dyst=(128, 32), dx=200000, dxst=(128, 96)),                 # heads between the heads
+    dict(dy=200256, dyst=(256, 32), dyd=1, dx=200000, dxst=(128, 32), x=400000),    # a half row of fp16 behind a row of fp32
+])
+def test_gradients_in_place_or_apart(call):
+    assert _grad(**{**dict(tokens=3, x=100000, dy=200000, dx=300000), **call}) == nj.NNJIT_EHIP
+
+
+@no_gpu
+def test_overlaps_are_those_of_the_bytes():
+    """Random strides: what is refused or not, against the sets of bytes; in place only with the same strides and type."""
+    rng = np.random.default_rng(0)
+    seen = {True: 0, False: 0, "careful": 0}
+    for _ in range(4000):
+        dim, heads, tokens = int(rng.integers(1, 5)), int(rng.integers(1, 4)), int(rng.integers(1, 4))
+
+        def rows(most):
+            if rng.random() < 0.5:
+                head = dim + int(rng.integers(0, 4))
+                return (heads - 1) * head + dim + int(rng.integers(0, most)), head
+            token = dim + int(rng.integers(0, 4))
+            return token, (tokens - 1) * token + dim + int(rng.integers(0, most))
+
+        dxst, half = rows(12), int(rng.integers(0, 2))
+        dyst = tuple(dxst) if rng.random() < 0.6 else rows(12)
+        if half and rng.random() < 0.6:
+            dyst = (2 * dxst[0], 2 * dxst[1])
+        dx = 1 << 20
+        dy = dx + 4 * int(rng.integers(-30, 30)) + 2 * half * int(rng.integers(0, 2))
+
+        def bytes_of(p, st, e):
+            return {p + e * (t * st[0] + h * st[1]) + i for t in range(tokens) for h in range(heads) for i in range(dim * e)}
+
+        meet = bool(bytes_of(dx, dxst, 4) & bytes_of(dy, dyst, 2 if half else 4))
+        same = dx == dy and not half and (tokens == 1 or dxst[0] == dyst[0]) and (heads == 1 or dxst[1] == dyst[1])
+        rc = _grad(tokens=tokens, heads=heads, dim=dim, x=1 << 30, dy=dy, dyst=dyst, dyd=half, dx=dx, dxst=dxst)
+        refused = rc == nj.NNJIT_EINVAL and "overlap them otherwise" in nj.nnjit_last_error()
+        assert refused or rc == nj.NNJIT_EHIP
+        if meet and not same:
+            assert refused, (tokens, heads, dim, dxst, dyst, half, dy - dx)
+        seen[refused] += 1
+        seen["careful"] += refused and not meet
+    assert seen[True] > 500 and seen[False] > 500 and seen["careful"] < 0.1 * seen[True], seen

@@ -59,6 +59,62 @@ def test_chain_masks_serve_tree_attention():
     assert (np.abs(got.double().cpu().numpy() - want) <= bound + 2.0 ** -24 * np.abs(want)).all()
 
 
+# ------------------------------------------------- norms: memory read and written
+
+def _qkv(dtype=torch.float16, heads=10, dim=64, tokens=70):
+    return torch.randn(tokens, heads, dim, device="cuda", generator=torch.Generator("cuda").manual_seed(1)).to(dtype)
+
+
+def test_norms_that_overlap_are_refused():
+    """Results over their operands with another type, stride or begin; nothing is launched."""
+    w, rows, slots = torch.ones(64, device="cuda"), _qkv(torch.float32), torch.arange(70, device="cuda")
+    kept = rows.clone()
+    x, halves = rows[:, :4], rows.view(torch.float16).view(70, 10, 2, 64)
+    cache = nj.PagedCache(*(torch.zeros(5, 16, 2, 64, dtype=torch.float16, device="cuda") for _ in range(2)))
+    other = nj.PagedCache(cache.k.float(), cache.v.float())
+    fp16 = torch.as_strided(rows.view(torch.float16), (70, 4, 64), (640, 64, 1))
+    bad = [
+        lambda: nj.norm_rotary(x, w, out=fp16), lambda: nj.norm_rotary(x, w, out=rows[:, 1:5]), lambda: nj.norm_rotary(x[1:], w, out=x[:-1]),
+        lambda: nj.norm_rotary(x, w, out=halves[:, :4, 0]), lambda: nj.norm_rotary(x, w, out=torch.as_strided(rows, (70, 4, 64), (512, 64, 1))),
+        lambda: nj.kv_append_slots(cache, slots, rows[:, 4:6], rows[:, 6:8], q=x, q_out=fp16),
+        lambda: nj.kv_append_slots(other, slots, rows[:, 4:6], rows[:, 6:8], q=x, q_out=rows[:, 1:5]),
+        lambda: nj.kv_append_slots(other, slots, rows[:, 4:6], rows[:, 8:10], q=x, q_out=rows[:, 5:9]),
+        lambda: nj.kv_append_slots(other, slots, rows[:, 8:10], rows[:, 4:6], q=x, q_out=rows[:, 5:9]),
+        lambda: nj.norm_rotary_grad(x, rows[:, 6:], w, dx=rows[:, 3:7]), lambda: nj.norm_rotary_grad(fp16, kept[:, :4], w, dx=x),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(nj.NnjitError, match="overlap"):
+            call()
+            raise AssertionError(f"call {i} was not refused")
+    torch.cuda.synchronize()
+    assert torch.equal(rows, kept)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_norms_in_place_and_side_by_side(dtype):
+    """Operands and results that are column ranges of one tensor; queries turned in place in a packed projection."""
+    w, table, pos = torch.rand(64, device="cuda") + 0.5, nj.rotary_table(100, 64), torch.arange(70, dtype=torch.int32, device="cuda")
+    rows = _qkv(dtype)
+    want = nj.norm_rotary(rows[:, :4], w, pos, table)
+    side = rows.clone()
+    nj.norm_rotary(side[:, :4], w, pos, table, out=side[:, 4:8])
+    assert torch.equal(side[:, 4:8], want) and torch.equal(side[:, :4], rows[:, :4]) and torch.equal(side[:, 8:], rows[:, 8:])
+    slots = torch.randperm(80, device="cuda")[:70]
+    slots[[3, 69]] = -1
+    made = []
+    for in_place in (False, True):
+        cache = nj.PagedCache(*(torch.zeros(5, 16, 2, 64, dtype=dtype, device="cuda") for _ in range(2)))
+        qkv = rows.clone()
+        q = qkv[:, :4]
+        out = q if in_place else q.clone()
+        nj.kv_append_slots(cache, slots, qkv[:, 4:6], qkv[:, 6:8], pos, table, q, out, nj.HeadNorm(w, w))
+        assert torch.equal(qkv[:, 4:], rows[:, 4:]) and torch.equal(out[[3, 69]], rows[[3, 69], :4])
+        made.append((out.clone(), cache.k, cache.v))
+    assert all(torch.equal(a, b) for a, b in zip(*made))
+    keep = slots >= 0
+    assert torch.equal(made[0][0][keep], want[keep])
+
+
 # ---------------------------------------------------------------- moves
 
 @pytest.mark.parametrize("rows", [14, 11, 7, 5])

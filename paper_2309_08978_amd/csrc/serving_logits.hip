@@ -90,9 +90,10 @@ adjust_logits_kernel(LogitParams p, int segments, int segment)
     for (int i = tid; i < N::kWords * SEGMENT / 4; i += THREADS) ((u32x4 *)noted)[i] = u32x4{0, 0, 0, 0};
     __syncthreads();
     if (p.bias_token) {
-        for (int i = tid; i < p.bias_len; i += THREADS) {
-            const unsigned v = (unsigned)(i == tid ? first_bias : bias_tokens[i]) - (unsigned)v0;   // (a negative token lies above every segment)
-            if (v < (unsigned)here) atomicMax(&entries[v], (unsigned)i + 1u);
+        // (unsigned: the last step of lists of almost 2^31 entries passes 31 bits)
+        for (unsigned i = tid; i < (unsigned)p.bias_len; i += THREADS) {
+            const unsigned v = (unsigned)(i == (unsigned)tid ? first_bias : bias_tokens[i]) - (unsigned)v0;   // (a negative token lies above every segment)
+            if (v < (unsigned)here) atomicMax(&entries[v], i + 1u);
         }
         if (NARROW) __syncthreads();                                   // (counts lie above the entries)
     }
@@ -106,7 +107,7 @@ adjust_logits_kernel(LogitParams p, int segments, int segment)
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) note(k * THREADS + tid, first[k]);
 #pragma unroll 4
-        for (int i = AHEAD * THREADS + tid; i < length; i += THREADS) note(i, tokens[i]);
+        for (unsigned i = AHEAD * THREADS + tid; i < (unsigned)length; i += THREADS) note((int)i, tokens[i]);
     }
     __syncthreads();
 

@@ -137,3 +137,20 @@ def test_move_with_fewer_rows_than_the_starts_say(rows, dtype):
                     want[m - n + i] = before[slots[m - n + p]]
             for s, w in zip(slots, want):
                 assert torch.equal(after[s], w)
+
+
+# ---------------------------------------------------------------- logits
+
+def test_logits_of_the_longest_lists():
+    """Histories and biases of as many entries as a call takes: their last ones count, and the walk ends there."""
+    n, vocab = (1 << 31) - 1, 8
+    x = torch.full((1, vocab), 2.0, device="cuda")
+    history = torch.full((1, n), -1, dtype=torch.int32, device="cuda")
+    history[0, 0], history[0, n // 2], history[0, n - 1], history[0, n - 2] = 3, 3, 3, 5
+    ones = torch.ones(1, device="cuda")
+    y = nj.adjust_logits(x, nj.LogitRules(history=history, prompt=_i32([1]), frequency=ones, presence=ones)).cpu()
+    assert y.tolist() == [[2.0, 2.0, 2.0, -1.0, 2.0, 0.0, 2.0, 2.0]]
+    tokens, values = history[:, :n - 1], torch.zeros((1, n), device="cuda")[:, :n - 1]
+    values[0, 0], values[0, n // 2], values[0, n - 2] = 1.0, 4.0, 8.0
+    y = nj.adjust_logits(x, nj.LogitRules(bias_token=tokens, bias_value=values)).cpu()
+    assert y.tolist() == [[2.0, 2.0, 2.0, 6.0, 2.0, 10.0, 2.0, 2.0]]

@@ -30,7 +30,7 @@ kv_move_kernel(MoveParams p, int elem_bytes)
     // place of the sequence's new token 0: from the starts as they stand, as appends and attention take it, though the
     // batch may hold fewer rows
     const long long past = (long long)batch.kv_len[b] - ((long long)batch.q_start[b + 1] - q0);
-    const int count = min(max(p.accepted[b], 0), p.path_len);
+    const int count = min(min(max(p.accepted[b], 0), p.path_len), added);     // (entries read behind their own place: none from `added` on)
     const int *table = batch.page_table + (long long)b * batch.ld_table;
 
     const int pieces = p.row_bytes / (int)sizeof(U);                 // of a head's row
@@ -42,12 +42,13 @@ kv_move_kernel(MoveParams p, int elem_bytes)
                  (long long)(in - head * pieces) * sizeof(U);
     const unsigned page_stride = value ? p.pool.v_page : p.pool.k_page, slot_stride = value ? p.pool.v_tok : p.pool.k_tok;
 
-    for (int first = 0; first < count; first += kEntries) {
-        const int i = first + i0;
-        if (first > 0) from = i < p.path_len ? path[i] : -1;
+    // (unsigned: the last step of almost 2^31 entries passes 31 bits)
+    for (unsigned first = 0; first < (unsigned)count; first += kEntries) {
+        const unsigned i = first + i0;
+        if (first > 0) from = i < (unsigned)p.path_len ? path[i] : -1;
         // (an entry at its own place is there already)
         const long long src = past + from, dst = past + i;
-        bool moves = mine && i < count && from > i && from < added && dst >= 0 && src < room;
+        bool moves = mine && i < (unsigned)count && from > (int)i && from < added && dst >= 0 && src < room;
         U kept = {};
         U *to = nullptr;
         if (moves) {

@@ -139,6 +139,22 @@ def test_move_with_fewer_rows_than_the_starts_say(rows, dtype):
                 assert torch.equal(after[s], w)
 
 
+def test_moves_along_the_longest_path():
+    """A path of as many entries as a call takes, all accepted, says the lengths; those that the sequence has move."""
+    n = (1 << 31) - 1
+    path = torch.zeros((1, n), dtype=torch.int32, device="cuda")
+    path[0, :4] = _i32([1, 3, 4, 6])
+    B = Batch([7], [30], 2, 2, 64, 16, "f16", seed=4).device()
+    rows = [B.k[s].clone() for s in B.key_slots(0)]
+    batch = nj.PagedBatch(_i32([0, 7]), _i32(B.keys), B.batch.page_table, tokens=7)
+    nj.kv_move(B.cache, batch, path, _i32([n]))
+    want = list(rows)
+    want[23], want[24], want[25], want[26] = rows[24], rows[26], rows[27], rows[29]
+    torch.cuda.synchronize()
+    for s, w in zip(B.key_slots(0), want):
+        assert torch.equal(B.dk[s].cpu(), w)
+
+
 # ---------------------------------------------------------------- logits
 
 def test_logits_of_the_longest_lists():

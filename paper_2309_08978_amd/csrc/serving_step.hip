@@ -157,11 +157,12 @@ paged_step_kernel(StepParams p)
         const int page_stride = page_groups * THREADS;
         const int page_first = has_pages ? (gridDim.x > 1 ? (int)blockIdx.x - row_groups : 0) * THREADS + tid : 0x7fffffff;
         for (int b = page_first; b <= n; b += page_stride) p.q_start[b] = start[b];
-        for (int i = page_first; i < pages; i += page_stride) {
-            const int b = holder(more, n, i);
+        // (unsigned: a step behind the last of almost 2^31 pages passes 31 bits)
+        for (unsigned at = page_first; at < (unsigned)pages; at += page_stride) {
+            const int i = at, b = holder(more, n, i);
             p.page_table[(long long)b * p.ld_table + old_pages[b] + i - more[b]] = page_taken(i);
         }
-        for (int i = page_first; i < pushes; i += page_stride) p.free_pages[count + i] = given_back(i);
+        for (unsigned at = page_first; at < (unsigned)pushes; at += page_stride) p.free_pages[count + at] = given_back(at);
         if (blockIdx.x == 0 && tid < 4)
             p.status[tid] = tid == 0 ? bad : tid == 1 ? (int)min(missing, 0x7fffffffll) : tid == 2 ? (bad ? 0 : (int)all_rows) : left;
 

@@ -59,6 +59,23 @@ def test_chain_masks_serve_tree_attention():
     assert (np.abs(got.double().cpu().numpy() - want) <= bound + 2.0 ** -24 * np.abs(want)).all()
 
 
+def test_a_step_of_almost_all_the_pages_that_a_pool_can_hold():
+    """Sequences that end give back 2^31 - 8192 pages in their order; the next step's rows take the last of them."""
+    n, columns, rows = 8192, (1 << 18) - 1, (1 << 24) - 1
+    given = n * columns
+    table = torch.arange(given, dtype=torch.int32, device="cuda").view(n, columns)
+    free, count = torch.full(((1 << 31) - 1,), -3, dtype=torch.int32, device="cuda"), _i32([0])
+    pool, step = nj.PagePool(free, count), nj.PagedStep(table, 1, rows)
+    none = torch.zeros(n, dtype=torch.int32, device="cuda")
+    nj.paged_step(step, pool, torch.full_like(none, columns), none, keep=none)
+    assert step.status.tolist() == [0, 0, 0, given] and count.tolist() == [given]
+    assert torch.equal(free[:given].view(n, columns), table) and bool((free[given:] == -3).all())
+    nj.paged_step(step, pool, step.kv_len, torch.full_like(none, 2047))
+    assert step.status.tolist() == [0, 0, 2047 * n, given - 2047 * n]
+    want = free[given - 2047 * n:given].flip(0)
+    assert torch.equal(table[:, :2047].reshape(-1), want) and torch.equal(step.slots[:2047 * n], want.long())
+
+
 # ------------------------------------------------- norms: memory read and written
 
 def _qkv(dtype=torch.float16, heads=10, dim=64, tokens=70):

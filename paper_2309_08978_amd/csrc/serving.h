@@ -208,6 +208,11 @@ struct LogitParams {
     void *y;
     long long ldx, ldy;
 };
+// The kernel that a call gets: threads of a workgroup, groups of four tokens a thread, one word of LDS a token (or two).
+struct LogitPlan {
+    int threads, quads, narrow;
+};
+LogitPlan logit_plan(int64_t rows, int64_t vocab, int64_t history_len, int64_t bias_len, int cus);
 hipError_t launch_adjust_logits(const LogitParams &p, int x_dtype, int y_dtype, bool vec, int cus, hipStream_t stream);
 
 // Runtime services for entry points outside runtime.cpp.

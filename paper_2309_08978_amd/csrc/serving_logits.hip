@@ -153,24 +153,33 @@ hipError_t launch_as(const LogitParams &p, bool vec, hipStream_t stream)
 template <typename S, typename D>
 hipError_t launch_typed(const LogitParams &p, bool vec, int cus, hipStream_t stream)
 {
-    // Long segments read the history seldom, short ones spread a call over more compute units; many threads read it in
-    // fewer steps and start later.  By 512 threads of 4 tokens, 1024 of 4, of 8 and of 16, histories of 4000, in us:
-    //   1 row of 32000 in fp32        3.9   4.3   5.2   7.0   (histories of 16000: 7.0   6.1   7.0   9.0)
-    //   8 rows of 128000 in fp32      4.9   4.8   5.5   7.0
-    //   32 rows of 128000 in fp16    11.0  10.5   8.2   8.6
-    //   64 rows of 128000 in fp16    18.1  18.0  13.5  12.7
-    // Two words a token: 16 leave one workgroup a compute unit: 64 rows, histories of 33000 28.8 with 8, 32.6 with 16.
-    const bool narrow = p.history_len < 1 << 15 && p.bias_len < 1 << 16;
-    auto groups = [&](int segment) { return (long long)p.rows * ((p.vocab + segment - 1) / segment); };
-    if (narrow && p.history_len <= 4096 && groups(2048) <= cus) return launch_as<S, D, true, 512, 1>(p, vec, stream);
-    if (groups(4096) <= cus) return narrow ? launch_as<S, D, true, 1024, 1>(p, vec, stream) : launch_as<S, D, false, 1024, 1>(p, vec, stream);
-    // (with 16 two fit a compute unit at once: not for a few that are left over: 300 rows of 20000 in fp16 15.6, with 8 14.6)
-    const long long longest = groups(16384), over = longest % (2 * cus);
-    if (narrow && (over == 0 || 2 * over >= 3 * cus || longest >= 8ll * cus)) return launch_as<S, D, true, 1024, 4>(p, vec, stream);
-    return narrow ? launch_as<S, D, true, 1024, 2>(p, vec, stream) : launch_as<S, D, false, 1024, 2>(p, vec, stream);
+    const LogitPlan plan = logit_plan(p.rows, p.vocab, p.history_len, p.bias_len, cus);
+    if (plan.threads == 512) return launch_as<S, D, true, 512, 1>(p, vec, stream);
+    if (plan.quads == 4) return launch_as<S, D, true, 1024, 4>(p, vec, stream);
+    if (plan.quads == 2) return plan.narrow ? launch_as<S, D, true, 1024, 2>(p, vec, stream) : launch_as<S, D, false, 1024, 2>(p, vec, stream);
+    return plan.narrow ? launch_as<S, D, true, 1024, 1>(p, vec, stream) : launch_as<S, D, false, 1024, 1>(p, vec, stream);
 }
 
 }  // namespace
+
+// Long segments read the history seldom, short ones spread a call over more compute units; many threads read it in
+// fewer steps and start later.  By 512 threads of 4 tokens, 1024 of 4, of 8 and of 16, histories of 4000, in us:
+//   1 row of 32000 in fp32        3.9   4.3   5.2   7.0   (histories of 16000: 7.0   6.1   7.0   9.0)
+//   8 rows of 128000 in fp32      4.9   4.8   5.5   7.0
+//   32 rows of 128000 in fp16    11.0  10.5   8.2   8.6
+//   64 rows of 128000 in fp16    18.1  18.0  13.5  12.7
+// Two words a token: 16 leave one workgroup a compute unit: 64 rows, histories of 33000 28.8 with 8, 32.6 with 16.
+LogitPlan logit_plan(int64_t rows, int64_t vocab, int64_t history_len, int64_t bias_len, int cus)
+{
+    const int narrow = history_len < 1 << 15 && bias_len < 1 << 16;
+    auto groups = [&](int64_t segment) { return rows * ((vocab + segment - 1) / segment); };
+    if (narrow && history_len <= 4096 && groups(2048) <= cus) return LogitPlan{512, 1, narrow};
+    if (groups(4096) <= cus) return LogitPlan{1024, 1, narrow};
+    // (with 16 two fit a compute unit at once: not for a few that are left over: 300 rows of 20000 in fp16 15.6, with 8 14.6)
+    const int64_t longest = groups(16384), over = longest % (2 * cus);
+    if (narrow && (over == 0 || 2 * over >= 3 * cus || longest >= 8ll * cus)) return LogitPlan{1024, 4, narrow};
+    return LogitPlan{1024, 2, narrow};
+}
 
 hipError_t launch_adjust_logits(const LogitParams &p, int x_dtype, int y_dtype, bool vec, int cus, hipStream_t stream)
 {

@@ -289,3 +289,30 @@ def words_of(allowed):
     padded[:, :vocab] = allowed
     w = (padded.reshape(rows, -1, 32) << np.arange(32, dtype=np.uint64)).sum(-1).astype(np.uint32)
     return torch.from_numpy(w.view(np.int32))
+
+
+class LogitPlan(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("threads", "quads", "narrow")]
+
+
+def logit_plan(rows, vocab, history, biases=60, cus=256) -> LogitPlan:
+    """nnjit::logit_plan (csrc/serving.h)."""
+    f = nj.load(build_if_missing=True)._ZN5nnjit10logit_planElllli
+    f.restype, f.argtypes = LogitPlan, [ctypes.c_int64] * 4 + [ctypes.c_int]
+    return f(rows, vocab, history, biases, cus)
+
+
+# (rows, vocab, history, threads, groups of four tokens a thread, one word of LDS a token): every kernel of the logit rules,
+# rows of one segment and of several, with last segments that hold little
+LOGIT_COVER = [
+    (5, 4097, 64, 512, 1, True),
+    (2, 130, 4096, 512, 1, True),
+    (3, 9001, 5000, 1024, 1, True),
+    (130, 4099, 90, 1024, 2, True),
+    (3, 9001, 33000, 1024, 1, False),
+    (300, 9001, 50, 1024, 2, True),
+    (130, 9000, 33000, 1024, 2, False),
+    (256, 16390, 90, 1024, 4, True),
+    (400, 9001, 50, 1024, 4, True),
+    (2100, 701, 20, 1024, 4, True),
+]

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2309_08978_amd as nj
+from tests.drafts_util import LOGIT_COVER, logit_plan
 from tests.test_drafts_cpu import _arrays, _grad, _logits, _step
 
 
@@ -137,3 +138,28 @@ def test_overlaps_are_those_of_the_bytes():
         seen[refused] += 1
         seen["careful"] += refused and not meet
     assert seen[True] > 500 and seen[False] > 500 and seen["careful"] < 0.1 * seen[True], seen
+
+
+# ------------------------------------------------------------- which kernel a row of logits gets
+
+@pytest.mark.parametrize("case", LOGIT_COVER, ids=str)
+def test_kernel_of_logits(case):
+    rows, vocab, history, threads, quads, narrow = case
+    p = logit_plan(rows, vocab, history)
+    assert (p.threads, p.quads, bool(p.narrow)) == (threads, quads, narrow)
+
+
+def test_logit_cover_is_whole():
+    """All that the rule of choice ever gives is among the covered cases."""
+    rng = np.random.default_rng(0)
+    have = {c[3:] for c in LOGIT_COVER}
+    for _ in range(20000):
+        p = logit_plan(int(2 ** rng.uniform(0, 20)), int(2 ** rng.uniform(0, 18)), int(2 ** rng.uniform(0, 17)), int(2 ** rng.uniform(0, 18)))
+        assert (p.threads, p.quads, bool(p.narrow)) in have
+    assert len(have) == 6
+
+
+def test_counts_and_entries_fit_their_words():
+    """One word a token: 15 bits of count above 16 of entry, the last bit for the prompt."""
+    assert logit_plan(64, 128000, (1 << 15) - 1, (1 << 16) - 1).narrow
+    assert not logit_plan(64, 128000, 1 << 15, 60).narrow and not logit_plan(64, 128000, 100, 1 << 16).narrow

@@ -6,8 +6,9 @@ import pytest
 import torch
 
 import paper_2309_08978_amd as nj
-from tests.drafts_util import attention_of, signed, tree_seen
+from tests.drafts_util import LOGIT_COVER, attention_of, signed, tree_seen
 from tests.serving_util import Batch
+from tests.test_gpu_drafts import _logits_case
 
 pytestmark = pytest.mark.gpu
 
@@ -187,3 +188,16 @@ def test_logits_of_the_longest_lists():
     values[0, 0], values[0, n // 2], values[0, n - 2] = 1.0, 4.0, 8.0
     y = nj.adjust_logits(x, nj.LogitRules(bias_token=tokens, bias_value=values)).cpu()
     assert y.tolist() == [[2.0, 2.0, 2.0, 6.0, 2.0, 10.0, 2.0, 2.0]]
+
+
+@pytest.mark.parametrize("case", LOGIT_COVER, ids=str)
+@pytest.mark.parametrize("src,dst", [("f32", "f32"), ("f32", "f16"), ("f16", "f32"), ("f16", "f16")])
+def test_every_kernel_of_logits(case, src, dst):
+    """Rows that are taken four tokens at a time and rows of no alignment, with a mask a row and with grammars; in place."""
+    rows, vocab, history = case[:3]
+    gap = -vocab % 4
+    length = [history] + list(range(1, rows)) if history > 4096 else None          # (one long one: the plain form counts slowly)
+    _logits_case(rows, vocab, history, src, dst, gap=gap, mask_rows=5, length=length, seed=2)
+    _logits_case(rows, vocab, history, src, dst, gap=gap + 1, shift=1, length=length, seed=3)
+    if src == dst:
+        _logits_case(rows, vocab, history, src, dst, gap=gap, length=length, in_place=True, seed=4)

@@ -6,9 +6,9 @@ import pytest
 import torch
 
 import paper_2309_08978_amd as nj
-from tests.drafts_util import LOGIT_COVER, attention_of, signed, tree_seen
-from tests.serving_util import Batch
-from tests.test_gpu_drafts import _logits_case
+from tests.drafts_util import LOGIT_COVER, attention_of, normed, signed, tree_seen, turned_with_bound
+from tests.serving_util import DT, Batch, rounded
+from tests.test_gpu_drafts import _angles, _inside, _logits_case, _np, _rows
 
 pytestmark = pytest.mark.gpu
 
@@ -131,6 +131,88 @@ def test_norms_in_place_and_side_by_side(dtype):
     assert all(torch.equal(a, b) for a, b in zip(*made))
     keep = slots >= 0
     assert torch.equal(made[0][0][keep], want[keep])
+
+
+# ------------------------------------------------------- norms of many rows
+
+# (tokens, query heads, key heads, dim, rotary dims, layout, elements before the first row, a weight a head, source, cache): 1024
+# tokens and more have workgroups of several tokens, whose last one may hold fewer; groups with several rows of a
+# token, of queries or of keys and values; rows from any address
+MANY = [
+    (1024, 32, 8, 128, 128, "half", 0, False, "f16", "f16"), (1025, 32, 8, 128, 128, "half", 0, True, "f32", "f16"),
+    (2051, 32, 8, 64, 64, "interleaved", 0, False, "f32", "f32"), (2051, 5, 1, 256, 256, "half", 0, True, "f16", "f16"),
+    (1025, 5, 1, 64, 32, "half", 0, True, "f16", "f32"), (2051, 5, 1, 128, 0, "half", 0, False, "f32", "f16"),
+    (1030, 32, 8, 96, 96, "interleaved", 0, False, "f16", "f16"), (1025, 1, 16, 64, 64, "half", 0, False, "f16", "f16"),
+    (3001, 2, 1, 8, 8, "half", 0, True, "f32", "f32"), (1027, 40, 1, 136, 8, "half", 0, False, "f32", "f16"),
+    (1025, 5, 2, 77, 30, "half", 3, False, "f16", "f16"), (1025, 6, 1, 128, 64, "interleaved", 1, True, "f32", "f16"),
+    (2051, 1, 3, 255, 254, "half", 0, False, "f32", "f32"),
+]
+
+
+@pytest.mark.parametrize("tokens,hq,hk,dim,rot,layout,shift,per_head,src,dtype", MANY)
+def test_norms_and_appends_of_many_rows(tokens, hq, hk, dim, rot, layout, shift, per_head, src, dtype):
+    """Element by element; skipped rows -- the last ones among them -- and slots that no row names stay as they were."""
+    rng = np.random.default_rng([tokens, dim])
+    qkv = _rows(rng, tokens, hq + 2 * hk, dim, src, 0, shift)
+    q, k, v = qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:]
+    weights = [torch.from_numpy(rng.standard_normal((h, dim) if per_head else dim) * 0.2 + 1).to(DT[src]).cuda() for h in (hq, hk)]
+    table, kw, cos, sin = None, {}, None, None
+    if rot:
+        t, pos, cos, sin = _angles(rng, tokens, rot)
+        table, pos = nj.RotaryTable(torch.from_numpy(t).cuda(), layout), torch.from_numpy(pos).cuda()
+        kw = dict(positions=pos, table=table)
+
+    def expected(x, w):
+        y, b = normed(_np(x), _np(w), 1e-5)
+        return turned_with_bound(y, b, cos, sin, layout) if rot else (y, b)
+
+    want_q, bound_q = expected(q, weights[0])
+    out = _rows(rng, tokens, hq, dim, dtype, 0, shift)
+    nj.norm_rotary(q, weights[0], eps=1e-5, out=out, **kw)
+    _inside(_np(out), want_q, rounded(want_q, bound_q, dtype))
+    again = nj.norm_rotary(q, weights[0], eps=1e-5, **kw) if shift == 0 else None
+    if again is not None:
+        packed = qkv.clone()
+        nj.norm_rotary(packed[:, :hq], weights[0], eps=1e-5, out=packed[:, :hq], **kw)
+        assert torch.equal(packed[:, :hq], again) and torch.equal(packed[:, hq:], qkv[:, hq:])
+
+    page, pages = 7, -(-tokens // 7) + 3
+    flat = torch.full((2, pages * page * hk * dim + shift), 3.0, dtype=DT[dtype], device="cuda")
+    cache = nj.PagedCache(*(f[shift:].view(pages, hk, page, dim).transpose(1, 2) for f in flat))
+    slots = rng.permutation(pages * page)[:tokens].astype(np.int64)
+    slots[rng.random(tokens) < 0.05] = -1
+    slots[[tokens - 1, tokens - 3]], slots[5] = -1, pages * page
+    live = (slots >= 0) & (slots < pages * page)
+    out = torch.full((tokens, hq, dim), 3.0, dtype=DT[dtype], device="cuda")
+    nj.kv_append_slots(cache, torch.from_numpy(slots).cuda(), k, v, kw.get("positions"), table, q, out, nj.HeadNorm(*weights, eps=1e-5))
+    _inside(_np(out)[live], want_q[live], rounded(want_q, bound_q, dtype)[live])
+    assert bool((out.cpu()[~torch.from_numpy(live)] == 3.0).all())
+    want_k, bound_k = expected(k, weights[1])
+    got_k, got_v = (_np(c).reshape(pages * page, hk, dim) for c in (cache.k, cache.v))
+    _inside(got_k[slots[live]], want_k[live], rounded(want_k, bound_k, dtype)[live])
+    assert np.array_equal(got_v[slots[live]], _np(v.to(DT[dtype]))[live])
+    named = np.zeros(pages * page, bool)
+    named[slots[live]] = True
+    assert (got_k[~named] == 3.0).all() and (got_v[~named] == 3.0).all()
+
+
+@pytest.mark.parametrize("heads,dim,shift", [(1, 64, 0), (3, 128, 0), (8, 64, 0), (32, 128, 0), (5, 256, 0), (40, 8, 0), (6, 64, 1), (33, 16, 3)])
+@pytest.mark.parametrize("per_head", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_weight_gradients_to_the_last_row(heads, dim, shift, per_head, dtype):
+    """Whole numbers, so that a row left out or taken twice shows: x = +-1 and eps = 0 in dims of a power of two make r = 1 exactly
+    (the mean of the squares is 1), and dy whole and up to 8 makes every partial sum of g x r a whole number below 2^24."""
+    for tokens in (1, 2, 3, 31, 33, 127, 500, 1025, 4000, 4099, 8191):
+        if tokens * heads * dim > 1 << 24:
+            continue
+        rng = np.random.default_rng([tokens, heads])
+        x, dy = _rows(rng, tokens, heads, dim, dtype, 0, shift), _rows(rng, tokens, heads, dim, dtype, 0, shift)
+        x.copy_(torch.from_numpy(rng.choice([-1.0, 1.0], (tokens, heads, dim))))
+        dy.copy_(torch.from_numpy(rng.integers(-8, 9, (tokens, heads, dim)).astype(np.float64)))
+        w = torch.ones((heads, dim) if per_head else dim, device="cuda")
+        dw = nj.norm_rotary_grad(dy, x, w, eps=0.0)[1]
+        want = (dy.double() * x.double()).sum(0) if per_head else (dy.double() * x.double()).sum((0, 1))
+        assert torch.equal(dw.double(), want), tokens
 
 
 # ---------------------------------------------------------------- moves

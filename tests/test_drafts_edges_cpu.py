@@ -1,10 +1,14 @@
 """Host-side tests of what the entry points of a step of drafted tokens take and
 refuse beyond the plain cases (no GPU)."""
+import inspect
+import textwrap
+
 import numpy as np
 import pytest
 import torch
 
 import paper_2309_08978_amd as nj
+from tests import drafts_util
 from tests.drafts_util import LOGIT_COVER, logit_plan
 from tests.test_drafts_cpu import _arrays, _grad, _logits, _step
 
@@ -163,3 +167,86 @@ def test_counts_and_entries_fit_their_words():
     """One word a token: 15 bits of count above 16 of entry, the last bit for the prompt."""
     assert logit_plan(64, 128000, (1 << 15) - 1, (1 << 16) - 1).narrow
     assert not logit_plan(64, 128000, 1 << 15, 60).narrow and not logit_plan(64, 128000, 100, 1 << 16).narrow
+
+
+# ------------------------------------------------------------- mistakes planted in the plain forms
+
+def _mistaken(module, name, right, wrong):
+    """The function with a mistake in its source."""
+    source = textwrap.dedent(inspect.getsource(getattr(module, name)))
+    assert source.count(right) == 1
+    space = dict(vars(module))
+    exec(compile(source.replace(right, wrong), name, "exec"), space)
+    return space[name]
+
+
+@pytest.mark.parametrize("right,wrong", [
+    ("free.pop()", "free.pop(0)"),                                                   # pages from the bottom of the stack
+    ("for b, c in back]", "for b, c in back[::-1]]"),                                # pages given back in another order
+    ("(seen[p] if 0 <= p < i else set())", "({p} if 0 <= p < i else set())"),        # the parent only
+    ("0 <= p < i", "0 <= p"),                                                        # parents that are no earlier node
+    ("keep[b] + len(mine) - 1", "keep[b] + i"),                                      # positions by index, not by depth
+    ("place = keep[b] + i", "place = held[b] + i"),                                  # places behind what was held
+    ("c in range(need(keep[b] + added[b]), need(held[b]))", "c in range(need(keep[b]), need(held[b]))"),
+    ("need = lambda t: -(-t // page)", "need = lambda t: t // page + 1"),
+])
+def test_mistakes_in_a_step_show(right, wrong):
+    """On one of the batches of requests, some array differs (or the step falls over a page that is not there)."""
+    bad = _mistaken(drafts_util, "plain_step", right, wrong)
+    for seed in range(5):
+        rng = np.random.default_rng(seed)
+        n, page = 6, 4
+        held = [int(x) for x in rng.integers(0, 40, n)]
+        keep = [int(rng.integers(0, h + 1)) for h in held]
+        added = [int(x) for x in rng.integers(0, 20, n)]
+        parent = [int(rng.integers(-1, 12)) for _ in range(sum(added))]
+        ids = rng.permutation(200).tolist()
+        table = [[ids.pop() for _ in range(-(-h // page))] for h in held]
+        table = [row + [0] * (20 - len(row)) for row in table]
+        made = []
+        for f in (drafts_util.plain_step, bad):
+            t, s = [list(r) for r in table], ids[:60] + [0] * 60
+            try:
+                made.append((f(held, keep, added, t, s, 60, 120, page, sum(added), parent, 1), t, s))
+            except IndexError:
+                made.append(None)
+        if made[0] != made[1]:
+            return
+    raise AssertionError("no batch shows it")
+
+
+@pytest.mark.parametrize("right,wrong", [
+    ("tokens[max(0, prompt[r]) if prompt is not None else 0:]", "tokens"),           # counts over the prompt as well
+    ("z[r, t] > 0 else", "z[r, t] < 0 else"),                                        # penalty the wrong way round
+    ("seen = {t for t in tokens", "seen = {t for t in made"),                        # the prompt's tokens not penalised
+    ("for t, v in bias[r] if", "for t, v in bias[r][::-1] if"),                      # the first bias, not the last
+    ("z[r, t] - f * c - p", "z[r, t] - f * c - p * c"),                              # presence by count
+    ("min(max(length[r], 0), len(history[r]))", "len(history[r])"),                  # lengths not looked at
+    ("np.where(allowed, z, -math.inf)", "z"),
+])
+def test_mistakes_in_logits_show(right, wrong):
+    rng = np.random.default_rng(0)
+    rows, vocab = 3, 12
+    kw = dict(history=rng.integers(0, vocab, (rows, 9)).tolist(), length=[9, 5, 7], prompt=[3, 2, 4], repetition=[1.3] * 3, presence=[0.4] * 3,
+              frequency=[0.2] * 3, bias=[[(1, 0.5), (1, -0.5), (4, 2.0)]] * 3, allowed=rng.random((rows, vocab)) < 0.7)
+    x = rng.standard_normal((rows, vocab))
+    want, bound = drafts_util.plain_logits(x, **kw)
+    got, _ = _mistaken(drafts_util, "plain_logits", right, wrong)(x, **kw)
+    fine = np.isfinite(want) & np.isfinite(got)
+    assert (np.isfinite(want) != np.isfinite(got)).any() or (np.abs(got[fine] - want[fine]) > bound[fine]).any()
+
+
+@pytest.mark.parametrize("right,wrong", [
+    ("r * (h - u * m)", "r * h"),                                                    # without the mean term
+    ("turn(dy, cos, sin, layout, -1.0)", "turn(dy, cos, sin, layout, 1.0)"),         # turned on, not back
+    ("dw = (g * u).sum(0)", "dw = (h * u).sum(0)"),                                  # the weight's gradient times the weight
+    ("dw = (g * u).sum(0)", "dw = (g * x).sum(0)"),                                  # ... of rows that are not normed
+    ("dw = (g * u).sum(0)", "dw = (g * u)[:-1].sum(0)"),                             # ... without the last token
+    ("g * weight\n", "g\n"),
+])
+def test_mistakes_in_gradients_show(right, wrong):
+    rng = np.random.default_rng(0)
+    x, dy, w, a = rng.standard_normal((3, 2, 8)), rng.standard_normal((3, 2, 8)), rng.standard_normal(8), rng.uniform(0, 6, (3, 4))
+    dx, dw, bound, dwb = drafts_util.norm_grad(x, dy, w, 1e-5, np.cos(a), np.sin(a), "half")
+    bad_dx, bad_dw, _, _ = _mistaken(drafts_util, "norm_grad", right, wrong)(x, dy, w, 1e-5, np.cos(a), np.sin(a), "half")
+    assert (np.abs(bad_dx - dx) > bound).any() or (np.abs(bad_dw - dw) > dwb).any()

@@ -649,7 +649,7 @@ int nnjit_norm_rotary(const nnjit_rotary_table *rotary, int64_t tokens, int64_t 
  * (of each head on its own if w_head > 0, dw [heads][head_dim], else of all heads, dw
  * [head_dim]; fp32, overwritten).  dx has x's type and may be dy or x (same
  * strides and type), but not overlap them otherwise; dx or dw may be NULL.  Sums are added in an order
- * that depends on the sizes only.  The stream's scratch holds the partial
+ * that depends on sizes, strides and alignment only.  The stream's scratch holds the partial
  * sums of dw. */
 int nnjit_norm_rotary_grad(const nnjit_rotary_table *rotary, int64_t tokens, int64_t heads, int64_t head_dim, const int32_t *positions,
                            const void *weight, int64_t w_head, int w_dtype, float eps,

@@ -18,7 +18,9 @@ handles that a program keeps, and ``paged_step`` / ``kv_append_slots`` /
 ``adjust_logits`` for a step of drafted tokens, with ``PagePool``, ``PagedStep``,
 ``HeadNorm`` and ``LogitRules``.  All of these run on the tensors' GPU, on
 ``stream`` or, without one, on the stream that torch works on there; an output
-that they allocate belongs to that stream.
+that they allocate belongs to that stream.  None of them is recorded by autograd, whatever
+requires a gradient: gradients are calls of their own (``rotary`` with ``transpose``,
+``norm_rotary_grad``), for an autograd function of the program's to make.
 """
 from __future__ import annotations
 
@@ -1102,7 +1104,8 @@ def norm_rotary(x, weight, positions=None, table: Optional[RotaryTable] = None, 
     """x [tokens, heads, head_dim] with every head scaled to a mean square of 1,
     times weight ([head_dim] or [heads, head_dim]), turned by the angles of positions
     (int32 [tokens]; without a table: not turned).  ``out`` (fp32 or fp16,
-    allocated like x if None) may be x."""
+    allocated like x if None) may be x.  The result carries no graph: its gradients are
+    ``norm_rotary_grad``'s."""
     _torch()
     tokens, heads, dim, dev, pp, tp, w_head = _norm_operands(x, weight, positions, table)
     if out is None:

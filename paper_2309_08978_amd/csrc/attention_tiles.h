@@ -35,8 +35,8 @@
 // to 2^-35 of it).  The sum that divides takes them unrounded; rounding is
 // unbiased, and its share of the result's error is that of the result's own
 // rounding to fp16 (2.5 .. 2.9e-4 in all, against 2.1e-4 with exact weights).  (Two
-// parts, as in attention_rows.h, would be half as many products again where
-// products are what bounds.)
+// parts, as in attention_rows.h, are half as many products again: 16 drafted trees of 32 nodes 65 us
+// against 56, 64 nodes behind 65536 keys 130 against 100, for 2.1e-4 against 2.7e-4 and 2.6e-4.)
 //
 // Why 32 rows a wave: K and V of a step are read from LDS once per 32 rows, half
 // as often as with 16 x 16 products; the sums and queries of 64 rows would leave

@@ -14,14 +14,15 @@
 // multiple of eight: 64 lanes a head, an element or pair at a time.
 //
 // Bandwidth-bound once the vector instructions are few: 4096 tokens of 32 heads of 128 in fp16
-// forward 13.2 us, 5.1 TB/s, backward 19.5, 5.2 (a large copy: 5.0), plus 3.9 for the sum of the partial gradients;
-// 2774 rows of 32 query and 8 key and value heads appended, fp32 to fp16: 23.6 us, 4.6
-// TB/s; one token's append 3.1 on the device.  (With 230 instructions a row of eight elements a lane -- both layouts in one
+// forward 13.2 us, 5.1 TB/s, one pass after the other of its kind, and 15.3 between backward passes over other operands;
+// backward 19.9, 5.1 (a large copy: 5.0), plus 3.9 to 4.6 for the sum of the partial gradients;
+// 2930 rows (and 37 of padding) of 32 query and 8 key and value heads appended, fp32 to fp16: 23.5 us a call, 4.7
+// TB/s; one token's append 3.2 on the device.  (With 230 instructions a row of eight elements a lane -- both layouts in one
 // kernel, weights and angles by single loads -- forward took 31 us, backward 36.)
 //
 // The weight's gradient is summed in registers over the rows of a workgroup, then over
-// its groups through LDS, then by a second launch over workgroups: in an order
-// that the sizes alone decide.
+// its groups through LDS, then by a second launch over workgroups: in an order that
+// sizes, strides and alignment decide.
 #include <type_traits>
 
 #include "kcommon.h"

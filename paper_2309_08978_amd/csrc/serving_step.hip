@@ -19,9 +19,10 @@
 // its rows' and those as far before them as a mask reaches in LDS.
 //
 // All latency: lengths, sums, then page table and stack, one after the other.  Eight
-// sequences that decode a token each: 4.2 us on the device (a call: 5.3); 256 requests that come, go and
-// shrink, with trees of up to 48 tokens (9000 rows): 7.1.  (With the sums behind a barrier each, lengths read again
-// for every page and all workgroups seeing to pages and rows: 9.5.)
+// sequences that decode a token each: 4.2 us on the device (a call: 5.4); 256 requests that come, go and
+// shrink, with trees of up to 48 tokens (7181 rows): a call every 7.1, 7.6 on the device under a
+// profiler.  (With the sums behind a barrier each, lengths read again for every page and all
+// workgroups seeing to pages and rows: 9.5 a call.)
 #include "serving.h"
 
 namespace nnjit {

@@ -283,3 +283,77 @@ def test_every_kernel_of_logits(case, src, dst):
     _logits_case(rows, vocab, history, src, dst, gap=gap + 1, shift=1, length=length, seed=3)
     if src == dst:
         _logits_case(rows, vocab, history, src, dst, gap=gap, length=length, in_place=True, seed=4)
+
+
+# ------------------------------------------------------------- far and shared memory
+
+def _far(shape, stride, dtype):
+    """A tensor whose first dimension's stride passes 2^31 elements (memory of its own)."""
+    size = (shape[0] - 1) * stride + int(np.prod(shape[1:]))
+    inner = torch.empty(shape[1:], device="meta").stride()
+    return torch.as_strided(torch.empty(size, dtype=dtype, device="cuda"), shape, (stride, *inner))
+
+
+FAR = (1 << 31) + 64
+
+
+def test_caches_past_31_bits():
+    """Pages more than 2^31 elements apart: appends, moves and trees as on a cache whose pages lie together."""
+    g = torch.Generator("cuda").manual_seed(2)
+    r = lambda *shape: torch.randn(*shape, device="cuda", generator=g).half()  # noqa: E731
+    near = nj.PagedCache(r(3, 16, 2, 64), r(3, 16, 2, 64))
+    far = nj.PagedCache(*(_far((3, 16, 2, 64), FAR, torch.float16) for _ in range(2)))
+    far.k.copy_(near.k)
+    far.v.copy_(near.v)
+    k, v, q, w = r(9, 2, 64), r(9, 2, 64), r(9, 8, 64), r(64).float() + 2
+    slots, table = _i32([40, 41, 47, 0, 1, 30, 31, -1, 44]).long(), nj.rotary_table(64, 64)
+    pos, pages = torch.arange(9, dtype=torch.int32, device="cuda"), _i32([[2, 0, 1]])
+    mask = _i32([[(2 << i) - 1] for i in range(9)])
+    got = []
+    for cache in (near, far):
+        turned = nj.kv_append_slots(cache, slots, k, v, pos, table, q, torch.zeros_like(q), nj.HeadNorm(w, w))
+        batch = nj.PagedBatch(_i32([0, 9]), _i32([44]), pages, tokens=9)
+        out = nj.tree_attention(turned, cache, batch, mask)
+        nj.kv_move(cache, batch, _i32([[1, 3, 5, 8]]), _i32([4]))
+        got.append((turned, out, nj.tree_attention(turned, cache, batch, mask), cache.k.clone(), cache.v.clone()))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("dim", [64, 63])
+def test_rows_past_31_bits(dim):
+    """Tokens more than 2^31 elements apart: norms and their gradients, element by element as side by side."""
+    x, dy = torch.randn(3, 2, dim, device="cuda").half(), torch.randn(3, 2, dim, device="cuda").half()
+    w = torch.rand(dim, device="cuda") + 0.5
+    fx, fy = _far(x.shape, FAR, torch.float16), _far(x.shape, FAR, torch.float16)
+    fx.copy_(x)
+    fy.copy_(dy)
+    y, (dx, dw) = nj.norm_rotary(x, w), nj.norm_rotary_grad(dy, x, w)
+    assert torch.equal(nj.norm_rotary(fx, w), y)
+    got = nj.norm_rotary_grad(fy, fx, w, dx=fy)
+    assert torch.equal(got[0], dx) and torch.equal(got[1], dw)
+    assert torch.equal(nj.norm_rotary(fx, w, out=fx), y)
+
+
+def test_logits_past_31_bits():
+    x = torch.randn(3, 5000, device="cuda").half()
+    far = _far(x.shape, FAR, torch.float16)
+    far.copy_(x)
+    rules = nj.LogitRules(history=_i32([[1, 2, 4999]] * 3), frequency=torch.ones(3, device="cuda"), mask=_i32([[-5] * 157] * 3))
+    want = nj.adjust_logits(x, rules)
+    assert torch.equal(nj.adjust_logits(far, rules, far), want) and torch.equal(far, want)
+
+
+@pytest.mark.parametrize("dim,tokens", [(64, 40), (128, 1100), (77, 33)])
+def test_norms_of_shared_rows(dim, tokens):
+    """x and dy that are one row, one token or one head for all: as of their copies."""
+    table, w = nj.rotary_table(2000, dim // 2 * 2), torch.rand(3, dim, device="cuda") + 0.5
+    pos = torch.arange(tokens, dtype=torch.int32, device="cuda")
+    full = torch.randn(tokens, 3, dim, device="cuda")
+    for x in (full[:1].expand_as(full), full[:, :1].expand_as(full), full[:1, :1].expand_as(full)):
+        # (of the alignment that a copy has: it picks the kernel)
+        y, (dx, dw) = nj.norm_rotary(x.contiguous(), w, pos, table), nj.norm_rotary_grad(x.contiguous(), full, w, pos, table)
+        assert torch.equal(nj.norm_rotary(x, w, pos, table), y)
+        for a, b in zip(nj.norm_rotary_grad(x, full, w, pos, table), (dx, dw)):
+            assert torch.equal(a, b)
+        for a, b in zip(nj.norm_rotary_grad(full, x, w, pos, table), nj.norm_rotary_grad(full, x.contiguous(), w, pos, table)):
+            assert torch.equal(a, b)
